@@ -436,6 +436,105 @@ int ensi_diagonalise_weights(ensi_ctx *ctx, const ensi_gk *gk, const ensi_ct *A,
 int ensi_ccmm_av(ensi_ctx *ctx, const ensi_gk *rk, const ensi_gk *gk, const ensi_ct *Ad, const ensi_ct *V, int32_t s, int32_t period,
                  int32_t baby, int32_t g0, const ensi_pt *mask_head, ensi_ct *out, void *stream);
 
+/* ---- the decoder layer on clear activations ------------------------------------------------------------------
+ * The same ternary layer for activations that are not encrypted: what a decrypted result is compared with, what scales and
+ * levels are chosen by, and the path of requests that need no encryption.  Activations are device arrays of one ENSI_T_* type;
+ * products, sums, norms and softmax statistics are held in 32 bits and rounded once at the end.  Strides are in elements.
+ * These calls only enqueue kernels on the stream, allocate nothing and may be captured into a graph.  Calls of one context must
+ * not overlap on different streams (ensi_clear_attention has a workspace).
+ * What lies on the device (lengths, tables) cannot be checked by a call that does not wait: the kernels check it,
+ * leave out what is wrong and note it in the cache's status (ensi_clear_cache_status). */
+#define ENSI_T_F32 0
+#define ENSI_T_BF16 1
+#define ENSI_T_F16 2
+
+/* Root-mean-square norm with the residual's addition and an output in 8 bits.  Per row of d elements (1 <= d <= 32768):
+ *   h = x + residual, rounded to the type (h = x without a residual); p_i = h_i gain_i; most = max |p_i|
+ *   codes_i = p_i (127 (1 / most)) rounded to the nearest whole number, ties to even
+ *   scale = most / (127 sqrt(mean h^2 + eps)), so that codes_i scale is the normed value;  out_i = p_i / sqrt(mean h^2 + eps)
+ * A row of zeros has codes 0 and scale 0.  A row whose p holds an infinity or NaN, or whose sum of squares leaves the range of 32 bits, has
+ * codes 0, scale NaN and out NaN.  sum_out receives h (with a residual only); it may be x or residual itself, out may be x.  At least one of
+ * out and codes; codes and scales go together, codes [rows][d] and scales [rows] without gaps. */
+typedef struct ensi_clear_norm_args {
+    const void *x, *residual, *gain;  /* residual: NULL for none */
+    void *sum_out, *out;              /* NULL: not wanted */
+    int8_t *codes;
+    float *scales;
+    int64_t rows, x_stride, residual_stride, sum_stride, out_stride; /* strides between rows */
+    int32_t d, type;
+    float eps;
+    int32_t pad;
+} ensi_clear_norm_args;
+int ensi_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args *args, void *stream);
+
+/* Ternary weights of a clear product, packed once at two bits each.  W: host int8 [d][m], -1, 0 or 1; w_scales: host float
+ * [groups][m] for groups of `group` rows of W (a multiple of 64), or [1][m] with group = 0.  d <= 131072, m <= 2^24.  The weights may be freed while
+ * calls that read them are enqueued: the free waits. */
+typedef struct ensi_cw ensi_cw;
+int ensi_clear_weights_prepare(ensi_ctx *ctx, const int8_t *W, const float *w_scales, int32_t d, int32_t m, int32_t group, ensi_cw **cw);
+void ensi_clear_weights_free(ensi_cw *cw);
+/* out[t][i] = scales[t] sum_g w_scales[g][i] sum_{j in group g} W[j][i] codes[t][j].  codes: device int8 [rows][d], rows
+ * codes_stride apart; scales: device float [rows]; out: [rows][m] of `type`, rows out_stride apart.  The inner sums are exact. */
+int ensi_clear_matmul(ensi_ctx *ctx, const ensi_cw *cw, const int8_t *codes, int64_t codes_stride, const float *scales, void *out,
+                      int64_t out_stride, int64_t rows, int32_t type, void *stream);
+
+/* A paged cache of keys and values in 8 bits (e4m3, without infinities), in the caller's device memory, which has to outlive the handle:
+ * k, v: codes [pages][heads][page][dim], 16-byte aligned; k_scale, v_scale: float [pages][heads][page / 16], one power of two from 2^-64 to
+ * 2^120 for 16 tokens of a head.  page: a multiple of 16; dim: 64, 96, 128, 192 or 256. */
+typedef struct ensi_kv ensi_kv;
+int ensi_clear_cache_wrap(ensi_ctx *ctx, void *k, void *v, float *k_scale, float *v_scale, int32_t pages, int32_t heads, int32_t page,
+                          int32_t dim, ensi_kv **kv);
+void ensi_clear_cache_free(ensi_kv *kv);
+/* What the kernels met since the last call, as ENSI_KV_* bits; waits for the stream and clears them. */
+#define ENSI_KV_BAD_PAGE 1   /* a page number outside the cache: its tokens were left out */
+#define ENSI_KV_BAD_LENGTH 2 /* a sequence whose offsets or length do not fit the arguments: it was left out */
+int ensi_clear_cache_status(ensi_ctx *ctx, ensi_kv *kv, int32_t *bits, void *stream);
+
+/* Sequences of the two calls below: sequence i has the new tokens begin[i] .. begin[i + 1] - 1 of `tokens`, which follow the lengths[i] tokens
+ * that it has in the cache; position p of it lies in page table[i][p / page].  begin: device int32 [seqs + 1], lengths: device int32 [seqs],
+ * table: device int32 [seqs][table_width], rows table_stride apart.  max_new: no sequence has more new tokens. */
+typedef struct ensi_clear_seqs {
+    const int32_t *begin, *lengths, *table;
+    int64_t table_stride, tokens;
+    int32_t seqs, table_width, max_new, pad;
+} ensi_clear_seqs;
+
+/* Rotates queries and keys by their positions and stores the new keys and values.  cos, sin: device float [positions][rot / 2];
+ * the pair (a, b) of a head becomes (a cos - b sin, b cos + a sin): elements (j, j + rot / 2) of the first rot elements with ENSI_ROT_HALF,
+ * (2 j, 2 j + 1) with ENSI_ROT_NEIGHBOURS; rot: a multiple of 16, 0 <= rot <= dim (0: nothing is rotated).  The scale of a block of 16 tokens is the smallest
+ * power of two, from 2^-64 on, that brings its values to 448 at most, and never below the scale its earlier tokens have: these are rounded again where
+ * it grows.  Values that are infinite or NaN are stored as NaN and leave the scale alone.
+ * q, k, v: [tokens][heads of each][dim], head rows without gaps, tokens *_stride apart; q and q_out NULL: no queries; q_out may be q. */
+#define ENSI_ROT_HALF 0
+#define ENSI_ROT_NEIGHBOURS 1
+typedef struct ensi_clear_append_args {
+    ensi_clear_seqs s;
+    const void *q, *k, *v;
+    void *q_out;
+    const float *cos, *sin;
+    int64_t q_stride, q_out_stride, k_stride, v_stride;
+    int32_t q_heads, rot, positions, pairs, type, pad;
+} ensi_clear_append_args;
+int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *args, void *stream);
+
+/* Attention of the new tokens, whose keys and values are in the cache already, over their sequences: token at position p sees the positions up to p, with
+ * window > 0 the last `window` of them.  Query head h reads key head h / (q_heads / heads).  t = q k / sqrt(dim), with cap > 0 cap tanh(t / cap);
+ * weights: ENSI_SCORE_SOFTMAX softmax(t), ENSI_SCORE_SIGMOID 1 / (1 + exp(-(t + bias))), not normalised.  NaN in places that a token does not see
+ * has no part in its result.  q, out: [tokens][q_heads][dim] of ENSI_T_BF16 or ENSI_T_F16.  max_length: no sequence is longer, new tokens included
+ * (up to 2^30). */
+#define ENSI_SCORE_SOFTMAX 0
+#define ENSI_SCORE_SIGMOID 1
+typedef struct ensi_clear_attention_args {
+    ensi_clear_seqs s;
+    const void *q;
+    void *out;
+    int64_t q_stride, out_stride;
+    int32_t q_heads, type, score, window, max_length;
+    float cap, bias;
+    int32_t pad;
+} ensi_clear_attention_args;
+int ensi_clear_attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *args, void *stream);
+
 /* ---- transform alone (parity and measurement of the NTT kernels) -------- */
 /* data: device u64[n_limbs][N]; limb r uses prime index prime_idx[r] (host
  * int32[n_limbs]; 0..L-1 = q, L..L+K-1 = p).  In place.  Forward output order

@@ -6,6 +6,7 @@ is missing or a call fails, an exception is raised.
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -27,6 +28,8 @@ EXPORTED = [
     "ensi_sk_import", "ensi_sk_export", "ensi_pk_import", "ensi_pk_export", "ensi_gk_import", "ensi_gk_export", "ensi_gk_elements",
     "ensi_ct_checksum", "ensi_weights_prepare", "ensi_weights_free", "ensi_ternary_matmul_prepared", "ensi_rescale_ternary_matmul_prepared",
     "ensi_rotate_static", "ensi_matrix_rate_probe",
+    "ensi_clear_norm", "ensi_clear_weights_prepare", "ensi_clear_weights_free", "ensi_clear_matmul", "ensi_clear_cache_wrap", "ensi_clear_cache_free",
+    "ensi_clear_cache_status", "ensi_clear_append", "ensi_clear_attention",
 ]
 
 
@@ -54,9 +57,15 @@ def load():
             if name.endswith("_free") or name == "ensi_last_error":
                 continue
             getattr(lib, name).restype = ctypes.c_int
-        for name in ("ensi_ctx_free", "ensi_sk_free", "ensi_pk_free", "ensi_gk_free", "ensi_pt_free", "ensi_ct_free", "ensi_weights_free"):
+        for name in ("ensi_ctx_free", "ensi_sk_free", "ensi_pk_free", "ensi_gk_free", "ensi_pt_free", "ensi_ct_free", "ensi_weights_free", "ensi_clear_weights_free",
+                     "ensi_clear_cache_free"):
             getattr(lib, name).restype = None
             getattr(lib, name).argtypes = [ctypes.c_void_p]
+        # short calls in a decoding loop: plain numbers and packed structs, converted by their declared types
+        p, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+        lib.ensi_clear_norm.argtypes = [p, ctypes.c_char_p, p]
+        lib.ensi_clear_matmul.argtypes = [p, p, p, i64, p, p, i64, i64, i32, p]
+        lib.ensi_clear_append.argtypes = lib.ensi_clear_attention.argtypes = [p, p, ctypes.c_char_p, p]
         _lib = lib
     return _lib
 
@@ -72,6 +81,68 @@ def _i8(a, shape=None):
     if shape is not None and tuple(a.shape) != tuple(shape):
         raise EnsiError("expected int8 array of shape %s, got %s" % (shape, a.shape))
     return a
+
+# Packed argument structs of include/ensi.h: ensi_clear_norm_args, ensi_clear_append_args and ensi_clear_attention_args (the latter two begin with ensi_clear_seqs)
+_NORM = struct.Struct("<7Q5q2ifi")
+_APPEND = struct.Struct("<3Q2q4i6Q4q6i")
+_ATTENTION = struct.Struct("<3Q2q4i2Q2q5i2fi")
+_PAIRS = {"half": 0, "neighbours": 1}
+_SCORES = {"softmax": 0, "sigmoid": 1}
+_TORCH = None
+
+
+def _torch():
+    """(current device, its current stream as a number, types by name) from torch, which the caller of a clear_* method has loaded."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda at: torch.cuda.current_stream(at).cuda_stream)
+        names = {n: getattr(torch, n) for n in ("int8", "uint8", "int32", "float32", "bfloat16", "float16", "float8_e4m3fn")}
+        names["codes"] = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        _TORCH = (torch.cuda.current_device, stream, names)
+    return _TORCH
+
+
+def _torch_types():
+    return _torch()[2]
+
+
+def _type(name, kind):
+    code = _TORCH[2]["codes"].get(kind)
+    if code is None:
+        raise EnsiError("%s must be float32, bfloat16 or float16, not %s" % (name, kind))
+    return code
+
+
+def _rows(name, t, shape, kind, at):
+    """Address and stride between rows of a tensor whose rows have no gaps."""
+    if isinstance(kind, str):
+        kind = _TORCH[2][kind]
+    if t.shape != shape or t.dtype is not kind or t.get_device() != at:
+        raise EnsiError("%s must be %s %s on device %d, got %s %s on device %d" % (name, kind, tuple(shape), at, t.dtype, tuple(t.shape), t.get_device()))
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1 or len(strides) == 3 and strides[1] != shape[2] and shape[1] > 1:
+        raise EnsiError("%s must have rows without gaps, its strides are %s" % (name, strides))
+    return t.data_ptr(), strides[0]
+
+
+def _whole(name, t, shape, kind, at):
+    """Address of a tensor without gaps."""
+    if isinstance(kind, str):
+        kind = _TORCH[2][kind]
+    if t.shape != shape or t.dtype is not kind or t.get_device() != at or not t.is_contiguous():
+        raise EnsiError("%s must be %s %s without gaps on device %d, got %s %s on device %d" % (name, kind, tuple(shape), at, t.dtype, tuple(t.shape), t.get_device()))
+    return t.data_ptr()
+
+
+def _seqs(table, begin, lengths, tokens, max_new, at):
+    """The fields of ensi_clear_seqs."""
+    seqs = lengths.shape[0]
+    if len(table.shape) != 2:
+        raise EnsiError("table must be [seqs][pages]")
+    pt, st = _rows("table", table, (seqs, table.shape[1]), "int32", at)
+    return (_whole("begin", begin, (seqs + 1,), "int32", at), _whole("lengths", lengths, (seqs,), "int32", at), pt, st, tokens, seqs, table.shape[1],
+            tokens if max_new is None else max_new, 0)
 
 
 class Context:
@@ -472,6 +543,132 @@ class Context:
         self._check(self.lib.ensi_ntt(self.h, ctypes.c_void_p(int(device_ptr)), len(prime_idx), _ptr(prime_idx), int(inverse),
                                       ctypes.c_void_p(stream)))
 
+    # ---- the decoder layer on clear activations.  Arrays are torch tensors on the context's device; `stream` is torch's current one unless
+    # another is given.  Nothing here waits: what only the device can see (lengths, tables) is reported by ClearCache.check.
+    def _on(self, stream):
+        device, current_stream, _ = _torch()
+        at = device()
+        return at, current_stream(at) if stream is None else stream
+
+    def clear_norm(self, x, gain, residual=None, eps=1e-5, sum_out=None, out=None, codes=None, scales=None, stream=None):
+        """h = x + residual; p = h gain; codes = round(p 127 / max |p|) with their scale for each row, out = p / sqrt(mean h^2 + eps), sum_out = h.
+        x, residual, sum_out, out: [rows][d] with any stride between rows; codes int8 [rows][d], scales float32 [rows].  Without codes and out, the
+        former are made.  Returns (codes, scales)."""
+        at, stream = self._on(stream)
+        kind, shape = x.dtype, x.shape
+        if len(shape) != 2:
+            raise EnsiError("x must be [rows][d]")
+        rows, d = shape
+        if codes is None and out is None:
+            codes = x.new_empty((rows, d), dtype=_torch_types()["int8"])
+        if codes is not None and scales is None:
+            scales = x.new_empty((rows,), dtype=_torch_types()["float32"])
+        px, sx = _rows("x", x, shape, kind, at)
+        pr, sr = (None, 0) if residual is None else _rows("residual", residual, shape, kind, at)
+        ps, ss = (None, 0) if sum_out is None else _rows("sum_out", sum_out, shape, kind, at)
+        po, so = (None, 0) if out is None else _rows("out", out, shape, kind, at)
+        args = _NORM.pack(px, pr or 0, _whole("gain", gain, (d,), kind, at), ps or 0, po or 0,
+                          0 if codes is None else _whole("codes", codes, shape, "int8", at),
+                          0 if scales is None else _whole("scales", scales, (rows,), "float32", at), rows, sx, sr, ss, so, d, _type("x", kind), eps, 0)
+        rc = self.lib.ensi_clear_norm(self.h, args, stream)
+        if rc:
+            self._check(rc)
+        return codes, scales
+
+    def clear_weights_prepare(self, W, w_scales, group=0):
+        """Ternary weights (int8 [d][m], host) with float scales [groups][m] for groups of `group` rows ([1][m] or [m] with group 0), packed on the device."""
+        W = np.ascontiguousarray(W)
+        if W.ndim != 2 or W.dtype != np.int8:
+            raise EnsiError("W must be int8 [d][m]")
+        d, m = W.shape
+        group = int(group)
+        w_scales = np.ascontiguousarray(w_scales, dtype=np.float32)
+        if w_scales.size != (-(-d // group) if group > 0 else 1) * m or w_scales.shape[-1] != m:
+            raise EnsiError("w_scales must be float [groups][m]")
+        cw = ctypes.c_void_p()
+        self._check(self.lib.ensi_clear_weights_prepare(self.h, _ptr(W), _ptr(w_scales), int(d), int(m), group, ctypes.byref(cw)))
+        return ClearWeights(self, cw, d, m, group)
+
+    def clear_matmul(self, weights, codes, scales, out=None, dtype=None, stream=None):
+        """out[t] = scales[t] (codes[t] W w_scales); codes int8 [rows][d] with any stride between rows, scales float32 [rows], out [rows][m] of a floating type
+        (made with `dtype` if not given)."""
+        at, stream = self._on(stream)
+        shape = codes.shape
+        if len(shape) != 2 or shape[1] != weights.d:
+            raise EnsiError("codes must be [rows][%d]" % weights.d)
+        rows = shape[0]
+        if out is None:
+            out = codes.new_empty((rows, weights.m), dtype=dtype)
+        kind = out.dtype
+        pc, sc = _rows("codes", codes, shape, "int8", at)
+        po, so = _rows("out", out, (rows, weights.m), kind, at)
+        rc = self.lib.ensi_clear_matmul(self.h, weights.h, pc, sc, _whole("scales", scales, (rows,), "float32", at), po, so, rows, _type("out", kind), stream)
+        if rc:
+            self._check(rc)
+        return out
+
+    def clear_cache(self, k, v, k_scale, v_scale):
+        """A paged cache over the caller's tensors: k, v uint8 or float8_e4m3fn [pages][heads][page][dim], k_scale, v_scale float32 [pages][heads][page / 16]."""
+        at, _ = self._on(0)
+        if k.dim() != 4:
+            raise EnsiError("k and v must be [pages][heads][page][dim]")
+        pages, heads, page, dim = k.shape
+        if k.element_size() != 1 or k.dtype not in (_torch_types()["uint8"], _torch_types()["float8_e4m3fn"]):
+            raise EnsiError("k and v must be uint8 or float8_e4m3fn")
+        scales = (pages, heads, page // 16)
+        ptrs = [_whole(n, t, k.shape, k.dtype, at) for n, t in (("k", k), ("v", v))] + [_whole(n, t, scales, "float32", at) for n, t in (("k_scale", k_scale), ("v_scale", v_scale))]
+        kv = ctypes.c_void_p()
+        self._check(self.lib.ensi_clear_cache_wrap(self.h, *(ctypes.c_void_p(p) for p in ptrs), int(pages), int(heads), int(page), int(dim), ctypes.byref(kv)))
+        return ClearCache(self, kv, (k, v, k_scale, v_scale))
+
+    def clear_append(self, cache, table, begin, lengths, k, v, cos, sin, q=None, q_out=None, pairs="half", max_new=None, stream=None):
+        """Rotates q [tokens][heads][dim] into q_out (made if not given) and k by their positions, and stores k and v [tokens][kv heads][dim] in the cache.
+        Sequence i has the tokens begin[i] .. begin[i + 1] - 1 behind lengths[i] cached ones; its pages are table[i] (all int32).  cos, sin: float32
+        [positions][rot / 2], or None for no rotation.  max_new: the most new tokens of a sequence (default: all of them).  Returns q_out."""
+        at, stream = self._on(stream)
+        tokens, kind = k.shape[0], k.dtype
+        shape = (tokens, cache.heads, cache.dim)
+        pk, sk = _rows("k", k, shape, kind, at)
+        pv, sv = _rows("v", v, shape, kind, at)
+        pq = po = sq = so = heads = 0
+        if q is not None:
+            heads = q.shape[1] if len(q.shape) == 3 else 0
+            if q_out is None:
+                q_out = q.new_empty(q.shape)
+            pq, sq = _rows("q", q, (tokens, heads, cache.dim), kind, at)
+            po, so = _rows("q_out", q_out, (tokens, heads, cache.dim), kind, at)
+        rot = positions = pc = ps = 0
+        if cos is not None:
+            if len(cos.shape) != 2:
+                raise EnsiError("cos and sin must be [positions][rot / 2]")
+            positions, rot = cos.shape[0], 2 * cos.shape[1]
+            pc, ps = _whole("cos", cos, cos.shape, "float32", at), _whole("sin", sin, cos.shape, "float32", at)
+        args = _APPEND.pack(*_seqs(table, begin, lengths, tokens, max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), _PAIRS[pairs], _type("k", kind), 0)
+        rc = self.lib.ensi_clear_append(self.h, cache.h, args, stream)
+        if rc:
+            self._check(rc)
+        return q_out
+
+    def clear_attention(self, cache, table, begin, lengths, q, out=None, cap=0.0, window=0, score="softmax", bias=0.0, max_new=None, max_length=None, stream=None):
+        """Causal attention of the new tokens q [tokens][heads][dim] (stored by clear_append before) over their sequences: scores q k / sqrt(dim), capped by
+        cap tanh(. / cap), within a window, through a softmax or as sigmoid(. + bias).  lengths as for clear_append (without the new tokens); max_length: the
+        longest sequence with its new tokens (default: what the table holds).  Returns out."""
+        at, stream = self._on(stream)
+        shape, kind = q.shape, q.dtype
+        if len(shape) != 3 or shape[2] != cache.dim:
+            raise EnsiError("q must be [tokens][heads][%d]" % cache.dim)
+        if out is None:
+            out = q.new_empty(shape)
+        pq, sq = _rows("q", q, shape, kind, at)
+        po, so = _rows("out", out, shape, kind, at)
+        if max_length is None:
+            max_length = min(table.shape[1] * cache.page, 1 << 30)
+        args = _ATTENTION.pack(*_seqs(table, begin, lengths, shape[0], max_new, at), pq, po, sq, so, shape[1], _type("q", kind), _SCORES[score], window, max_length, cap, bias, 0)
+        rc = self.lib.ensi_clear_attention(self.h, cache.h, args, stream)
+        if rc:
+            self._check(rc)
+        return out
+
     # ---- timers
     def profile_enable(self, on=True):
         self._check(self.lib.ensi_profile_enable(self.h, int(on)))
@@ -540,3 +737,28 @@ class Ciphertexts(_Handle):
         out = np.empty((n, 2, limbs, self.ctx.N), dtype=np.uint64)
         self.ctx._check(self.ctx.lib.ensi_ct_export(self.ctx.h, self.h, _ptr(out)))
         return out
+
+
+class ClearWeights(_Handle):
+    """Packed ternary weights of a clear product."""
+
+    def __init__(self, ctx, h, d, m, group):
+        super().__init__(ctx, h, "ensi_clear_weights_free", n=m)
+        self.d, self.m, self.group = int(d), int(m), group
+
+
+class ClearCache(_Handle):
+    """A paged 8-bit cache over tensors of the caller, which it keeps."""
+
+    def __init__(self, ctx, h, tensors):
+        super().__init__(ctx, h, "ensi_clear_cache_free")
+        self.tensors = tensors
+        self.pages, self.heads, self.page, self.dim = (int(x) for x in tensors[0].shape)
+
+    def check(self, stream=None):
+        """Waits for the stream and raises if a call since the last check met a page or a length that does not fit (and left it out)."""
+        bits = ctypes.c_int32()
+        _, stream = self.ctx._on(stream)
+        self.ctx._check(self.ctx.lib.ensi_clear_cache_status(self.ctx.h, self.h, ctypes.byref(bits), ctypes.c_void_p(stream)))
+        if bits.value:
+            raise EnsiError("the cache met %s: left out" % " and ".join(t for b, t in ((1, "page numbers outside it"), (2, "sequences that do not fit the arguments")) if bits.value & b))

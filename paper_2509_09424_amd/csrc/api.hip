@@ -340,6 +340,7 @@ extern "C" void ensi_ctx_free(ensi_ctx *ctx) {
     if (ctx->ws_mt) (void)hipFree(ctx->ws_mt);
     if (ctx->ws_rep) (void)hipFree(ctx->ws_rep);
     if (ctx->ws_rtmp) (void)hipFree(ctx->ws_rtmp);
+    if (ctx->ws_clear) (void)hipFree(ctx->ws_clear);
     for (MatmulPlan *p : ctx->plans) free_plan(p);
     for (StageSlot &sl : ctx->stage) {
         if (sl.host) (void)hipHostFree(sl.host);

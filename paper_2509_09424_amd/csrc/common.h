@@ -309,6 +309,7 @@ struct ensi_ctx {
     u64 sampler_ctr = 0;
     void *static_scratch = nullptr;  // this device's copy of the statically linked workspace (api_static.hip)
     size_t static_scratch_bytes = 0;
+    float *ws_clear = nullptr;   // partial results of attention on clear activations: fixed size, made with the first cache
     StageSlot stage[ENSI_STAGE_SLOTS];
     int stage_next = 0;
     int n_cu = 0;                // compute units of the context's device (0: not queried yet)
