@@ -17,13 +17,15 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function", "-Wno-unused-parameter",
 ]
+# flags of single sources: matrix instructions that keep their sums in ordinary registers, where every tile's softmax works on them
+SOURCE_FLAGS = {"clear_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def compile_one(src, out, extra=(), verbose=False):
     src, _, ring = src.partition(":")
     if ring:
         extra = list(extra) + ["-DKS_RING=" + ring]
-    cmd = [HIPCC] + FLAGS + list(extra) + ["-I" + os.path.join(CSRC, "inc"), "-c", os.path.join(CSRC, src), "-o", out]
+    cmd = [HIPCC] + FLAGS + SOURCE_FLAGS.get(src, []) + list(extra) + ["-I" + os.path.join(CSRC, "inc"), "-c", os.path.join(CSRC, src), "-o", out]
     if verbose:
         print(" ".join(cmd))
     subprocess.check_call(cmd)

@@ -46,6 +46,7 @@ struct Wide<ENSI_T_BF16> {
         return u.v;
     }
     static __device__ __forceinline__ f32x4 mfma16(vec a, vec b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16 mfma32(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 template <>
 struct Wide<ENSI_T_F16> {
@@ -62,6 +63,7 @@ struct Wide<ENSI_T_F16> {
         return u.v;
     }
     static __device__ __forceinline__ f32x4 mfma16(vec a, vec b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16 mfma32(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
 // Bytes (k, j) of four words of keys to words of places: e[j] holds byte j of d[0..3]
@@ -77,10 +79,10 @@ __device__ __forceinline__ void transpose4(u32 (&d)[4]) {
 __device__ __forceinline__ u32 nan_bytes(u32 w) { return (w & 0x7f7f7f7f) + 0x01010101; }
 
 // The score t of a product q c, in units of the exponent: softmax log2 e t, sigmoid t log2 e + bias log2 e
-template <int SCORE>
+template <int SCORE, bool CAP>
 __device__ __forceinline__ float score_of(float qc, float scale, const AttentionView &a) {
     float t = qc * (a.factor * scale);
-    if (a.cap > 0) {
+    if (CAP) {
         // cap tanh(t / cap) = cap (1 - 2 / (1 + exp(2 t / cap)))
         const float e = __builtin_amdgcn_exp2f(t * a.cap_inv);  // cap_inv = 2 log2 e / cap
         t = a.cap - 2.0f * a.cap * __builtin_amdgcn_rcpf(1.0f + e);
@@ -89,16 +91,16 @@ __device__ __forceinline__ float score_of(float qc, float scale, const Attention
     return SCORE == ENSI_SCORE_SIGMOID ? t + a.bias : t;
 }
 
-// Where the rows of a tile of 16 (query tokens times the heads that share a key head) look: keys [lo, hi), lo rounded down to a tile of 32.
+// Where the rows of a tile (query tokens times the heads that share a key head, token by token) look: from key lo, rounded down to a tile of 32, to key `last`.
 struct RowTile {
     int rows;             // of the tile; 0: none
     int first, last;      // positions of its first and last row
-    int lo, tiles;
+    int lo, tiles;        // tiles of 32 keys
 };
-__device__ __forceinline__ RowTile row_tile(const SeqPart &part, int tile, int group, int window) {
+__device__ __forceinline__ RowTile row_tile(const SeqPart &part, int row0, int most, int group, int window) {
     RowTile r;
-    const int row0 = 16 * tile, rows = part.count * group;
-    r.rows = max(0, min(16, rows - row0));
+    const int rows = part.count * group;
+    r.rows = max(0, min(most, rows - row0));
     r.first = part.ctx + row0 / group;
     r.last = part.ctx + (row0 + max(r.rows, 1) - 1) / group;
     r.lo = window > 0 ? max(0, r.first - window + 1) & ~31 : 0;
@@ -139,7 +141,7 @@ __device__ __forceinline__ float half_lift(float from, float to) { return from =
 // Keys split over waves and workgroups: few rows, long caches.  A workgroup has one tile of 16 rows of a key head and `split` of its keys; its four
 // waves take tiles of 32 keys in turn, straight from memory into registers, and are joined in LDS; parts of several workgroups are joined by
 // k_clear_attention_join.  The cache has to be read once: bound by memory.
-template <int TYPE, int DIM, int SCORE>
+template <int TYPE, int DIM, int SCORE, bool CAP>
 __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, int split_tiles) {
     typedef typename Elem<TYPE>::type T;
     typedef Wide<TYPE> W;
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, g = lane / 16;
     const int seq = blockIdx.z, head = blockIdx.x / a.row_tiles, tile = blockIdx.x % a.row_tiles, split = blockIdx.y;
     const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
-    const RowTile rt = row_tile(part, tile, a.group, a.window);
+    const RowTile rt = row_tile(part, 16 * tile, 16, a.group, a.window);
     const int tile0 = split * split_tiles, tile1 = min(tile0 + split_tiles, rt.tiles);
     if (rt.rows == 0 || tile0 >= tile1) return;
     const int row = 16 * tile + min(n, rt.rows - 1), token = part.first + row / a.group, pos = part.ctx + row / a.group;
@@ -180,46 +182,53 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
             }
         }
         const int turns = min(32, (tile1 - batch + 3) / 4);
+        // keys: lane (n, g) has places DIM / 4 g .. of key n; values: places PIECE n .. of keys 4 g .. 4 g + 3 of either half
+        constexpr int WORDS = (PIECE + REST + 3) / 4;
+        struct Codes {
+            u32x2 k[2][STEPS];
+            u32 v[2][WORDS][4];
+        };
+        const int k_at = n * DIM + g * (DIM / 4), v_at = 4 * g * DIM + PIECE * n, rest_at = 4 * g * DIM + MAIN + REST * n;
+        const auto fetch = [&](Codes &to, int i) {
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                // a wave's base and a lane's offset of 32 bits: no registers for 64-bit addresses
+                const unsigned char *p = a.kv.k + (int64_t)__builtin_amdgcn_readlane(my_block, 2 * i + h) * (KV_BLOCK * DIM);
+#pragma unroll
+                for (int s = 0; s < STEPS; s++) to.k[h][s] = *(const u32x2 *)(p + (u32)(k_at + 8 * s));
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const unsigned char *p = a.kv.v + (int64_t)__builtin_amdgcn_readlane(my_block, 2 * i + h) * (KV_BLOCK * DIM);
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    typedef u32 piece __attribute__((ext_vector_type(PIECE / 4)));
+                    const piece v = *(const piece *)(p + (u32)(v_at + r * DIM));
+#pragma unroll
+                    for (int w = 0; w < PIECE / 4; w++) to.v[h][w][r] = v[w];
+                    if (REST == 4) to.v[h][WORDS - 1][r] = *(const u32 *)(p + (u32)(rest_at + r * DIM));
+                    if (REST == 2) to.v[h][WORDS - 1][r] = *(const unsigned short *)(p + (u32)(rest_at + r * DIM));
+                }
+            }
+        };
         for (int i = 0; i < turns; i++) {
             const int key0 = rt.lo + 32 * (batch + 4 * i);
-            int block[2], good[2];
+            int good[2];
             float ks[2], vs[2];
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                block[h] = __builtin_amdgcn_readlane(my_block, 2 * i + h);
                 good[h] = __builtin_amdgcn_readlane(my_good, 2 * i + h);
                 ks[h] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), 2 * i + h));
                 vs[h] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 2 * i + h));
             }
-            // keys: lane (n, g) has places DIM / 4 g .. of key n
-            u32x2 kc[2][STEPS];
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const unsigned char *p = a.kv.k + ((int64_t)block[h] * KV_BLOCK + n) * DIM + g * (DIM / 4);
-#pragma unroll
-                for (int s = 0; s < STEPS; s++) kc[h][s] = *(const u32x2 *)(p + 8 * s);
-            }
-            // values: lane (n, g) has places PIECE n .. of keys 4 g .. 4 g + 3 of either half
-            constexpr int WORDS = (PIECE + REST + 3) / 4;
-            u32 vc[2][WORDS][4];
-#pragma unroll
-            for (int h = 0; h < 2; h++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const unsigned char *p = a.kv.v + ((int64_t)block[h] * KV_BLOCK + 4 * g + r) * DIM;
-                    typedef u32 piece __attribute__((ext_vector_type(PIECE / 4)));
-                    const piece v = *(const piece *)(p + PIECE * n);
-#pragma unroll
-                    for (int w = 0; w < PIECE / 4; w++) vc[h][w][r] = v[w];
-                    if (REST == 4) vc[h][WORDS - 1][r] = *(const u32 *)(p + MAIN + 4 * n);
-                    if (REST == 2) vc[h][WORDS - 1][r] = *(const unsigned short *)(p + MAIN + 2 * n);
-                }
+            Codes now;
+            fetch(now, i);
             f32x4 qk[2];
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 qk[h] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-                for (int s = 0; s < STEPS; s++) qk[h] = W::mfma16(W::widen(kc[h][s][0], kc[h][s][1]), q[s], qk[h]);
+                for (int s = 0; s < STEPS; s++) qk[h] = W::mfma16(W::widen(now.k[h][s][0], now.k[h][s][1]), q[s], qk[h]);
             }
             float u[2][4];
             const bool masked = key0 + 31 > rt.first || (a.window > 0 && key0 <= rt.last - a.window) || !good[0] || !good[1];
@@ -231,7 +240,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
             for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    u[h][r] = score_of<SCORE>(qk[h][r], ks[h], a);
+                    u[h][r] = score_of<SCORE, CAP>(qk[h][r], ks[h], a);
                     if (SCORE == ENSI_SCORE_SIGMOID) u[h][r] = vs[h] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[h][r]));
                 }
             if (masked) {
@@ -279,35 +288,46 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
 #pragma unroll
                 for (int x = 0; x < WORDS; x++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++) nans |= nan_bytes(vc[h][x][r]);
-            const bool any_nan = __any((nans & 0x80808080) != 0);
-            f16x8 visible;
-            if (any_nan) {
+                    for (int r = 0; r < 4; r++) nans |= nan_bytes(now.v[h][x][r]);
+            if (__any((nans & 0x80808080) != 0)) {
+                // rare: NaN goes to the places of the rows that see its token, and its code becomes 0
+                f16x8 visible;
 #pragma unroll
                 for (int h = 0; h < 2; h++)
 #pragma unroll
                     for (int r = 0; r < 4; r++) visible[4 * h + r] = sees(h, r) ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+                for (int x = 0; x < WORDS; x++) {
+                    u32 ones[2][4];  // 1.0 in e4m3 where the code is NaN
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+#pragma unroll
+                        for (int r = 0; r < 4; r++) {
+                            const u32 hit = (nan_bytes(now.v[h][x][r]) & 0x80808080) >> 7;
+                            ones[h][r] = hit * 0x38;
+                            now.v[h][x][r] &= ~(hit * 0xff);
+                        }
+                        transpose4(ones[h]);
+                    }
+#pragma unroll
+                    for (int b = 0; b < 4; b++) {
+                        if (4 * x + b >= TILES) continue;
+                        const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(Wide<ENSI_T_F16>::widen(ones[0][b], ones[1][b]), visible, (f32x4){0, 0, 0, 0}, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; r++)
+                            if (hit[r] > 0) st.o[4 * x + b][r] = __builtin_nanf("");
+                    }
+                }
             }
 #pragma unroll
             for (int x = 0; x < WORDS; x++) {
 #pragma unroll
-                for (int h = 0; h < 2; h++) transpose4(vc[h][x]);
+                for (int h = 0; h < 2; h++) transpose4(now.v[h][x]);
 #pragma unroll
                 for (int b = 0; b < 4; b++) {
                     const int j = 4 * x + b;
                     if (j >= TILES) continue;
-                    u32 c0 = vc[0][x][b], c1 = vc[1][x][b];
-                    if (any_nan) {
-                        const u32 n0 = nan_bytes(c0) & 0x80808080, n1 = nan_bytes(c1) & 0x80808080;
-                        // 0x38 is 1.0 in e4m3: ones where the code is NaN
-                        const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(Wide<ENSI_T_F16>::widen((n0 >> 7) * 0x38, (n1 >> 7) * 0x38), visible, (f32x4){0, 0, 0, 0}, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 4; r++)
-                            if (hit[r] > 0) st.o[j][r] = __builtin_nanf("");
-                        c0 &= ~((n0 >> 7) * 0xff);
-                        c1 &= ~((n1 >> 7) * 0xff);
-                    }
-                    const f16x8 v = Wide<ENSI_T_F16>::widen(c0, c1);
+                    const f16x8 v = Wide<ENSI_T_F16>::widen(now.v[0][x][b], now.v[1][x][b]);
                     st.o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p.v, st.o[j], 0, 0, 0);
                     if (TYPE == ENSI_T_F16) st.o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p_lo.v, st.o[j], 0, 0, 0);
                 }
@@ -367,41 +387,357 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
     }
 }
 
-// Joins the parts of a row: a workgroup of DIM threads to a row.
+// Joins the parts of a row: a workgroup to a row.  The references first, a thread to a part, then the outputs: DIM / 4 threads to a part, as many
+// parts side by side as there are threads, added in LDS.
+#define JOIN_MAX 256  // parts of a row
 template <int TYPE, int DIM, int SCORE>
-__global__ __launch_bounds__(DIM) void k_clear_attention_join(AttentionView a, int split_tiles) {
+__global__ __launch_bounds__(256) void k_clear_attention_join(AttentionView a, int split_tiles) {
     typedef typename Elem<TYPE>::type T;
-    const int seq = blockIdx.z, head = blockIdx.x / a.row_tiles, tile = blockIdx.x % a.row_tiles, n = blockIdx.y, d = threadIdx.x;
+    constexpr int QUADS = DIM / 4, SLICES = 256 / QUADS;
+    const int seq = blockIdx.z, head = blockIdx.x / a.row_tiles, tile = blockIdx.x % a.row_tiles, n = blockIdx.y, t = threadIdx.x;
     const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
-    const RowTile rt = row_tile(part, tile, a.group, a.window);
+    const RowTile rt = row_tile(part, 16 * tile, 16, a.group, a.window);
     if (n >= rt.rows || rt.tiles <= split_tiles) return;
     const int splits = (rt.tiles + split_tiles - 1) / split_tiles;
     const float *ws = a.ws + ((int64_t)seq * gridDim.x + blockIdx.x) * a.splits * (16 * DIM + 32);
-    float m = -__builtin_inff();
-    for (int s = 0; s < splits; s++) m = fmaxf(m, ws[(int64_t)s * (16 * DIM + 32) + 16 * DIM + n]);
-    if (m == -__builtin_inff()) m = 0;
-    float o = 0, l = 0;
-    for (int s = 0; s < splits; s++) {
-        const float *p = ws + (int64_t)s * (16 * DIM + 32);
-        const float h = half_lift(p[16 * DIM + n], m);
-        l += p[16 * DIM + 16 + n] * h * h;
-        o += p[n * DIM + d] * (h * h);
+    __shared__ float factor[JOIN_MAX], top[4], sums[4];
+    __shared__ f32x4 parts[SLICES][QUADS];
+    const int quad = t % QUADS, slice = t / QUADS;
+    float m = -__builtin_inff(), l = 0;
+    if (t < splits) {
+        m = ws[(int64_t)t * (16 * DIM + 32) + 16 * DIM + n];
+        l = ws[(int64_t)t * (16 * DIM + 32) + 16 * DIM + 16 + n];
     }
+    float most = m;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
+    if (t % 64 == 0) top[t / 64] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    if (most == -__builtin_inff()) most = 0;
+    const float h = half_lift(m, most);
+    if (t < splits) factor[t] = h * h;
+    l = t < splits ? l * h * h : 0;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) l += __shfl_xor(l, k);
+    if (t % 64 == 0) sums[t / 64] = l;
+    __syncthreads();
+    f32x4 o = {0, 0, 0, 0};
+    if (slice < SLICES) {
+#pragma unroll 4
+        for (int s = slice; s < splits; s += SLICES) {
+            const f32x4 v = *(const f32x4 *)(ws + (int64_t)s * (16 * DIM + 32) + n * DIM + 4 * quad);
+            const float f = factor[s];
+#pragma unroll
+            for (int i = 0; i < 4; i++) o[i] = __builtin_fmaf(v[i], f, o[i]);
+        }
+        parts[slice][quad] = o;
+    }
+    __syncthreads();
+    if (t >= QUADS) return;
+    l = sums[0] + sums[1] + sums[2] + sums[3];
+    const float f = SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(most) : l == 0 ? 0.0f : 1.0f / l;
+    o = (f32x4){0, 0, 0, 0};
+    for (int s = 0; s < SLICES; s++) o += parts[s][t];
     const int row = 16 * tile + n, token = part.first + row / a.group, q_head = head * a.group + row % a.group;
-    const float f = SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(m) : l == 0 ? 0.0f : 1.0f / l;
-    ((T *)a.out)[(int64_t)token * a.out_stride + (int64_t)q_head * DIM + d] = (T)(o * f);
+    typedef T quad_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    quad_t w;
+#pragma unroll
+    for (int i = 0; i < 4; i++) w[i] = (T)(o[i] * f);
+    *(quad_t *)((T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM + 4 * t) = w;
 }
 
+// Rows split over waves, keys shared: many rows (prompts).  A workgroup has 128 rows of a key head, 32 to a wave, and walks their keys in tiles of 64.
+// A wave fetches one block of 16 keys and values of a tile (the codes of the next tile are under way while one is computed), widens them to 16 bits and puts them into
+// LDS, values transposed and in the order in which the score's registers hold their keys; two buffers, one barrier a tile.  The matrix cores,
+// LDS reads (32 KB a wave and tile at 128 places) and the softmax's vector instructions are about equally busy.
+template <int DIM>
+struct RowsLds {
+    static constexpr int KEYS = 64, K_ROW = DIM * 2 + 16, V_ROW = KEYS * 2 + 16;  // bytes; 16 more keep the rows of a fragment on different banks
+    static constexpr int K_BYTES = KEYS * K_ROW, V_BYTES = DIM * V_ROW, BUFFER = K_BYTES + V_BYTES;
+    static constexpr int BUFFERS = 2 * BUFFER <= 80 * 1024 ? 2 : 1;
+};
+
+template <int TYPE, int DIM, int SCORE, bool CAP>
+__global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_rows(AttentionView a) {
+    typedef typename Elem<TYPE>::type T;
+    typedef Wide<TYPE> W;
+    typedef typename W::vec vec;
+    typedef RowsLds<DIM> L;
+    constexpr int STEPS = DIM / 16, TILES = DIM / 32, ITEMS = (DIM / 2 + 63) / 64;  // of the values: 8 keys x 4 places
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ int has_nan[2][4];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 32, half = lane / 32;
+    const int seq = blockIdx.z, head = blockIdx.x % a.kv.heads, tile = a.row_tiles - 1 - blockIdx.x / a.kv.heads;  // the longest rows first
+    const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
+    const RowTile all = row_tile(part, 128 * tile, 128, a.group, a.window);
+    if (all.rows == 0) return;
+    const int row0 = 128 * tile + 32 * wave;
+    const RowTile mine = row_tile(part, row0, 32, a.group, a.window);  // rows may be 0: such a wave only fetches
+    const int row = min(row0 + n, part.count * a.group - 1), token = part.first + row / a.group, pos = part.ctx + row / a.group;
+    const int q_head = head * a.group + row % a.group;
+    vec q[STEPS];
+    {
+        typedef vec loose __attribute__((aligned(2)));
+        const T *p = (const T *)a.q + (int64_t)token * a.q_stride + (int64_t)q_head * DIM + 8 * half;
+#pragma unroll
+        for (int s = 0; s < STEPS; s++) q[s] = *(const loose *)(p + 16 * s);
+    }
+    f32x16 o[TILES];
+#pragma unroll
+    for (int j = 0; j < TILES; j++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) o[j][r] = 0;
+    float st_m = -__builtin_inff(), st_l = 0;
+    const int tiles = (all.last + 1 - all.lo + 63) / 64;
+    // what 16 tiles need to know of their blocks of 16 keys: lane l has block l % 4 of tile l / 4
+    int my_block = 0, my_good = 0;
+    float my_k = 1, my_v = 1;
+    const auto look_up = [&](int first) {
+        const int key = all.lo + 64 * first + 16 * lane;
+        my_block = my_good = 0;
+        my_k = my_v = 1;
+        if (key <= all.last) {
+            const int page = a.s.table[seq * a.s.table_stride + key / a.kv.page];
+            if (page >= 0 && page < a.kv.pages) {
+                my_block = ((page * (int64_t)a.kv.heads + head) * a.kv.page + key % a.kv.page) / KV_BLOCK;
+                my_good = 1;
+                my_k = a.kv.ks[my_block];
+                my_v = fmaxf(a.kv.vs[my_block], 0x1p-64f);
+            } else
+                atomicOr(a.kv.status, ENSI_KV_BAD_PAGE);
+        }
+    };
+    // a wave's block of a tile: keys, DIM / 4 bytes of row lane / 4; values, items (half of the block's keys, 4 places)
+    u32x2 kc[DIM / 32];
+    u32 vc[ITEMS][8];
+    const auto fetch = [&](int t) {
+        const int64_t block = __builtin_amdgcn_readlane(my_block, 4 * (t % 16) + wave);
+        const unsigned char *k = a.kv.k + block * (KV_BLOCK * DIM), *v = a.kv.v + block * (KV_BLOCK * DIM);
+#pragma unroll
+        for (int i = 0; i < DIM / 32; i++) kc[i] = *(const u32x2 *)(k + (u32)(lane * (DIM / 4) + 8 * i));
+#pragma unroll
+        for (int i = 0; i < ITEMS; i++) {
+            const int item = lane + 64 * i, h = item / (DIM / 4), places = 4 * (item % (DIM / 4));
+            if (DIM / 2 % 64 == 0 || item < DIM / 2) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) vc[i][e] = *(const u32 *)(v + (u32)((4 * h + 8 * (e / 4) + e % 4) * DIM + places));
+            }
+        }
+    };
+    const auto put = [&](int buffer) {
+        unsigned char *at = lds + (L::BUFFERS == 2 ? buffer * L::BUFFER : 0);
+        unsigned char *k = at + (16 * wave + lane / 4) * L::K_ROW + (lane % 4) * (DIM / 2);
+#pragma unroll
+        for (int i = 0; i < DIM / 32; i++) *(vec *)(k + 16 * i) = W::widen(kc[i][0], kc[i][1]);
+        u32 nans = 0;
+#pragma unroll
+        for (int i = 0; i < ITEMS; i++) {
+            const int item = lane + 64 * i, h = item / (DIM / 4), places = 4 * (item % (DIM / 4));
+            if (DIM / 2 % 64 == 0 || item < DIM / 2) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const u32 hit = nan_bytes(vc[i][e]) & 0x80808080;
+                    nans |= hit;
+                }
+                u32 x[2][4];
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e / 4][e % 4] = vc[i][e];
+                transpose4(x[0]);
+                transpose4(x[1]);
+#pragma unroll
+                for (int j = 0; j < 4; j++) *(f16x8 *)(at + L::K_BYTES + (places + j) * L::V_ROW + 32 * wave + 16 * h) = Wide<ENSI_T_F16>::widen(x[0][j], x[1][j]);
+            }
+        }
+        const bool any = __any(nans != 0);
+        if (any) {
+            // rare: NaN becomes 0 in LDS; who reads the tile looks its places up
+#pragma unroll
+            for (int i = 0; i < ITEMS; i++) {
+                const int item = lane + 64 * i, h = item / (DIM / 4), places = 4 * (item % (DIM / 4));
+                if (DIM / 2 % 64 == 0 || item < DIM / 2) {
+                    u32 x[2][4];
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e / 4][e % 4] = vc[i][e] & ~(((nan_bytes(vc[i][e]) & 0x80808080) >> 7) * 0xff);
+                    transpose4(x[0]);
+                    transpose4(x[1]);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) *(f16x8 *)(at + L::K_BYTES + (places + j) * L::V_ROW + 32 * wave + 16 * h) = Wide<ENSI_T_F16>::widen(x[0][j], x[1][j]);
+                }
+            }
+        }
+        if (lane == 0) has_nan[buffer][wave] = any;
+    };
+    look_up(0);
+    fetch(0);
+    put(0);
+    __syncthreads();
+    for (int t = 0; t < tiles; t++) {
+        const int buffer = t % 2, key0 = all.lo + 64 * t;
+        int good[4], block[4];
+        float ks[4], vs[4];
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            good[b] = __builtin_amdgcn_readlane(my_good, 4 * (t % 16) + b);
+            block[b] = __builtin_amdgcn_readlane(my_block, 4 * (t % 16) + b);
+            ks[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), 4 * (t % 16) + b));
+            vs[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 4 * (t % 16) + b));
+        }
+        if (t + 1 < tiles) {
+            if ((t + 1) % 16 == 0) look_up(t + 1);
+            fetch(t + 1);
+        }
+        // a wave whose rows see nothing of the tile goes on
+        if (mine.rows > 0 && key0 <= mine.last && (a.window <= 0 || key0 + 63 > mine.first - a.window)) {
+            const unsigned char *at = lds + (L::BUFFERS == 2 ? buffer * L::BUFFER : 0);
+            f32x16 qk[2];
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+#pragma unroll
+                for (int r = 0; r < 16; r++) qk[x][r] = 0;
+#pragma unroll
+                for (int s = 0; s < STEPS; s++) qk[x] = W::mfma32(*(const vec *)(at + (32 * x + n) * L::K_ROW + 32 * s + 16 * half), q[s], qk[x]);
+            }
+            // register r of half x, block b = 2 x + r / 8: key 16 b + 8 (r % 8 / 4) + 4 half + r % 4
+            const auto sees = [&](int b, int e) {
+                const int key = key0 + 16 * b + 8 * (e / 4) + 4 * half + e % 4;
+                return good[b] && key <= pos && (a.window <= 0 || key > pos - a.window);
+            };
+            const bool masked = key0 + 63 > mine.first || (a.window > 0 && key0 <= mine.last - a.window) || !(good[0] & good[1] & good[2] & good[3]);
+            float u[4][8], most = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+#pragma unroll
+            for (int b = 0; b < 4; b++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    float v = qk[b / 2][8 * (b % 2) + e];
+                    // softmax without a cap: the product itself, its factor enters with the exponent
+                    if (CAP || SCORE == ENSI_SCORE_SIGMOID) v = score_of<SCORE, CAP>(v, ks[b], a);
+                    if (SCORE == ENSI_SCORE_SIGMOID) v = vs[b] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v));
+                    u[b][e] = v;
+                }
+            if (masked) {
+#pragma unroll
+                for (int b = 0; b < 4; b++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        if (!sees(b, e)) u[b][e] = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+            }
+            float factor[4];
+#pragma unroll
+            for (int b = 0; b < 4; b++) {
+                factor[b] = CAP || SCORE == ENSI_SCORE_SIGMOID ? 1.0f : a.factor * ks[b];
+                float top = fmaxf(fmaxf(fmaxf(u[b][0], u[b][1]), fmaxf(u[b][2], u[b][3])), fmaxf(fmaxf(u[b][4], u[b][5]), fmaxf(u[b][6], u[b][7])));
+                if (SCORE == ENSI_SCORE_SOFTMAX) top = __builtin_fmaf(top, factor[b], __builtin_amdgcn_logf(vs[b]));
+                most = fmaxf(most, top);
+            }
+            most = fmaxf(most, __shfl_xor(most, 32));
+            if (SCORE == ENSI_SCORE_SIGMOID) most = fmaxf(__builtin_amdgcn_logf(most), -120.0f);
+            const float m = fmaxf(st_m, most), base = m == -__builtin_inff() ? 0.0f : m;
+            const float lift = half_lift(st_m, base);
+            st_m = m;
+            if (__any(lift != 1.0f)) {
+                const float f = lift * lift;
+#pragma unroll
+                for (int j = 0; j < TILES; j++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) o[j][r] *= f;
+                st_l = st_l * lift * lift;
+            }
+            union Weights {
+                _Float16 e[8];
+                f16x8 v;
+            } p[4];
+            const float unit = SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(-base) : 0;
+#pragma unroll
+            for (int b = 0; b < 4; b++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    float w;
+                    if (SCORE == ENSI_SCORE_SIGMOID)
+                        w = u[b][e] * unit;
+                    else {
+                        w = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], -base));
+                        st_l += w;
+                        w *= vs[b];
+                    }
+                    p[b].e[e] = (_Float16)w;
+                }
+            if (has_nan[buffer][0] | has_nan[buffer][1] | has_nan[buffer][2] | has_nan[buffer][3]) {
+                // rare: NaN to the places of the rows that see its token, from the codes themselves
+                for (int b = 0; b < 4; b++) {
+                    f16x8 visible;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) visible[e] = sees(b, e) ? (_Float16)1.0f : (_Float16)0.0f;
+                    const unsigned char *v = a.kv.v + (int64_t)block[b] * (KV_BLOCK * DIM);
+#pragma unroll
+                    for (int j = 0; j < TILES; j++) {
+                        f16x8 ones;
+#pragma unroll
+                        for (int e = 0; e < 8; e++) ones[e] = (v[(8 * (e / 4) + 4 * half + e % 4) * DIM + 32 * j + n] & 0x7f) == 0x7f ? (_Float16)1.0f : (_Float16)0.0f;
+                        f32x16 hit;
+#pragma unroll
+                        for (int r = 0; r < 16; r++) hit[r] = 0;
+                        hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(ones, visible, hit, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 16; r++)
+                            if (hit[r] > 0) o[j][r] = __builtin_nanf("");
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < TILES; j++)
+#pragma unroll
+                for (int b = 0; b < 4; b++)
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 32 * b + 16 * half), p[b].v, o[j], 0, 0, 0);
+        }
+        if (L::BUFFERS == 1) __syncthreads();  // everybody has read this tile
+        if (t + 1 < tiles) put((t + 1) % 2);
+        __syncthreads();
+    }
+    st_l += __shfl_xor(st_l, 32);
+    if (row0 + n >= part.count * a.group) return;
+    const float f = SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(st_m) : st_l == 0 ? 0.0f : 1.0f / st_l;
+    T *out = (T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM;
+#pragma unroll
+    for (int j = 0; j < TILES; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            typedef T quad __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            quad w;
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = (T)(o[j][4 * e + i] * f);
+            *(quad *)(out + 32 * j + 8 * e + 4 * half) = w;
+        }
+}
+
+#ifndef USE_ROWS
+#define USE_ROWS (blocks >= 256)
+#endif
 template <int TYPE, int DIM, int SCORE>
 static void attention_go(ensi_ctx *ctx, AttentionView v, hipStream_t st) {
     const int heads = v.kv.heads;
+    const int64_t blocks = (int64_t)v.s.seqs * heads * (((int64_t)v.s.max_new * v.group + 127) / 128);
+    if (USE_ROWS) {
+        v.row_tiles = (int)(((int64_t)v.s.max_new * v.group + 127) / 128);
+        ScopedTimer timer(ctx, "k_clear_attention", st);
+        const auto go = [&](auto kernel) {
+            constexpr int bytes = RowsLds<DIM>::BUFFERS * RowsLds<DIM>::BUFFER;
+            (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+            hipLaunchKernelGGL(kernel, dim3(heads * v.row_tiles, 1, v.s.seqs), dim3(256), bytes, st, v);
+        };
+        if (v.cap > 0) go(k_clear_attention_rows<TYPE, DIM, SCORE, true>);
+        else go(k_clear_attention_rows<TYPE, DIM, SCORE, false>);
+        return;
+    }
     v.row_tiles = (int)(((int64_t)v.s.max_new * v.group + 15) / 16);
     const int64_t base = (int64_t)v.s.seqs * heads * v.row_tiles;
     // the most tiles of 32 keys that a tile of rows looks at: those of its window, begun within a tile and ended within one
     const int tokens = min(v.s.max_new, 15 / v.group + 2);
     const int span = v.window > 0 ? (int)min((int64_t)v.max_length, (int64_t)v.window + tokens - 1 + 31) : v.max_length;
     const int tiles = (span + 31) / 32;
-    int splits = (int)min((int64_t)(tiles + 3) / 4, max((int64_t)1, 2048 / base));
+    // as many parts as give a wave 8 tiles, which evens out sequences of different lengths; more where the CUs would stand idle
+    int splits = (int)min((int64_t)(tiles + 3) / 4, max((int64_t)(tiles + 31) / 32, 768 / base));
+    splits = min(max(splits, 1), JOIN_MAX);
     const int64_t room = (int64_t)CLEAR_WS_FLOATS / (base * (16 * DIM + 32));
     if (splits > room) splits = (int)max((int64_t)1, room);
     int split_tiles = (tiles + splits - 1) / splits;
@@ -411,12 +747,13 @@ static void attention_go(ensi_ctx *ctx, AttentionView v, hipStream_t st) {
     const dim3 grid(heads * v.row_tiles, splits, v.s.seqs);
     {
         ScopedTimer timer(ctx, "k_clear_attention", st);
-        hipLaunchKernelGGL((k_clear_attention_keys<TYPE, DIM, SCORE>), grid, dim3(256), 0, st, v, split_tiles);
+        if (v.cap > 0) hipLaunchKernelGGL((k_clear_attention_keys<TYPE, DIM, SCORE, true>), grid, dim3(256), 0, st, v, split_tiles);
+        else hipLaunchKernelGGL((k_clear_attention_keys<TYPE, DIM, SCORE, false>), grid, dim3(256), 0, st, v, split_tiles);
     }
     if (splits == 1) return;
     ScopedTimer timer(ctx, "k_clear_attention_join", st);
     const int rows = (int)min((int64_t)16, (int64_t)v.s.max_new * v.group);
-    hipLaunchKernelGGL((k_clear_attention_join<TYPE, DIM, SCORE>), dim3(heads * v.row_tiles, rows, v.s.seqs), dim3(DIM), 0, st, v, split_tiles);
+    hipLaunchKernelGGL((k_clear_attention_join<TYPE, DIM, SCORE>), dim3(heads * v.row_tiles, rows, v.s.seqs), dim3(256), 0, st, v, split_tiles);
 }
 
 template <int TYPE, int SCORE>
