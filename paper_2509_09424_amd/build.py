@@ -18,7 +18,7 @@ FLAGS = [
     "-Wall", "-Wno-unused-function", "-Wno-unused-parameter",
 ]
 # flags of single sources: matrix instructions that keep their sums in ordinary registers, where every tile's softmax works on them
-SOURCE_FLAGS = {"clear_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+SOURCE_FLAGS = {"clear_matmul.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "clear_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def compile_one(src, out, extra=(), verbose=False):

@@ -15,6 +15,13 @@ static int current_device(ensi_ctx *ctx) {
     if (hipGetDevice(&cur) != hipSuccess || cur != ctx->device) ENSI_FAIL(ctx, ENSI_E_HIP, "the context's device is not current");
     return ENSI_OK;
 }
+// The workspace of the clear calls, made with the first cache or the first weights of a context.
+static int clear_workspace(ensi_ctx *ctx) {
+    if (ctx->ws_clear) return ENSI_OK;
+    hipError_t e = ctx->pool->alloc((void **)&ctx->ws_clear, CLEAR_WS_FLOATS * sizeof(float));
+    if (e != hipSuccess) ENSI_FAIL(ctx, ENSI_E_NOMEM, "clear workspace: device allocation failed: %s", hipGetErrorString(e));
+    return ENSI_OK;
+}
 static int type_size(int type) { return type == ENSI_T_F32 ? 4 : type == ENSI_T_BF16 || type == ENSI_T_F16 ? 2 : 0; }
 
 // Rows of `width` elements, `stride` apart, as a range of addresses
@@ -57,6 +64,7 @@ extern "C" int ensi_clear_weights_prepare(ensi_ctx *ctx, const int8_t *W, const 
     if (d < 1 || d > 131072 || m < 1 || m > (1 << 24)) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear weights: %d x %d (up to 131072 x 2^24)", d, m);
     if (group < 0 || group % 64) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear weights: groups of %d rows (a multiple of 64, or 0)", group);
     if (int rc = current_device(ctx)) return rc;
+    if (int rc = clear_workspace(ctx)) return rc;
     const int groups = group ? (int)(((int64_t)d + group - 1) / group) : 1;
     ensi_cw *cw = new (std::nothrow) ensi_cw();
     if (!cw) ENSI_FAIL(ctx, ENSI_E_NOMEM, "no host memory");
@@ -64,15 +72,15 @@ extern "C" int ensi_clear_weights_prepare(ensi_ctx *ctx, const int8_t *W, const 
     cw->d = d;
     cw->m = m;
     cw->group = group;
-    cw->k_chunks = (d + 255) / 256;
-    cw->m_tiles = (m + 15) / 16;
-    cw->m_pad = 16 * cw->m_tiles;
+    cw->units = (d + 127) / 128;
+    cw->m_pad = (m + 127) & ~127;  // whole workgroups of either kernel's tiles
+    cw->m_tiles = cw->m_pad / 16;
     // on the default stream, which the copies and the wait below order
     DevBuf raw;
     int wrong = 0;
     hipError_t e = raw.alloc(ctx, (size_t)d * m + 8 + sizeof(int));
     int *bad = (int *)((char *)raw.p + (((size_t)d * m + 7) & ~(size_t)7));
-    if (e == hipSuccess) e = ctx->pool->alloc((void **)&cw->w, (size_t)cw->m_tiles * cw->k_chunks * 1024);
+    if (e == hipSuccess) e = ctx->pool->alloc((void **)&cw->w, (size_t)cw->m_tiles * cw->units * 512);
     if (e == hipSuccess) e = ctx->pool->alloc((void **)&cw->scales, (size_t)groups * cw->m_pad * sizeof(float));
     if (e != hipSuccess) {
         ensi_clear_weights_free(cw);
@@ -83,7 +91,7 @@ extern "C" int ensi_clear_weights_prepare(ensi_ctx *ctx, const int8_t *W, const 
     if (e == hipSuccess) e = hipMemset(cw->scales, 0, (size_t)groups * cw->m_pad * sizeof(float));
     if (e == hipSuccess) e = hipMemcpy2D(cw->scales, (size_t)cw->m_pad * 4, w_scales, (size_t)m * 4, (size_t)m * 4, groups, hipMemcpyHostToDevice);
     if (e == hipSuccess) {
-        launch_clear_pack((const int8_t *)raw.p, d, m, cw->k_chunks, cw->m_tiles, cw->w, bad, nullptr);
+        launch_clear_pack((const int8_t *)raw.p, d, m, cw->units, cw->m_tiles, cw->w, bad, nullptr);
         e = hipGetLastError();
     }
     if (e == hipSuccess) e = hipMemcpy(&wrong, bad, sizeof wrong, hipMemcpyDeviceToHost);
@@ -134,10 +142,7 @@ extern "C" int ensi_clear_cache_wrap(ensi_ctx *ctx, void *k, void *v, float *k_s
         for (int j = 0; j < i; j++)
             if (a[i].meets(a[j])) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear cache: its arrays overlap");
     if (int rc = current_device(ctx)) return rc;
-    if (!ctx->ws_clear) {
-        hipError_t e = ctx->pool->alloc((void **)&ctx->ws_clear, CLEAR_WS_FLOATS * sizeof(float));
-        if (e != hipSuccess) ENSI_FAIL(ctx, ENSI_E_NOMEM, "clear cache: device allocation failed: %s", hipGetErrorString(e));
-    }
+    if (int rc = clear_workspace(ctx)) return rc;
     ensi_kv *kv = new (std::nothrow) ensi_kv();
     if (!kv) ENSI_FAIL(ctx, ENSI_E_NOMEM, "no host memory");
     kv->ctx = ctx;

@@ -77,9 +77,9 @@ __device__ __forceinline__ SeqPart seq_part(const ensi_clear_seqs &s, int seq, i
 struct ensi_cw {
     ensi_ctx *ctx;
     int d, m, group;
-    int k_chunks, m_tiles;  // chunks of 256 rows, tiles of 16 columns
-    u32 *w = nullptr;       // [m_tiles][k_chunks][64 lanes][4]: two bits a weight, see k_clear_matmul
-    float *scales = nullptr;  // [groups][m_pad], m_pad = 16 m_tiles
+    int units, m_tiles;     // units of 128 rows, tiles of 16 columns
+    u32 *w = nullptr;       // two bits a weight, 512 bytes a tile and unit: k_clear_pack
+    float *scales = nullptr;  // [groups][m_pad], m_pad = 16 m_tiles, a multiple of 128
     int m_pad;
 };
 struct ensi_kv {
@@ -91,10 +91,10 @@ struct ensi_kv {
 void launch_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args &a, hipStream_t st);
 void launch_clear_matmul(ensi_ctx *ctx, const ensi_cw *cw, const int8_t *codes, int64_t codes_stride, const float *scales, void *out,
                          int64_t out_stride, int64_t rows, int type, hipStream_t st);
-void launch_clear_pack(const int8_t *d_W, int d, int m, int k_chunks, int m_tiles, u32 *w, int *bad, hipStream_t st);
+void launch_clear_pack(const int8_t *d_W, int d, int m, int units, int m_tiles, u32 *w, int *bad, hipStream_t st);
 void launch_clear_append(ensi_ctx *ctx, const KvView &kv, const ensi_clear_append_args &a, hipStream_t st);
 void launch_clear_attention(ensi_ctx *ctx, const KvView &kv, const ensi_clear_attention_args &a, hipStream_t st);
 
-// Partial results of keys split over workgroups (ensi_clear_attention).  One allocation of fixed size, made with the first cache of a context
-// and never moved, so that calls allocate nothing and a captured graph's pointers stay good.
+// Workspace of the clear calls: partial results of keys split over workgroups (attention), aligned copies of codes (matmul).  One allocation of fixed size, made
+// with the first cache or weights of a context and never moved, so that calls allocate nothing and a captured graph's pointers stay good.
 #define CLEAR_WS_FLOATS ((size_t)16 << 20)
