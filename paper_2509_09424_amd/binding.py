@@ -96,10 +96,12 @@ def _torch():
     global _TORCH
     if _TORCH is None:
         import torch
+        torch.cuda.current_device()  # initialises
+        device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda at: torch.cuda.current_stream(at).cuda_stream)
         names = {n: getattr(torch, n) for n in ("int8", "uint8", "int32", "float32", "bfloat16", "float16", "float8_e4m3fn")}
         names["codes"] = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-        _TORCH = (torch.cuda.current_device, stream, names)
+        _TORCH = (device, stream, names)
     return _TORCH
 
 
@@ -114,24 +116,23 @@ def _type(name, kind):
     return code
 
 
+def _refuse(name, t, shape, kind, at):
+    raise EnsiError("%s must be %s %s without gaps in its rows on device %d, got %s %s with strides %s on device %d" % (
+        name, kind, tuple(shape), at, t.dtype, tuple(t.shape), t.stride(), t.get_device()))
+
+
 def _rows(name, t, shape, kind, at):
     """Address and stride between rows of a tensor whose rows have no gaps."""
-    if isinstance(kind, str):
-        kind = _TORCH[2][kind]
-    if t.shape != shape or t.dtype is not kind or t.get_device() != at:
-        raise EnsiError("%s must be %s %s on device %d, got %s %s on device %d" % (name, kind, tuple(shape), at, t.dtype, tuple(t.shape), t.get_device()))
     strides = t.stride()
-    if strides[-1] != 1 and shape[-1] > 1 or len(strides) == 3 and strides[1] != shape[2] and shape[1] > 1:
-        raise EnsiError("%s must have rows without gaps, its strides are %s" % (name, strides))
+    if t.shape != shape or t.dtype is not kind or t.get_device() != at or strides[-1] != 1 and shape[-1] > 1 or len(strides) == 3 and strides[1] != shape[2] and shape[1] > 1:
+        _refuse(name, t, shape, kind, at)
     return t.data_ptr(), strides[0]
 
 
 def _whole(name, t, shape, kind, at):
     """Address of a tensor without gaps."""
-    if isinstance(kind, str):
-        kind = _TORCH[2][kind]
     if t.shape != shape or t.dtype is not kind or t.get_device() != at or not t.is_contiguous():
-        raise EnsiError("%s must be %s %s without gaps on device %d, got %s %s on device %d" % (name, kind, tuple(shape), at, t.dtype, tuple(t.shape), t.get_device()))
+        _refuse(name, t, shape, kind, at)
     return t.data_ptr()
 
 
@@ -140,8 +141,9 @@ def _seqs(table, begin, lengths, tokens, max_new, at):
     seqs = lengths.shape[0]
     if len(table.shape) != 2:
         raise EnsiError("table must be [seqs][pages]")
-    pt, st = _rows("table", table, (seqs, table.shape[1]), "int32", at)
-    return (_whole("begin", begin, (seqs + 1,), "int32", at), _whole("lengths", lengths, (seqs,), "int32", at), pt, st, tokens, seqs, table.shape[1],
+    kind, width = _TORCH[2]["int32"], table.shape[1]
+    pt, st = _rows("table", table, (seqs, width), kind, at)
+    return (_whole("begin", begin, (seqs + 1,), kind, at), _whole("lengths", lengths, (seqs,), kind, at), pt, st, tokens, seqs, width,
             tokens if max_new is None else max_new, 0)
 
 
@@ -546,7 +548,7 @@ class Context:
     # ---- the decoder layer on clear activations.  Arrays are torch tensors on the context's device; `stream` is torch's current one unless
     # another is given.  Nothing here waits: what only the device can see (lengths, tables) is reported by ClearCache.check.
     def _on(self, stream):
-        device, current_stream, _ = _torch()
+        device, current_stream, _ = _TORCH or _torch()
         at = device()
         return at, current_stream(at) if stream is None else stream
 
@@ -568,8 +570,8 @@ class Context:
         ps, ss = (None, 0) if sum_out is None else _rows("sum_out", sum_out, shape, kind, at)
         po, so = (None, 0) if out is None else _rows("out", out, shape, kind, at)
         args = _NORM.pack(px, pr or 0, _whole("gain", gain, (d,), kind, at), ps or 0, po or 0,
-                          0 if codes is None else _whole("codes", codes, shape, "int8", at),
-                          0 if scales is None else _whole("scales", scales, (rows,), "float32", at), rows, sx, sr, ss, so, d, _type("x", kind), eps, 0)
+                          0 if codes is None else _whole("codes", codes, shape, _TORCH[2]["int8"], at),
+                          0 if scales is None else _whole("scales", scales, (rows,), _TORCH[2]["float32"], at), rows, sx, sr, ss, so, d, _type("x", kind), eps, 0)
         rc = self.lib.ensi_clear_norm(self.h, args, stream)
         if rc:
             self._check(rc)
@@ -600,9 +602,9 @@ class Context:
         if out is None:
             out = codes.new_empty((rows, weights.m), dtype=dtype)
         kind = out.dtype
-        pc, sc = _rows("codes", codes, shape, "int8", at)
+        pc, sc = _rows("codes", codes, shape, _TORCH[2]["int8"], at)
         po, so = _rows("out", out, (rows, weights.m), kind, at)
-        rc = self.lib.ensi_clear_matmul(self.h, weights.h, pc, sc, _whole("scales", scales, (rows,), "float32", at), po, so, rows, _type("out", kind), stream)
+        rc = self.lib.ensi_clear_matmul(self.h, weights.h, pc, sc, _whole("scales", scales, (rows,), _TORCH[2]["float32"], at), po, so, rows, _type("out", kind), stream)
         if rc:
             self._check(rc)
         return out
@@ -616,7 +618,7 @@ class Context:
         if k.element_size() != 1 or k.dtype not in (_torch_types()["uint8"], _torch_types()["float8_e4m3fn"]):
             raise EnsiError("k and v must be uint8 or float8_e4m3fn")
         scales = (pages, heads, page // 16)
-        ptrs = [_whole(n, t, k.shape, k.dtype, at) for n, t in (("k", k), ("v", v))] + [_whole(n, t, scales, "float32", at) for n, t in (("k_scale", k_scale), ("v_scale", v_scale))]
+        ptrs = [_whole(n, t, k.shape, k.dtype, at) for n, t in (("k", k), ("v", v))] + [_whole(n, t, scales, _torch_types()["float32"], at) for n, t in (("k_scale", k_scale), ("v_scale", v_scale))]
         kv = ctypes.c_void_p()
         self._check(self.lib.ensi_clear_cache_wrap(self.h, *(ctypes.c_void_p(p) for p in ptrs), int(pages), int(heads), int(page), int(dim), ctypes.byref(kv)))
         return ClearCache(self, kv, (k, v, k_scale, v_scale))
@@ -642,7 +644,8 @@ class Context:
             if len(cos.shape) != 2:
                 raise EnsiError("cos and sin must be [positions][rot / 2]")
             positions, rot = cos.shape[0], 2 * cos.shape[1]
-            pc, ps = _whole("cos", cos, cos.shape, "float32", at), _whole("sin", sin, cos.shape, "float32", at)
+            f32 = _TORCH[2]["float32"]
+            pc, ps = _whole("cos", cos, cos.shape, f32, at), _whole("sin", sin, cos.shape, f32, at)
         args = _APPEND.pack(*_seqs(table, begin, lengths, tokens, max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), _PAIRS[pairs], _type("k", kind), 0)
         rc = self.lib.ensi_clear_append(self.h, cache.h, args, stream)
         if rc:
