@@ -95,6 +95,13 @@ void launch_clear_pack(const int8_t *d_W, int d, int m, int units, int m_tiles, 
 void launch_clear_append(ensi_ctx *ctx, const KvView &kv, const ensi_clear_append_args &a, hipStream_t st);
 void launch_clear_attention(ensi_ctx *ctx, const KvView &kv, const ensi_clear_attention_args &a, hipStream_t st);
 
+// Raises a kernel's limit of dynamic LDS, once in a context.
+inline void clear_lds(ensi_ctx *ctx, const void *kernel, int bytes) {
+    for (int i = 0; i < ctx->clear_lds_n; i++)
+        if (ctx->clear_lds[i] == kernel) return;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess && ctx->clear_lds_n < CLEAR_LDS_KERNELS) ctx->clear_lds[ctx->clear_lds_n++] = kernel;
+}
+
 // Workspace of the clear calls: partial results of keys split over workgroups (attention), aligned copies of codes (matmul).  One allocation of fixed size, made
 // with the first cache or weights of a context and never moved, so that calls allocate nothing and a captured graph's pointers stay good.
 #define CLEAR_WS_FLOATS ((size_t)16 << 20)

@@ -9,8 +9,8 @@
 // A tile of scores is held as [key][query]: a lane has one query, so the statistics of a row are per lane, and the weights leave the score's
 // registers in the order in which the second product reads them; the order of its keys is that of the registers, for the values too.
 //
-// Masks are applied to scores; a masked weight is 0, and 0 times a value that is NaN must not count: tiles that hold such codes (any lane sees one)
-// take a second, rare path.
+// Masks are applied to scores; a masked weight is 0, and 0 times a value that is NaN must not count: NaN codes of values are taken as 0, and where a token of the
+// sequence has one, the rows that see it get their NaN at the end, from a second look at the tiles that had any.
 #include "clear.h"
 
 struct AttentionView {
@@ -75,6 +75,11 @@ __device__ __forceinline__ void transpose4(u32 (&d)[4]) {
     d[2] = __builtin_amdgcn_perm(t3, t1, 0x05040100);
     d[3] = __builtin_amdgcn_perm(t3, t1, 0x07060302);
 }
+// The larger one, NaN if either is: a row that sees NaN is NaN whatever its other scores are.  (The maximum that passes over NaN costs one more
+// instruction for every operand.)
+__device__ __forceinline__ float most_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float most_of(float a, float b, float c) { return most_of(most_of(a, b), c); }
+
 // Bit 7 of every byte whose code is NaN
 __device__ __forceinline__ u32 nan_bytes(u32 w) { return (w & 0x7f7f7f7f) + 0x01010101; }
 
@@ -107,6 +112,20 @@ __device__ __forceinline__ RowTile row_tile(const SeqPart &part, int row0, int m
     r.tiles = (r.last + 1 - r.lo + 31) / 32;
     return r;
 }
+
+// The block of 16 keys that holds a key, as a row of the scales; -1: its page is outside the cache.
+__device__ __forceinline__ int block_of(const AttentionView &a, int seq, int head, int key) {
+    const int page = a.s.table[seq * a.s.table_stride + key / a.kv.page];
+    if (page < 0 || page >= a.kv.pages) return -1;
+    return (int)(((page * (int64_t)a.kv.heads + head) * a.kv.page + key % a.kv.page) / KV_BLOCK);
+}
+__device__ __forceinline__ bool is_nan(unsigned char code) { return (code & 0x7f) == 0x7f; }
+// Which of a lane's keys its row sees, without a branch: places from low + 1 to high behind key0.
+struct Seen {
+    int low;
+    __device__ __forceinline__ Seen(const AttentionView &a, int reach) : low(a.window > 0 ? reach - a.window : INT32_MIN) {}
+    __device__ __forceinline__ bool at(int place, int high) const { return (place <= high) & (place > low); }
+};
 
 // How a lane holds its dims: PIECE of one load, then REST of a second one, for widths that are no power of two times 16; in bytes of a row, and
 // of the whole row the first MAIN.
@@ -164,6 +183,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
     }
     Rows16<DIM> st;
     st.clear();
+    int nan_from = INT32_MAX, nan_to = -1;  // keys between which values had NaN
     for (int batch = tile0 + wave; batch < tile1; batch += 4 * 32) {
         // 32 tiles of this wave at once: lane l looks up the block of 16 keys of half l % 2 of tile l / 2
         int my_block = 0, my_good = 0;
@@ -171,12 +191,12 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
         {
             const int t = batch + 4 * (lane / 2), key = rt.lo + 32 * t + 16 * (lane % 2);
             if (t < tile1 && key <= rt.last) {
-                const int page = a.s.table[seq * a.s.table_stride + key / a.kv.page];
-                if (page >= 0 && page < a.kv.pages) {
-                    my_block = ((page * (int64_t)a.kv.heads + head) * a.kv.page + key % a.kv.page) / KV_BLOCK;
+                const int block = block_of(a, seq, head, key);
+                if (block >= 0) {
+                    my_block = block;
                     my_good = 1;
-                    my_k = a.kv.ks[my_block];
-                    my_v = fmaxf(a.kv.vs[my_block], 0x1p-64f);
+                    my_k = a.kv.ks[block];
+                    my_v = fmaxf(a.kv.vs[block], 0x1p-64f);
                 } else
                     atomicOr(a.kv.status, ENSI_KV_BAD_PAGE);
             }
@@ -232,10 +252,6 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
             }
             float u[2][4];
             const bool masked = key0 + 31 > rt.first || (a.window > 0 && key0 <= rt.last - a.window) || !good[0] || !good[1];
-            const auto sees = [&](int h, int r) {
-                const int key = key0 + 16 * h + 4 * g + r;
-                return good[h] && key <= pos && (a.window <= 0 || key > pos - a.window);
-            };
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
@@ -244,23 +260,26 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
                     if (SCORE == ENSI_SCORE_SIGMOID) u[h][r] = vs[h] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[h][r]));
                 }
             if (masked) {
+                const int reach = pos - key0 - 4 * g;
+                const Seen seen(a, reach);
 #pragma unroll
-                for (int h = 0; h < 2; h++)
+                for (int h = 0; h < 2; h++) {
+                    const int high = good[h] ? reach : INT32_MIN;
 #pragma unroll
-                    for (int r = 0; r < 4; r++)
-                        if (!sees(h, r)) u[h][r] = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+                    for (int r = 0; r < 4; r++) u[h][r] = seen.at(16 * h + r, high) ? u[h][r] : SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+                }
             }
             float lv[2], most = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 lv[h] = SCORE == ENSI_SCORE_SIGMOID ? 0 : __builtin_amdgcn_logf(vs[h]);
-                float top = fmaxf(fmaxf(u[h][0], u[h][1]), fmaxf(u[h][2], u[h][3]));
-                most = fmaxf(most, top + lv[h]);
+                const float top = most_of(most_of(u[h][0], u[h][1], u[h][2]), u[h][3]);
+                most = most_of(most, top + lv[h]);
             }
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
-            if (SCORE == ENSI_SCORE_SIGMOID) most = fmaxf(__builtin_amdgcn_logf(most), -120.0f);
-            const float m = fmaxf(st.m, most), base = m == -__builtin_inff() ? 0.0f : m;
+            most = most_of(most, __shfl_xor(most, 16));
+            most = most_of(most, __shfl_xor(most, 32));
+            if (SCORE == ENSI_SCORE_SIGMOID) most = most_of(__builtin_amdgcn_logf(most), -120.0f);
+            const float m = most_of(st.m, most), base = m == -__builtin_inff() ? 0.0f : m;
             const float lift = half_lift(st.m, base);
             st.m = m;
             if (__any(lift != 1.0f)) {
@@ -290,33 +309,20 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
 #pragma unroll
                     for (int r = 0; r < 4; r++) nans |= nan_bytes(now.v[h][x][r]);
             if (__any((nans & 0x80808080) != 0)) {
-                // rare: NaN goes to the places of the rows that see its token, and its code becomes 0
-                f16x8 visible;
+                bool inside = false;  // of a token of the sequence, not of what lies behind its end
 #pragma unroll
                 for (int h = 0; h < 2; h++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++) visible[4 * h + r] = sees(h, r) ? (_Float16)1.0f : (_Float16)0.0f;
-#pragma unroll
-                for (int x = 0; x < WORDS; x++) {
-                    u32 ones[2][4];  // 1.0 in e4m3 where the code is NaN
-#pragma unroll
-                    for (int h = 0; h < 2; h++) {
+                    for (int x = 0; x < WORDS; x++)
 #pragma unroll
                         for (int r = 0; r < 4; r++) {
-                            const u32 hit = (nan_bytes(now.v[h][x][r]) & 0x80808080) >> 7;
-                            ones[h][r] = hit * 0x38;
-                            now.v[h][x][r] &= ~(hit * 0xff);
+                            const u32 hit = nan_bytes(now.v[h][x][r]) & 0x80808080;
+                            inside |= hit && key0 + 16 * h + 4 * g + r <= rt.last;
+                            now.v[h][x][r] &= ~((hit >> 7) * 0xff);
                         }
-                        transpose4(ones[h]);
-                    }
-#pragma unroll
-                    for (int b = 0; b < 4; b++) {
-                        if (4 * x + b >= TILES) continue;
-                        const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(Wide<ENSI_T_F16>::widen(ones[0][b], ones[1][b]), visible, (f32x4){0, 0, 0, 0}, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 4; r++)
-                            if (hit[r] > 0) st.o[4 * x + b][r] = __builtin_nanf("");
-                    }
+                if (__any(inside)) {
+                    nan_from = min(nan_from, key0);
+                    nan_to = key0 + 31;
                 }
             }
 #pragma unroll
@@ -334,6 +340,17 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
             }
         }
     }
+    for (int key = nan_from; key <= min(nan_to, rt.last); key++) {
+        // rare, and of this wave's tiles only
+        const int block = (key - rt.lo) / 32 % 4 == (tile0 + wave) % 4 ? block_of(a, seq, head, key) : -1;
+        if (block < 0 || key > pos || (a.window > 0 && key <= pos - a.window)) continue;
+        const unsigned char *v = a.kv.v + ((int64_t)block * KV_BLOCK + key % KV_BLOCK) * DIM;
+#pragma unroll
+        for (int j = 0; j < TILES; j++)
+#pragma unroll
+            for (int r = 0; r < 4; r++)
+                if (is_nan(v[j < PIECE ? PIECE * (4 * g + r) + j : MAIN + REST * (4 * g + r) + j - PIECE])) st.o[j][r] = __builtin_nanf("");
+    }
     // a lane has the sum of its keys only
     st.l += __shfl_xor(st.l, 16);
     st.l += __shfl_xor(st.l, 32);
@@ -350,7 +367,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
         }
         __syncthreads();
         if (wave < half) {
-            const float om = part_m[wave][lane], m = fmaxf(st.m, om), base = m == -__builtin_inff() ? 0.0f : m;
+            const float om = part_m[wave][lane], m = most_of(st.m, om), base = m == -__builtin_inff() ? 0.0f : m;
             const float h0 = half_lift(st.m, base), h1 = half_lift(om, base), mine = h0 * h0, other = h1 * h1;
 #pragma unroll
             for (int j = 0; j < TILES; j++) {
@@ -453,7 +470,8 @@ __global__ __launch_bounds__(256) void k_clear_attention_join(AttentionView a, i
 // LDS reads (32 KB a wave and tile at 128 places) and the softmax's vector instructions are about equally busy.
 template <int DIM>
 struct RowsLds {
-    static constexpr int KEYS = 64, K_ROW = DIM * 2 + 16, V_ROW = KEYS * 2 + 16;  // bytes; 16 more keep the rows of a fragment on different banks
+    static constexpr int KEYS = 64, K_ROW = DIM * 2 + 16, V_ROW = KEYS * 2 + 16;  // bytes; 16 more keep the rows of a fragment on different banks,
+    // and the chunks of 8 keys of a row of values are permuted with the row's number by 16, which does so for the rows, 4 apart, that a wave writes
     static constexpr int K_BYTES = KEYS * K_ROW, V_BYTES = DIM * V_ROW, BUFFER = K_BYTES + V_BYTES;
     static constexpr int BUFFERS = 2 * BUFFER <= 80 * 1024 ? 2 : 1;
 };
@@ -466,7 +484,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
     typedef RowsLds<DIM> L;
     constexpr int STEPS = DIM / 16, TILES = DIM / 32, ITEMS = (DIM / 2 + 63) / 64;  // of the values: 8 keys x 4 places
     extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ int has_nan[2][4];
+    __shared__ int nan_tiles[2];  // first and last tile whose values had NaN
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 32, half = lane / 32;
     const int seq = blockIdx.z, head = blockIdx.x % a.kv.heads, tile = a.row_tiles - 1 - blockIdx.x / a.kv.heads;  // the longest rows first
     const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
@@ -489,6 +507,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
 #pragma unroll
         for (int r = 0; r < 16; r++) o[j][r] = 0;
     float st_m = -__builtin_inff(), st_l = 0;
+    bool wide = false;  // of a wave: value scales outside 2^-40 .. 2^40 were met
     const int tiles = (all.last + 1 - all.lo + 63) / 64;
     // what 16 tiles need to know of their blocks of 16 keys: lane l has block l % 4 of tile l / 4
     int my_block = 0, my_good = 0;
@@ -498,12 +517,12 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
         my_block = my_good = 0;
         my_k = my_v = 1;
         if (key <= all.last) {
-            const int page = a.s.table[seq * a.s.table_stride + key / a.kv.page];
-            if (page >= 0 && page < a.kv.pages) {
-                my_block = ((page * (int64_t)a.kv.heads + head) * a.kv.page + key % a.kv.page) / KV_BLOCK;
+            const int block = block_of(a, seq, head, key);
+            if (block >= 0) {
+                my_block = block;
                 my_good = 1;
-                my_k = a.kv.ks[my_block];
-                my_v = fmaxf(a.kv.vs[my_block], 0x1p-64f);
+                my_k = a.kv.ks[block];
+                my_v = fmaxf(a.kv.vs[block], 0x1p-64f);
             } else
                 atomicOr(a.kv.status, ENSI_KV_BAD_PAGE);
         }
@@ -525,61 +544,64 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
             }
         }
     };
-    const auto put = [&](int buffer) {
-        unsigned char *at = lds + (L::BUFFERS == 2 ? buffer * L::BUFFER : 0);
+    const auto put = [&](int t) {
+        unsigned char *at = lds + (L::BUFFERS == 2 ? t % 2 * L::BUFFER : 0);
         unsigned char *k = at + (16 * wave + lane / 4) * L::K_ROW + (lane % 4) * (DIM / 2);
 #pragma unroll
         for (int i = 0; i < DIM / 32; i++) *(vec *)(k + 16 * i) = W::widen(kc[i][0], kc[i][1]);
         u32 nans = 0;
 #pragma unroll
+        for (int i = 0; i < ITEMS; i++)
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (DIM / 2 % 64 == 0 || lane + 64 * i < DIM / 2) nans |= nan_bytes(vc[i][e]);
+        if (__any((nans & 0x80808080) != 0)) {
+            bool inside = false;  // of a token of the sequence, not of what lies behind its end
+#pragma unroll
+            for (int i = 0; i < ITEMS; i++) {
+                const int item = lane + 64 * i, h = item / (DIM / 4);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const u32 hit = item < DIM / 2 ? nan_bytes(vc[i][e]) & 0x80808080 : 0;
+                    inside |= hit && all.lo + 64 * t + 16 * wave + 4 * h + 8 * (e / 4) + e % 4 <= all.last;
+                    vc[i][e] &= ~((hit >> 7) * 0xff);
+                }
+            }
+            if (inside) {
+                atomicMin(&nan_tiles[0], t);
+                atomicMax(&nan_tiles[1], t);
+            }
+        }
+#pragma unroll
         for (int i = 0; i < ITEMS; i++) {
             const int item = lane + 64 * i, h = item / (DIM / 4), places = 4 * (item % (DIM / 4));
             if (DIM / 2 % 64 == 0 || item < DIM / 2) {
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const u32 hit = nan_bytes(vc[i][e]) & 0x80808080;
-                    nans |= hit;
-                }
                 u32 x[2][4];
 #pragma unroll
                 for (int e = 0; e < 8; e++) x[e / 4][e % 4] = vc[i][e];
                 transpose4(x[0]);
                 transpose4(x[1]);
 #pragma unroll
-                for (int j = 0; j < 4; j++) *(f16x8 *)(at + L::K_BYTES + (places + j) * L::V_ROW + 32 * wave + 16 * h) = Wide<ENSI_T_F16>::widen(x[0][j], x[1][j]);
+                for (int j = 0; j < 4; j++) *(f16x8 *)(at + L::K_BYTES + (places + j) * L::V_ROW + 16 * ((2 * wave + h) ^ (places / 16 % 4))) = Wide<ENSI_T_F16>::widen(x[0][j], x[1][j]);
             }
         }
-        const bool any = __any(nans != 0);
-        if (any) {
-            // rare: NaN becomes 0 in LDS; who reads the tile looks its places up
-#pragma unroll
-            for (int i = 0; i < ITEMS; i++) {
-                const int item = lane + 64 * i, h = item / (DIM / 4), places = 4 * (item % (DIM / 4));
-                if (DIM / 2 % 64 == 0 || item < DIM / 2) {
-                    u32 x[2][4];
-#pragma unroll
-                    for (int e = 0; e < 8; e++) x[e / 4][e % 4] = vc[i][e] & ~(((nan_bytes(vc[i][e]) & 0x80808080) >> 7) * 0xff);
-                    transpose4(x[0]);
-                    transpose4(x[1]);
-#pragma unroll
-                    for (int j = 0; j < 4; j++) *(f16x8 *)(at + L::K_BYTES + (places + j) * L::V_ROW + 32 * wave + 16 * h) = Wide<ENSI_T_F16>::widen(x[0][j], x[1][j]);
-                }
-            }
-        }
-        if (lane == 0) has_nan[buffer][wave] = any;
     };
+    if (threadIdx.x == 0) {
+        nan_tiles[0] = INT32_MAX;
+        nan_tiles[1] = -1;
+    }
+    __syncthreads();
     look_up(0);
     fetch(0);
     put(0);
     __syncthreads();
     for (int t = 0; t < tiles; t++) {
-        const int buffer = t % 2, key0 = all.lo + 64 * t;
-        int good[4], block[4];
+        const int key0 = all.lo + 64 * t;
+        int good[4];
         float ks[4], vs[4];
 #pragma unroll
         for (int b = 0; b < 4; b++) {
             good[b] = __builtin_amdgcn_readlane(my_good, 4 * (t % 16) + b);
-            block[b] = __builtin_amdgcn_readlane(my_block, 4 * (t % 16) + b);
             ks[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), 4 * (t % 16) + b));
             vs[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 4 * (t % 16) + b));
         }
@@ -589,20 +611,30 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
         }
         // a wave whose rows see nothing of the tile goes on
         if (mine.rows > 0 && key0 <= mine.last && (a.window <= 0 || key0 + 63 > mine.first - a.window)) {
-            const unsigned char *at = lds + (L::BUFFERS == 2 ? buffer * L::BUFFER : 0);
+            const unsigned char *at = lds + (L::BUFFERS == 2 ? t % 2 * L::BUFFER : 0);
+            // fragments of AHEAD steps under way: left to itself, the compiler keeps two reads under way, and a wave waits for LDS most of its time
             f32x16 qk[2];
+            constexpr int AHEAD = STEPS < 4 ? STEPS : 4;
+            vec kf[AHEAD][2];
+            const auto read_keys = [&](int s) {
 #pragma unroll
-            for (int x = 0; x < 2; x++) {
+                for (int x = 0; x < 2; x++) kf[s % AHEAD][x] = *(const vec *)(at + (32 * x + n) * L::K_ROW + 32 * s + 16 * half);
+            };
+#pragma unroll
+            for (int s = 0; s < AHEAD; s++) read_keys(s);
+#pragma unroll
+            for (int x = 0; x < 2; x++)
 #pragma unroll
                 for (int r = 0; r < 16; r++) qk[x][r] = 0;
 #pragma unroll
-                for (int s = 0; s < STEPS; s++) qk[x] = W::mfma32(*(const vec *)(at + (32 * x + n) * L::K_ROW + 32 * s + 16 * half), q[s], qk[x]);
+            for (int s = 0; s < STEPS; s++) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int x = 0; x < 2; x++) qk[x] = W::mfma32(kf[s % AHEAD][x], q[s], qk[x]);
+                if (s + AHEAD < STEPS) read_keys(s + AHEAD);
             }
+            __builtin_amdgcn_sched_barrier(0);
             // register r of half x, block b = 2 x + r / 8: key 16 b + 8 (r % 8 / 4) + 4 half + r % 4
-            const auto sees = [&](int b, int e) {
-                const int key = key0 + 16 * b + 8 * (e / 4) + 4 * half + e % 4;
-                return good[b] && key <= pos && (a.window <= 0 || key > pos - a.window);
-            };
             const bool masked = key0 + 63 > mine.first || (a.window > 0 && key0 <= mine.last - a.window) || !(good[0] & good[1] & good[2] & good[3]);
             float u[4][8], most = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
 #pragma unroll
@@ -616,23 +648,26 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
                     u[b][e] = v;
                 }
             if (masked) {
+                const int reach = pos - key0 - 4 * half;
+                const Seen seen(a, reach);
 #pragma unroll
-                for (int b = 0; b < 4; b++)
+                for (int b = 0; b < 4; b++) {
+                    const int high = good[b] ? reach : INT32_MIN;
 #pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        if (!sees(b, e)) u[b][e] = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+                    for (int e = 0; e < 8; e++) u[b][e] = seen.at(16 * b + 8 * (e / 4) + e % 4, high) ? u[b][e] : SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+                }
             }
-            float factor[4];
+            float factor[4], lv[4];
 #pragma unroll
             for (int b = 0; b < 4; b++) {
                 factor[b] = CAP || SCORE == ENSI_SCORE_SIGMOID ? 1.0f : a.factor * ks[b];
-                float top = fmaxf(fmaxf(fmaxf(u[b][0], u[b][1]), fmaxf(u[b][2], u[b][3])), fmaxf(fmaxf(u[b][4], u[b][5]), fmaxf(u[b][6], u[b][7])));
-                if (SCORE == ENSI_SCORE_SOFTMAX) top = __builtin_fmaf(top, factor[b], __builtin_amdgcn_logf(vs[b]));
-                most = fmaxf(most, top);
+                lv[b] = __builtin_amdgcn_logf(vs[b]);
+                const float top = most_of(most_of(most_of(u[b][0], u[b][1], u[b][2]), u[b][3], u[b][4]), most_of(u[b][5], u[b][6], u[b][7]));
+                most = most_of(most, SCORE == ENSI_SCORE_SOFTMAX ? __builtin_fmaf(top, factor[b], lv[b]) : top);
             }
-            most = fmaxf(most, __shfl_xor(most, 32));
-            if (SCORE == ENSI_SCORE_SIGMOID) most = fmaxf(__builtin_amdgcn_logf(most), -120.0f);
-            const float m = fmaxf(st_m, most), base = m == -__builtin_inff() ? 0.0f : m;
+            most = most_of(most, __shfl_xor(most, 32));
+            if (SCORE == ENSI_SCORE_SIGMOID) most = most_of(__builtin_amdgcn_logf(most), -120.0f);
+            const float m = most_of(st_m, most), base = m == -__builtin_inff() ? 0.0f : m;
             const float lift = half_lift(st_m, base);
             st_m = m;
             if (__any(lift != 1.0f)) {
@@ -643,56 +678,76 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
                     for (int r = 0; r < 16; r++) o[j][r] *= f;
                 st_l = st_l * lift * lift;
             }
+            // the values of the first two blocks on their way while the weights are formed
+            f16x8 vf[2][TILES];
+            const auto read_values = [&](int b) {
+#pragma unroll
+                for (int j = 0; j < TILES; j++) vf[b % 2][j] = *(const f16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 16 * ((2 * b + half) ^ (2 * (j % 2) + n / 16)));
+            };
+            read_values(0);
+            read_values(1);
+            __builtin_amdgcn_sched_barrier(0);
             union Weights {
                 _Float16 e[8];
                 f16x8 v;
             } p[4];
-            const float unit = SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(-base) : 0;
+            if (SCORE == ENSI_SCORE_SIGMOID) {
+                const float unit = __builtin_amdgcn_exp2f(-base);
 #pragma unroll
-            for (int b = 0; b < 4; b++)
+                for (int b = 0; b < 4; b++)
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    float w;
-                    if (SCORE == ENSI_SCORE_SIGMOID)
-                        w = u[b][e] * unit;
-                    else {
-                        w = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], -base));
-                        st_l += w;
-                        w *= vs[b];
+                    for (int e = 0; e < 8; e++) p[b].e[e] = (_Float16)(u[b][e] * unit);
+            } else {
+                // With all value scales so far between 2^-40 and 2^40 the weight 2^(t + log2 s' - M) can be formed at once and divided by s' for the sum, a block at a
+                // time: what is lost of the sum is below 2^-46 of its largest term.
+                wide |= fmaxf(fmaxf(fabsf(lv[0]), fabsf(lv[1])), fmaxf(fabsf(lv[2]), fabsf(lv[3]))) > 40;
+                if (!wide) {
+#pragma unroll
+                    for (int b = 0; b < 4; b++) {
+                        const float shift = lv[b] - base;
+                        float sum = 0;
+#pragma unroll
+                        for (int e = 0; e < 8; e++) {
+                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], shift));
+                            sum += w;
+                            p[b].e[e] = (_Float16)w;
+                        }
+                        st_l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vs[b]), st_l);
                     }
-                    p[b].e[e] = (_Float16)w;
-                }
-            if (has_nan[buffer][0] | has_nan[buffer][1] | has_nan[buffer][2] | has_nan[buffer][3]) {
-                // rare: NaN to the places of the rows that see its token, from the codes themselves
-                for (int b = 0; b < 4; b++) {
-                    f16x8 visible;
+                } else {
 #pragma unroll
-                    for (int e = 0; e < 8; e++) visible[e] = sees(b, e) ? (_Float16)1.0f : (_Float16)0.0f;
-                    const unsigned char *v = a.kv.v + (int64_t)block[b] * (KV_BLOCK * DIM);
+                    for (int b = 0; b < 4; b++)
 #pragma unroll
-                    for (int j = 0; j < TILES; j++) {
-                        f16x8 ones;
-#pragma unroll
-                        for (int e = 0; e < 8; e++) ones[e] = (v[(8 * (e / 4) + 4 * half + e % 4) * DIM + 32 * j + n] & 0x7f) == 0x7f ? (_Float16)1.0f : (_Float16)0.0f;
-                        f32x16 hit;
-#pragma unroll
-                        for (int r = 0; r < 16; r++) hit[r] = 0;
-                        hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(ones, visible, hit, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 16; r++)
-                            if (hit[r] > 0) o[j][r] = __builtin_nanf("");
-                    }
+                        for (int e = 0; e < 8; e++) {
+                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], -base));
+                            st_l += w;
+                            p[b].e[e] = (_Float16)(w * vs[b]);
+                        }
                 }
             }
 #pragma unroll
-            for (int j = 0; j < TILES; j++)
+            for (int b = 0; b < 4; b++) {
 #pragma unroll
-                for (int b = 0; b < 4; b++)
-                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 32 * b + 16 * half), p[b].v, o[j], 0, 0, 0);
+                for (int j = 0; j < TILES; j++) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[b % 2][j], p[b].v, o[j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (b + 2 < 4) read_values(b + 2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         if (L::BUFFERS == 1) __syncthreads();  // everybody has read this tile
-        if (t + 1 < tiles) put((t + 1) % 2);
+        if (t + 1 < tiles) put(t + 1);
         __syncthreads();
+    }
+    if (nan_tiles[1] >= 0)
+    for (int key = all.lo + 64 * nan_tiles[0]; key <= min(all.lo + 64 * nan_tiles[1] + 63, all.last); key++) {
+        const int block = block_of(a, seq, head, key);
+        if (block < 0 || key > pos || (a.window > 0 && key <= pos - a.window)) continue;
+        const unsigned char *v = a.kv.v + ((int64_t)block * KV_BLOCK + key % KV_BLOCK) * DIM + 4 * half;
+#pragma unroll
+        for (int j = 0; j < TILES; j++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                if (is_nan(v[32 * j + 8 * (r / 4) + r % 4])) o[j][r] = __builtin_nanf("");
     }
     st_l += __shfl_xor(st_l, 32);
     if (row0 + n >= part.count * a.group) return;
@@ -710,19 +765,31 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
         }
 }
 
-#ifndef USE_ROWS
-#define USE_ROWS (blocks >= 256)
-#endif
+// Whether rows are split over waves and their keys shared, or keys over waves: microseconds of either as measured (bf16, no cap).  Rows: for a tile of 64 keys 1.4 up to 96
+// places of a head, 1.75 at 128, 2.8 at 192, 3.5 at 256, while two workgroups of 128 rows find room on a CU (one from 192 on); 500 + 1024 tokens of 20 over 5 heads of 128
+// 50, 100 + 2048 73, 2048 + 4096 286.  Keys: 60e6 products of a query, a key and a place in 1: these three 55, 118 and 577; 500 + 512 tokens 28 (rows 35), five prompts of 77
+// behind up to 1500 on 16 heads of 96 21 (45), 1000 + 1000 of 16 over 4 heads of 256 94 (112).
+static bool attention_by_rows(const AttentionView &v, int span) {
+    const int dim = v.kv.dim;
+    const double blocks = (double)v.s.seqs * v.kv.heads * (((int64_t)v.s.max_new * v.group + 127) / 128);
+    const double rows_us = 4 + (span + 63) / 64 * std::max(1.4, dim / 73.0) * std::max(1.0, blocks / (dim <= 128 ? 400 : 256));
+    const double pairs = (double)v.s.seqs * v.s.max_new * v.q_heads * std::max(span - v.s.max_new / 2, 1);
+    const double keys_us = 6 + pairs * dim / 60e6;
+    return v.s.max_new > 1 && rows_us < keys_us;
+}
+
 template <int TYPE, int DIM, int SCORE>
 static void attention_go(ensi_ctx *ctx, AttentionView v, hipStream_t st) {
     const int heads = v.kv.heads;
-    const int64_t blocks = (int64_t)v.s.seqs * heads * (((int64_t)v.s.max_new * v.group + 127) / 128);
-    if (USE_ROWS) {
+    // the most keys that a tile of 16 rows looks at: those of its window, begun within a tile of 32 and ended within one
+    const int tokens = min(v.s.max_new, 15 / v.group + 2);
+    const int span = v.window > 0 ? (int)min((int64_t)v.max_length, (int64_t)v.window + tokens - 1 + 31) : v.max_length;
+    if (attention_by_rows(v, span)) {
         v.row_tiles = (int)(((int64_t)v.s.max_new * v.group + 127) / 128);
         ScopedTimer timer(ctx, "k_clear_attention", st);
         const auto go = [&](auto kernel) {
             constexpr int bytes = RowsLds<DIM>::BUFFERS * RowsLds<DIM>::BUFFER;
-            (void)hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+            clear_lds(ctx, (const void *)kernel, bytes);
             hipLaunchKernelGGL(kernel, dim3(heads * v.row_tiles, 1, v.s.seqs), dim3(256), bytes, st, v);
         };
         if (v.cap > 0) go(k_clear_attention_rows<TYPE, DIM, SCORE, true>);
@@ -731,18 +798,19 @@ static void attention_go(ensi_ctx *ctx, AttentionView v, hipStream_t st) {
     }
     v.row_tiles = (int)(((int64_t)v.s.max_new * v.group + 15) / 16);
     const int64_t base = (int64_t)v.s.seqs * heads * v.row_tiles;
-    // the most tiles of 32 keys that a tile of rows looks at: those of its window, begun within a tile and ended within one
-    const int tokens = min(v.s.max_new, 15 / v.group + 2);
-    const int span = v.window > 0 ? (int)min((int64_t)v.max_length, (int64_t)v.window + tokens - 1 + 31) : v.max_length;
     const int tiles = (span + 31) / 32;
-    // as many parts as give a wave 8 tiles, which evens out sequences of different lengths; more where the CUs would stand idle
-    int splits = (int)min((int64_t)(tiles + 3) / 4, max((int64_t)(tiles + 31) / 32, 768 / base));
-    splits = min(max(splits, 1), JOIN_MAX);
+    // Parts of a row's keys.  A decoding step: 8 tiles for a wave, which evens out sequences of different lengths (48 sequences of up to 8192 tokens 66 us, in one part 91); in
+    // either case more where the CUs would stand idle (one sequence of 32768 tokens: 15 us of keys in 128 parts).  Joining the parts costs 5 us for few rows and 10 for the
+    // thousands of a prompt, more than it gives where there are workgroups enough (5 prompts of 77 tokens: 21 us in one part, 27 in two).
+    const bool idle = base < (v.s.max_new > 1 ? 128 : 256);
+    int splits = max(v.s.max_new > 1 ? 1 : (tiles + 31) / 32, idle ? (int)(768 / base) : 1);
+    splits = min(splits, min((tiles + 3) / 4, JOIN_MAX));
+    splits = max(splits, 1);
     const int64_t room = (int64_t)CLEAR_WS_FLOATS / (base * (16 * DIM + 32));
     if (splits > room) splits = (int)max((int64_t)1, room);
     int split_tiles = (tiles + splits - 1) / splits;
-    split_tiles = (split_tiles + 3) & ~3;  // a tile for every wave
-    splits = (tiles + split_tiles - 1) / split_tiles;
+    split_tiles = max((split_tiles + 3) & ~3, 4);  // a tile for every wave
+    splits = max((tiles + split_tiles - 1) / split_tiles, 1);
     v.splits = splits;
     const dim3 grid(heads * v.row_tiles, splits, v.s.seqs);
     {

@@ -297,14 +297,11 @@ __global__ __launch_bounds__(256) void k_clear_align(const signed char *codes, i
 // 1000 x 2560 x 2560 33 and 2000 x 2560 x 6912 119: 3 and 1 for 0.43e9 products (0.30e9).  Many rows: 200 and 500 x 2560 x 2560 21, 1000 x 2560 x 6912
 // 26, 2000 of them 40, 4096 74, with groups 100 x 2560 x 2560 32, 1000 of them 40 and 2000 x 2560 x 6912 72: for a unit of 128 places 1 (1.6) while the
 // workgroups have a CU to themselves, then 1 for 230 (120) of them; the copy of unaligned codes 4 on top.
-#ifndef MANY_RULE
-#define MANY_RULE many_us < few_us
-#endif
 static bool matmul_is_many(const MatmulView &v, bool aligned) {
     const double few_us = 3 + (double)v.rows * v.d * v.m / (v.group ? 0.30e9 : 0.43e9);
     const double blocks = (double)((v.rows + 127) / 128) * ((v.m + MANY_COLS - 1) / MANY_COLS);
     const double many_us = v.units * (v.group ? std::max(1.6, blocks / 120) : std::max(1.0, blocks / 230)) + (aligned ? 0 : 4);
-    return MANY_RULE;
+    return many_us < few_us;
 }
 template <int TYPE, int TILES>
 static void matmul_few(const MatmulView &v, hipStream_t st) {
@@ -313,10 +310,10 @@ static void matmul_few(const MatmulView &v, hipStream_t st) {
     else hipLaunchKernelGGL((k_clear_matmul_few<TYPE, TILES, false>), grid, block, 0, st, v);
 }
 template <int TYPE, int TM, bool GROUPED>
-static void matmul_many(const MatmulView &v, hipStream_t st) {
+static void matmul_many(ensi_ctx *ctx, const MatmulView &v, hipStream_t st) {
     const int blocks = (int)((int64_t)((v.rows + 32 * TM - 1) / (32 * TM)) * ((v.m + MANY_COLS - 1) / MANY_COLS));
     const int bytes = 3 * ManyLds<TM, GROUPED>::BUFFER;
-    (void)hipFuncSetAttribute((const void *)k_clear_matmul_many<TYPE, TM, GROUPED>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    clear_lds(ctx, (const void *)k_clear_matmul_many<TYPE, TM, GROUPED>, bytes);
     hipLaunchKernelGGL((k_clear_matmul_many<TYPE, TM, GROUPED>), dim3((u32)((blocks + 7) / 8 * 8)), dim3(512), bytes, st, v);
 }
 template <int TYPE>
@@ -325,8 +322,8 @@ static void matmul_type(ensi_ctx *ctx, const MatmulView &v, hipStream_t st) {
     if (matmul_is_many(v, aligned)) {
         const auto many = [&](const MatmulView &u) {
             ScopedTimer timer(ctx, "k_clear_matmul", st);
-            if (u.group) return matmul_many<TYPE, 4, true>(u, st);
-            matmul_many<TYPE, 4, false>(u, st);
+            if (u.group) return matmul_many<TYPE, 4, true>(ctx, u, st);
+            matmul_many<TYPE, 4, false>(ctx, u, st);
         };
         if (aligned) return many(v);
         // slices of the rows that the workspace holds

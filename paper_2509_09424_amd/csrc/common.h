@@ -215,6 +215,7 @@ struct StageSlot {
     bool pending = false;
 };
 #define ENSI_STAGE_SLOTS 8
+#define CLEAR_LDS_KERNELS 64
 
 // Two words of a ciphertext at a time.  Wrapped batches are u64 arrays of the caller, aligned to a word and no more: these
 // may be read and written in one access all the same, but not by a type that claims 16 bytes.
@@ -309,7 +310,9 @@ struct ensi_ctx {
     u64 sampler_ctr = 0;
     void *static_scratch = nullptr;  // this device's copy of the statically linked workspace (api_static.hip)
     size_t static_scratch_bytes = 0;
-    float *ws_clear = nullptr;   // partial results of attention on clear activations: fixed size, made with the first cache
+    float *ws_clear = nullptr;   // workspace of the calls on clear activations: fixed size, made with the first cache or weights
+    const void *clear_lds[CLEAR_LDS_KERNELS];  // of their kernels, those whose limit of dynamic LDS is raised
+    int clear_lds_n = 0;
     StageSlot stage[ENSI_STAGE_SLOTS];
     int stage_next = 0;
     int n_cu = 0;                // compute units of the context's device (0: not queried yet)
