@@ -664,9 +664,10 @@ class Context:
             out = q.new_empty(shape)
         pq, sq = _rows("q", q, shape, kind, at)
         po, so = _rows("out", out, shape, kind, at)
+        s = _seqs(table, begin, lengths, shape[0], max_new, at)
         if max_length is None:
             max_length = min(table.shape[1] * cache.page, 1 << 30)
-        args = _ATTENTION.pack(*_seqs(table, begin, lengths, shape[0], max_new, at), pq, po, sq, so, shape[1], _type("q", kind), _SCORES[score], window, max_length, cap, bias, 0)
+        args = _ATTENTION.pack(*s, pq, po, sq, so, shape[1], _type("q", kind), _SCORES[score], window, max_length, cap, bias, 0)
         rc = self.lib.ensi_clear_attention(self.h, cache.h, args, stream)
         if rc:
             self._check(rc)
