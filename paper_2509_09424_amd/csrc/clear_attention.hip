@@ -773,7 +773,7 @@ static bool attention_by_rows(const AttentionView &v, int span) {
     const int dim = v.kv.dim;
     const double blocks = (double)v.s.seqs * v.kv.heads * (((int64_t)v.s.max_new * v.group + 127) / 128);
     const double rows_us = 4 + (span + 63) / 64 * std::max(1.4, dim / 73.0) * std::max(1.0, blocks / (dim <= 128 ? 400 : 256));
-    const double pairs = (double)v.s.seqs * v.s.max_new * v.q_heads * std::max(span - v.s.max_new / 2, 1);
+    const double pairs = (double)v.s.seqs * v.s.max_new * v.q_heads * (v.window > 0 ? span : std::max(span - v.s.max_new / 2, 1));
     const double keys_us = 6 + pairs * dim / 60e6;
     return v.s.max_new > 1 && rows_us < keys_us;
 }
@@ -799,11 +799,11 @@ static void attention_go(ensi_ctx *ctx, AttentionView v, hipStream_t st) {
     v.row_tiles = (int)(((int64_t)v.s.max_new * v.group + 15) / 16);
     const int64_t base = (int64_t)v.s.seqs * heads * v.row_tiles;
     const int tiles = (span + 31) / 32;
-    // Parts of a row's keys.  A decoding step: 8 tiles for a wave, which evens out sequences of different lengths (48 sequences of up to 8192 tokens 66 us, in one part 91); in
-    // either case more where the CUs would stand idle (one sequence of 32768 tokens: 15 us of keys in 128 parts).  Joining the parts costs 5 us for few rows and 10 for the
-    // thousands of a prompt, more than it gives where there are workgroups enough (5 prompts of 77 tokens: 21 us in one part, 27 in two).
-    const bool idle = base < (v.s.max_new > 1 ? 128 : 256);
-    int splits = max(v.s.max_new > 1 ? 1 : (tiles + 31) / 32, idle ? (int)(768 / base) : 1);
+    // Parts of a row's keys.  A decoding step: 8 tiles for a wave, which evens out sequences of different lengths (48 sequences of up to 8192 tokens 66 us, in one part 91).
+    // More where the CUs would stand idle, two workgroups for each of them (one sequence of 32768 tokens: 18.4 us with 102 parts, 19.7 with 128 or 38), unless a wave has no
+    // more than 4 tiles: joining the parts costs 5 us for few rows and 10 for the thousands of a prompt (5 prompts of 77 tokens: 21 us in one part, 27 in two).
+    const bool idle = base < (v.s.max_new > 1 ? 128 : 256) && tiles > 16;
+    int splits = max(v.s.max_new > 1 ? 1 : (tiles + 31) / 32, idle ? (int)(512 / base) : 1);
     splits = min(splits, min((tiles + 3) / 4, JOIN_MAX));
     splits = max(splits, 1);
     const int64_t room = (int64_t)CLEAR_WS_FLOATS / (base * (16 * DIM + 32));

@@ -2,8 +2,8 @@
 //
 // Per row: h = x + r (rounded to the type), p = h g, most = max |p|; codes = rint(p (127 (1 / most))), scale = most / (127 rms), out = p / rms.
 // The root cancels in the codes, so they need the row's maximum only, and both row values come from one pass over the row: it is read
-// once, p stays in registers, and what is bound by memory for many rows (norm of 4096 x 2560 bf16 with a residual: 7 bytes an element) is bound
-// by the launch for few.
+// once and p stays in registers.  Many rows are bound by memory (4096 x 2560 bf16 with a residual, 7 bytes an element: 14.6 us, 5.0 TB/s, where a copy of 4 GiB reaches 4.8), few
+// by the launch and three latencies (1 x 2560: 2.8 us).
 #include "clear.h"
 
 struct NormView {
@@ -18,9 +18,9 @@ struct NormView {
 
 // LANES threads hold a row, V chunks of 8 elements each: thread t has chunks t, t + LANES, ...
 template <int TYPE, int LANES, int V>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_clear_norm(NormView a) {
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void k_clear_norm(NormView a) {
     typedef typename Elem<TYPE>::type T;
-    constexpr int PER_BLOCK = LANES < 256 ? 256 / LANES : 1;
+    constexpr int PER_BLOCK = LANES == 64 ? 4 : 1;  // rows
     const int t = threadIdx.x % LANES;
     const int64_t row = (int64_t)blockIdx.x * PER_BLOCK + threadIdx.x / LANES;
     if (PER_BLOCK > 1 && row >= a.rows) return;  // a whole wave: nothing is shared between the rows of a block
@@ -135,22 +135,26 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_clear_norm(NormVi
 
 template <int TYPE, int LANES, int V>
 static void norm_go(const NormView &v, hipStream_t st) {
-    constexpr int PER_BLOCK = LANES < 256 ? 256 / LANES : 1;
+    constexpr int PER_BLOCK = LANES == 64 ? 4 : 1;  // rows
     hipLaunchKernelGGL((k_clear_norm<TYPE, LANES, V>), dim3((u32)((v.rows + PER_BLOCK - 1) / PER_BLOCK)), dim3(PER_BLOCK * LANES), 0, st, v);
 }
 
 template <int TYPE>
 static void norm_type(const NormView &v, hipStream_t st) {
     const int chunks = (v.d + 7) / 8;
-    // a wave to a row where there are rows for all CUs and a row fits its registers, else a workgroup
-    if (v.rows >= 1024 && chunks <= 8 * 64) {
+    // Few chunks to a thread for few rows, whose latency decides (1 x 2560 with a residual: 2.8 us with 512 threads to a row, 3.2 with 256, 5.0 with 64; 512 rows 5.0, 5.0 and
+    // 6.6), a wave to a row without a barrier for many (4096 rows: 17.2, 16.8 and 14.6 us; 2048: 10.8, 10.1 and 10.6).  200 x 8192: 5.4 us with 512, 6.4 with 256;
+    // 1024 x 8191 14.5 with either.
+    if (chunks <= 64) return norm_go<TYPE, 64, 1>(v, st);
+    if (v.rows > 2048 && chunks <= 8 * 64) {
         if (chunks <= 2 * 64) return norm_go<TYPE, 64, 2>(v, st);
         if (chunks <= 5 * 64) return norm_go<TYPE, 64, 5>(v, st);
         return norm_go<TYPE, 64, 8>(v, st);
     }
-    if (chunks <= 256) return norm_go<TYPE, 256, 1>(v, st);
-    if (chunks <= 2 * 256) return norm_go<TYPE, 256, 2>(v, st);
-    if (chunks <= 4 * 256) return norm_go<TYPE, 256, 4>(v, st);
+    if (chunks <= 128) return norm_go<TYPE, 128, 1>(v, st);
+    if (v.rows > 1024 && chunks <= 2 * 256) return norm_go<TYPE, 256, 2>(v, st);
+    if (chunks <= 512) return norm_go<TYPE, 512, 1>(v, st);
+    if (chunks <= 2 * 512) return norm_go<TYPE, 512, 2>(v, st);
     return norm_go<TYPE, 1024, 4>(v, st);
 }
 

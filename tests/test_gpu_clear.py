@@ -75,6 +75,13 @@ def test_norm(ctx, kind, rows, d, pad, residual):
         assert torch.equal(sum_out.cpu(), h)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, d, pad, residual", [(2050, 500, 1, True), (2049, 1023, 0, False), (2051, 2000, 3, True), (2049, 4089, 0, True), (1025, 1030, 5, True)])
+def test_norm_of_many_rows(ctx, kind, rows, d, pad, residual):
+    """A wave to a row, of every number of chunks."""
+    test_norm(ctx, kind, rows, d, pad, residual)
+
+
 @pytest.mark.parametrize("rows", [3, 1500])
 def test_norm_in_place(ctx, rows):
     g = gen(rows)
@@ -139,6 +146,13 @@ def test_matmul(ctx, kind, rows, d, m, group, pad):
     flushed = 2.0 ** -25 if kind == "f16" else 0  # half a step of the smallest numbers
     assert (off <= half_step(kind) * want.abs() * (1 + 1e-6) + (0 if not group else (d // 64 + 6)) * U32 * terms + 3 * U32 * want.abs() + flushed).all()
     weights.free()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, d, m, group, pad", [(1500, 2048, 2050, 0, 0), (1300, 2000, 3001, 0, 5), (2050, 1030, 2500, 128, 0), (2000, 1536, 2600, 256, 16), (1111, 1543, 4100, 0, 0)])
+def test_matmul_of_many_rows(ctx, kind, rows, d, m, group, pad):
+    """Sizes where the matrix cores decide: rows that are aligned and that are not, edges in every direction."""
+    test_matmul(ctx, kind, rows, d, m, group, pad)
 
 
 def test_matmul_scales_pass_nan_and_rows_stay_apart(ctx):
@@ -394,6 +408,41 @@ def test_attention(ctx, kind, ctxs, news, heads, group, dim, page, cap, window, 
     cache.free()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("ctxs, news, heads, group, dim, page, cap, window, score", [
+    ([70, 0], [1800, 1000], 8, 4, 64, 16, 0.0, 0, "softmax"), ([200], [1500], 8, 4, 128, 64, 0.0, 0, "softmax"), ([33], [1501], 8, 2, 96, 32, 20.0, 300, "softmax"),
+    ([10], [1500], 4, 6, 192, 16, 0.0, 0, "sigmoid"), ([100], [1450], 8, 4, 256, 64, 0.0, 500, "softmax"), ([5, 300, 40], [1500, 0, 911], 8, 2, 64, 48, 9.0, 0, "sigmoid")])
+def test_attention_of_prompts(ctx, kind, ctxs, news, heads, group, dim, page, cap, window, score):
+    """Prompts that share their keys in a workgroup; the reference on the GPU in 64 bits, a head at a time."""
+    c = Cache(ctx, ctxs, news, heads, dim, page, sum(ctxs) + sum(news) + dim)
+    c.fill_new()
+    q = (torch.randn(c.tokens, heads * group, dim, generator=c.g) / 16).to(TYPES[kind])
+    cache = c.wrap(ctx)
+    bias = -math.log(max(ctxs) + max(news)) if score == "sigmoid" else 0.0
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), cap=cap, window=window, score=score, bias=bias, max_new=max(news), max_length=max(a + b for a, b in zip(ctxs, news)))
+    cache.check()
+    for i, (ctx_len, new) in enumerate(zip(ctxs, news)):
+        first, n = int(c.begin[i]), ctx_len + new
+        at = torch.arange(ctx_len, n, device="cuda")[:, None]
+        key = torch.arange(n, device="cuda")
+        seen = (key <= at) & (key > at - window if window else key >= 0)
+        for h in range(heads if new else 0):
+            k, v = c.values("k", i, h).cuda(), c.values("v", i, h).cuda()
+            for j in range(h * group, (h + 1) * group):
+                s = q[first:first + new, j].cuda().double() @ k.T / math.sqrt(dim)
+                top = s.abs().amax(1, keepdim=True)
+                if cap:
+                    s = cap * torch.tanh(s / cap)
+                p = torch.softmax(s.masked_fill(~seen, -math.inf), 1) if score == "softmax" else torch.sigmoid(s + bias).masked_fill(~seen, 0)
+                out, size = p @ v, p @ v.abs()
+                # as in attention_near, with weights of 11 bits in either type: their roundings, each half a step at most, add up to no more than half a step of the sum of sizes
+                weight = 2.0 ** -11 + n * U32 + (top * 8 + 16 + 4 * cap) * 2 * U32
+                bound = half_step(kind) * out.abs() * (1 + 2.0 ** -7) + weight * size + n * 2.0 ** -25 * size.amax(1, keepdim=True) * 64 + torch.finfo(TYPES[kind]).smallest_normal * 2.0 ** -7
+                off = (got[first:first + new, j].double() - out).abs()
+                assert (off <= bound).all(), (i, j, (off / bound).max())
+    cache.free()
+
+
 @pytest.mark.parametrize("news", [[1], [90], [400]])
 def test_attention_with_scales_far_apart(ctx, news):
     """Value scales from 2^-60 to 2^100 in one sequence: the tokens that a row leans on decide, and what is small beside them is lost only beside them."""
@@ -411,6 +460,46 @@ def test_attention_with_scales_far_apart(ctx, news):
     got = ctx.clear_attention(cache, *c.where, q.cuda(), window=100)
     attention_near(c, "bf16", got, q, window=100)
     cache.free()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("window", [0, 700])
+def test_attention_of_prompts_with_nan_and_scales_far_apart(ctx, score, window):
+    """A long prompt whose keys are shared in workgroups: a NaN among the values of one head reaches its place in the rows that see it, one among another's keys the whole
+    rows that see it; a third head's value scales are far apart."""
+    c = Cache(ctx, [50], [1800], 8, 64, 16, 7)
+    c.fill_new()
+    page = lambda p: int(c.table[0, p // 16])  # noqa: E731
+    for b in range(1850 // 16 + 1):
+        c.scales["v"][page(16 * b), 5, 0] = 2.0 ** (-60 if b % 2 else -30)
+    c.scales["v"][page(900), 5, 0] = 2.0 ** 100
+    q = (torch.randn(c.tokens, 32, 64, generator=c.g) / 16).to(torch.bfloat16)
+    call = lambda: ctx.clear_attention(c.wrap(ctx), *c.where, q.cuda(), window=window, score=score).cpu()  # noqa: E731
+    clean = call()
+    assert clean.isfinite().all()
+    at_v, at_k = 777, 1001
+    c.codes["v"][page(at_v), 2, at_v % 16, 11] = 0xff
+    c.codes["k"][page(at_k), 6, at_k % 16, 3] = 0x7f
+    got = call()
+    pos = torch.arange(50, 1850)
+    sees = lambda p: (pos >= p) & (pos - window < p if window else pos >= 0)  # noqa: E731
+    want = clean.clone()
+    want[sees(at_v), 8:12, 11] = math.nan
+    want[sees(at_k), 24:28] = math.nan
+    assert torch.equal(got.isnan(), want.isnan())
+    # (its code counts as 0 where it is not seen, and the other heads are as they were)
+    assert torch.equal(got.nan_to_num(), want.nan_to_num())
+    # the head with scales far apart, against the definition
+    k, v = c.values("k", 0, 5).cuda(), c.values("v", 0, 5).cuda()
+    key, at = torch.arange(1850, device="cuda"), pos.cuda()[:, None]
+    seen = (key <= at) & (key > at - window if window else key >= 0)
+    for j in range(20, 24):
+        s = q[:, j].cuda().double() @ k.T / 8
+        p = torch.softmax(s.masked_fill(~seen, -math.inf), 1) if score == "softmax" else torch.sigmoid(s).masked_fill(~seen, 0)
+        out, size = p @ v, p @ v.abs()
+        bound = half_step("bf16") * out.abs() * 1.01 + (2.0 ** -11 + 1850 * U32 + (s.abs().amax(1, keepdim=True) * 8 + 16) * 2 * U32) * size + 1850 * 2.0 ** -25 * size.amax(1, keepdim=True) * 64 + 2.0 ** -133
+        off = (got[:, j].cuda().double() - out).abs()
+        assert (off <= bound).all(), (off / bound).max()
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
