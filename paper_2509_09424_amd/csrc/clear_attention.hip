@@ -678,14 +678,13 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
                     for (int r = 0; r < 16; r++) o[j][r] *= f;
                 st_l = st_l * lift * lift;
             }
-            // the values of the first two blocks on their way while the weights are formed
+            // the values of the first block on their way while the weights are formed (those of two would not fit the registers at 128 places)
             f16x8 vf[2][TILES];
             const auto read_values = [&](int b) {
 #pragma unroll
                 for (int j = 0; j < TILES; j++) vf[b % 2][j] = *(const f16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 16 * ((2 * b + half) ^ (2 * (j % 2) + n / 16)));
             };
             read_values(0);
-            read_values(1);
             __builtin_amdgcn_sched_barrier(0);
             union Weights {
                 _Float16 e[8];
@@ -725,6 +724,8 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
                         }
                 }
             }
+            read_values(1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int b = 0; b < 4; b++) {
 #pragma unroll
