@@ -448,7 +448,7 @@ int ensi_ccmm_av(ensi_ctx *ctx, const ensi_gk *rk, const ensi_gk *gk, const ensi
 #define ENSI_T_BF16 1
 #define ENSI_T_F16 2
 
-/* Root-mean-square norm with the residual's addition and an output in 8 bits.  Per row of d elements (1 <= d <= 32768):
+/* Root-mean-square norm with the residual's addition and an output in 8 bits.  Per row of d elements (1 <= d <= 32768, up to 2^21 rows):
  *   h = x + residual, rounded to the type (h = x without a residual); p_i = h_i gain_i; most = max |p_i|
  *   codes_i = p_i (127 (1 / most)) rounded to the nearest whole number, ties to even
  *   scale = most / (127 sqrt(mean h^2 + eps)), so that codes_i scale is the normed value;  out_i = p_i / sqrt(mean h^2 + eps)

@@ -7,6 +7,7 @@
 #include "clear.h"
 
 #define CLEAR_MAX_HEADS 4096
+#define CLEAR_MAX_NORM_ROWS (1 << 21)  // a grid has fewer than 2^32 threads, a row up to 1024 of them
 #define CLEAR_MAX_SEQS 65535      // a grid's third dimension
 #define CLEAR_MAX_NEW (1 << 20)   // its second one, in blocks of 16 tokens
 
@@ -35,7 +36,8 @@ extern "C" int ensi_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args *a, voi
     if (!ctx || !a) return ENSI_E_BADARG;
     const int size = type_size(a->type);
     if (!size) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: unknown type %d", a->type);
-    if (a->d < 1 || a->d > 32768 || a->rows < 0 || a->rows > INT32_MAX) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear norm: %lld rows of %d elements (1 to 32768)", (long long)a->rows, a->d);
+    if (a->d < 1 || a->d > 32768 || a->rows < 0 || a->rows > CLEAR_MAX_NORM_ROWS)
+        ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear norm: %lld rows (up to %d) of %d elements (1 to 32768)", (long long)a->rows, CLEAR_MAX_NORM_ROWS, a->d);
     if (!(a->eps >= 0)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: eps must not be negative");
     if (a->rows == 0) return ENSI_OK;
     if (!a->x || !a->gain) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: x and gain are needed");

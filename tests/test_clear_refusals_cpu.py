@@ -67,6 +67,7 @@ norm(BADARG, "type", type=3)
 norm(SHAPE, "elements", d=0)
 norm(SHAPE, "elements", d=32769)
 norm(SHAPE, "elements", rows=-1)
+norm(SHAPE, "elements", rows=(1 << 21) + 1)
 norm(BADARG, "eps", eps=-1.0)
 norm(BADARG, "eps", eps=float("nan"))
 norm(BADARG, "gain", gain=0)
