@@ -591,6 +591,91 @@ def test_empty_calls(ctx):
     cache.free()
 
 
+# ---- offsets past 32 bits ---------------------------------------------------------------------------------------------------
+
+
+def test_product_and_norm_past_32_bits(ctx):
+    """Codes, outputs and sums with more than 2^31 elements: the last rows are what a call of these rows alone gives."""
+    rows, d, m, last = 70000, 32768, 32000, 600
+    x = torch.zeros(rows, d, dtype=torch.bfloat16, device="cuda")
+    x[-last:] = torch.randn(last, d, generator=gen(1)).to(torch.bfloat16).cuda()
+    gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(x)
+    codes, scales = ctx.clear_norm(x, gain, out=out, codes=torch.empty(rows, d, dtype=torch.int8, device="cuda"))
+    few_out = torch.empty_like(x[-last:])
+    few_codes, few_scales = ctx.clear_norm(x[-last:], gain, out=few_out, codes=torch.empty(last, d, dtype=torch.int8, device="cuda"))
+    near = 64 * U32  # of each from the sum of squares, as in test_norm
+    assert torch.equal(codes[-last:], few_codes) and not codes[:-last].any() and not scales[:-last].any()
+    assert ((scales[-last:].double() - few_scales.double()).abs() <= 2 * near * few_scales.double()).all()
+    assert ((out[-last:].double() - few_out.double()).abs() <= (2 * near + 2 * half_step("bf16")) * few_out.double().abs() * (1 + 2.0 ** -7)).all()
+    del x, out
+    W = torch.randint(-1, 2, (64, m), generator=gen(2)).to(torch.int8)
+    weights = ctx.clear_weights_prepare(W.numpy(), np.full(m, 0.5, dtype=np.float32))
+    narrow = codes[:, -64:]  # rows of 64 codes, 32768 apart
+    scales = torch.ones(rows, device="cuda")
+    got = ctx.clear_matmul(weights, narrow, scales, dtype=torch.bfloat16)
+    few = ctx.clear_matmul(weights, few_codes[:, -64:], scales[:last], dtype=torch.bfloat16)
+    want = few_codes[:, -64:].double() @ W.cuda().double() * 0.5
+    assert torch.equal(got[-last:], few) and torch.equal(few, want.to(torch.bfloat16)) and not got[:-last].any()
+    weights.free()
+
+
+@pytest.mark.parametrize("news", [[1], [3], [900]])
+def test_pages_past_32_bits(ctx, news):
+    """A cache of 4.6 GiB for keys and as much for values, pages at its end, held as e4m3: the codes and outputs of a small one of bytes, bit for bit."""
+    heads, dim, page = 8, 128, 64
+    c = Cache(ctx, [200], news, heads, dim, page, 21)
+    q = (torch.randn(c.tokens, 2 * heads, dim, generator=c.g) / 16).to(torch.bfloat16).cuda()
+    kv = [torch.randn(c.tokens, heads, dim, generator=c.g).to(torch.bfloat16).cuda() for _ in "kv"]
+    small = c.wrap(ctx)
+    pages, mine = 75000, len(c.codes["k"])
+    far = pages - mine
+    big = [torch.zeros(pages, heads, page, dim, dtype=torch.uint8, device="cuda") for _ in "kv"] + [torch.ones(pages, heads, page // 16, device="cuda") for _ in "kv"]
+    for b, t in zip(big, c.dev):
+        b[far:] = t
+    large = ctx.clear_cache(*(b.view(torch.float8_e4m3fn) for b in big[:2]), *big[2:])
+    table, begin, lengths = c.where
+    results = []
+    for cache, where in ((small, table), (large, torch.where(table < 0, table, table + far))):
+        ctx.clear_append(cache, where, begin, lengths, *kv, None, None)
+        results.append(ctx.clear_attention(cache, where, begin, lengths, q, max_new=news[0], max_length=200 + news[0]))
+        cache.check()
+    for b, t in zip(big, c.dev):
+        assert torch.equal(b[far:].view(torch.uint8), t.view(torch.uint8))
+        assert (b[:far] == (1 if b.is_floating_point() else 0)).all()
+    assert torch.equal(*results)
+    small.free()
+    large.free()
+
+
+def test_most_rows_and_largest_bounds(ctx):
+    """The most rows of a product and of a norm, and the largest bounds that a caller may give: the results of ordinary calls."""
+    rows = 1 << 20
+    W = torch.randint(-1, 2, (70, 16), generator=gen(3)).to(torch.int8)
+    weights = ctx.clear_weights_prepare(W.numpy(), np.full(16, 0.5, dtype=np.float32))
+    codes = torch.randint(-128, 128, (rows, 70), generator=gen(4)).to(torch.int8).cuda()
+    got = ctx.clear_matmul(weights, codes, torch.ones(rows, device="cuda"), dtype=torch.float32)
+    assert torch.equal(got, (codes.float() @ W.cuda().float()) * 0.5)  # sums of whole numbers up to 70 x 128: exact
+    weights.free()
+    x = torch.ones(2 * rows, 9, dtype=torch.bfloat16, device="cuda")
+    codes, scales = ctx.clear_norm(x, x[0], codes=torch.zeros(2 * rows, 9, dtype=torch.int8, device="cuda"))
+    assert (codes == 127).all() and (scales == scales[0]).all()
+    c = Cache(ctx, [40, 3], [20, 1], 1, 64, 16, 22)
+    q = (torch.randn(c.tokens, 2, 64, generator=c.g) / 16).to(torch.bfloat16)
+    kv = torch.randn(c.tokens, 2, 64, generator=c.g).to(torch.bfloat16).cuda()
+    results = []
+    for bounds in ((20, 60), (1 << 20, 1 << 30)):
+        cache = c.wrap(ctx)
+        ctx.clear_append(cache, *c.where, kv[:, :1], kv[:, 1:], None, None, max_new=bounds[0])
+        got = ctx.clear_attention(cache, *c.where, q.cuda(), max_new=bounds[0], max_length=bounds[1])
+        cache.check()
+        results.append([t.nan_to_num(nan=-1.0) if t.is_floating_point() else t for t in c.dev])
+        c.codes, c.scales = {"k": c.dev[0].cpu(), "v": c.dev[1].cpu()}, {"k": c.dev[2].cpu(), "v": c.dev[3].cpu()}
+        attention_near(c, "bf16", got, q)
+        cache.free()
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
 # ---- streams and graphs -----------------------------------------------------------------------------------------------------
 
 
