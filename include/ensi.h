@@ -439,7 +439,8 @@ int ensi_ccmm_av(ensi_ctx *ctx, const ensi_gk *rk, const ensi_gk *gk, const ensi
 /* ---- the decoder layer on clear activations ------------------------------------------------------------------
  * The same ternary layer for activations that are not encrypted: what a decrypted result is compared with, what scales and
  * levels are chosen by, and the path of requests that need no encryption.  Activations are device arrays of one ENSI_T_* type;
- * products, sums, norms and softmax statistics are held in 32 bits and rounded once at the end.  Strides are in elements.
+ * products, sums, norms and softmax statistics are held in 32 bits and rounded once at the end; the weights of the attention enter
+ * their product with the values in 16 bits (two terms of bf16: half a step of 2^-16, and the exponents of 32 bits).  Strides are in elements.
  * These calls only enqueue kernels on the stream, allocate nothing and may be captured into a graph.  Calls of one context must
  * not overlap on different streams (ensi_clear_attention has a workspace).
  * What lies on the device (lengths, tables) cannot be checked by a call that does not wait: the kernels check it,

@@ -3,8 +3,10 @@
 // Keys are codes c with a power of two s as scale, so q k = s (q c): codes widen to the queries' 16 bits without rounding, the matrix instruction
 // forms q c in 32 bits, and the scale enters with the factor that the exponent needs anyway.  Values v = s' c' are folded the other way round: their
 // scale multiplies the weight.  With t the score in units of log2 e, the running reference M is the maximum of t + log2 s'; e = 2^(t - M) is what the
-// softmax's sum adds up, w = e s' <= 1 the weight of the code c'.  Scales are 2^-64 to 2^120, so the largest e of a row is 2^-120 to 2^64 and
-// its sum in 32 bits loses nothing, and the largest weight is 1: weights in 16 bits lose only what is 2^-24 of the row's largest contribution.
+// softmax's sum adds up, w = e s' <= 1 the weight of the code c'.  The matrix instruction takes weights as two terms of bf16, the nearest one and the nearest to what
+// is left, 16 bits together with the exponents of 32 (f16 would end 2^-40 below the largest weight at best, and where the largest one's values are 0 the small ones
+// are the result).  Both are held lifted: scales are 2^-64 to 2^120, so the largest e 2^32 is 2^-88 to 2^96 and sums of 2^30 of them stay in range,
+// and w 2^70 leaves 2^-196 of the largest weight and sums of 2^30 products with codes in range.
 //   sigmoid scores need no sum; w = sigmoid(t) s' 2^-M with the same reference.
 // A tile of scores is held as [key][query]: a lane has one query, so the statistics of a row are per lane, and the weights leave the score's
 // registers in the order in which the second product reads them; the order of its keys is that of the registers, for the values too.
@@ -154,7 +156,47 @@ struct Rows16 {
             for (int r = 0; r < 4; r++) o[j][r] *= f;
     }
 };
-// 2^(from - to) in two equal factors: references may be 184 apart by their scales alone, which a sum has to survive
+// 2^32 on the terms e of a softmax's sum, 2^70 on the weights
+#define SUM_LIFT 32
+#define WEIGHT_LIFT 70
+// The weight of a term e = 2^(t - M + SUM_LIFT) and its value's scale s': 2^31 and 2^7 keep both factors in range whatever s' is.
+__device__ __forceinline__ float weight_of(float e, float scale) { return e * 0x1p31f * (scale * 0x1p7f); }
+static_assert(WEIGHT_LIFT == SUM_LIFT + 31 + 7, "lifts of weight_of");
+// Eight weights in two terms of bf16, set in twos: either term of both in one conversion
+struct Weights {
+    union {
+        u32 w[4];
+        bf16x8 v;
+    } hi, lo;
+    static __device__ __forceinline__ u32 pack(float a, float b) {
+        const bf16x2 v = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(u32, v);
+    }
+    __device__ __forceinline__ void set(int i, float a, float b) {
+        u32 w = pack(a, b);
+        asm("" : "+v"(w));  // (the compiler would convert `a` once more by itself)
+        hi.w[i / 2] = w;
+        lo.w[i / 2] = pack(a - __builtin_bit_cast(float, w << 16), b - __builtin_bit_cast(float, w & 0xffff0000));
+    }
+};
+// What turns a row's sums into its outputs, 2^e f: the reference of sigmoid scores, or the softmax's sum l.  Factor and exponent apart, as their product can leave the range.
+struct Last {
+    float f;
+    int e;
+    __device__ __forceinline__ float operator()(float o) const { return __builtin_ldexpf(o * f, e); }
+};
+template <int SCORE>
+__device__ __forceinline__ Last last_of(float m, float l) {
+    if (SCORE == ENSI_SCORE_SIGMOID) {
+        const float whole = floorf(m);
+        return {__builtin_amdgcn_exp2f(m - whole), (int)whole - WEIGHT_LIFT};
+    }
+    if (l == 0) return {0, 0};
+    return {1.0f / __builtin_amdgcn_frexp_mantf(l), SUM_LIFT - WEIGHT_LIFT - __builtin_amdgcn_frexp_expf(l)};
+}
+// 2^(from - to) in two equal factors: references may be 184 apart by their scales alone, which sums have to survive: the factors enter one after the other
+// where their product would be small
+#define HALF_LIFT_DEEP 0x1p-32f
 __device__ __forceinline__ float half_lift(float from, float to) { return from == to ? 1.0f : __builtin_amdgcn_exp2f(0.5f * (from - to)); }
 
 // Keys split over waves and workgroups: few rows, long caches.  A workgroup has one tile of 16 rows of a key head and `split` of its keys; its four
@@ -283,24 +325,25 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
             const float lift = half_lift(st.m, base);
             st.m = m;
             if (__any(lift != 1.0f)) {
-                st.scale(lift * lift);
+                const bool deep = __any(lift < HALF_LIFT_DEEP);
+                if (deep) st.scale(lift);
+                st.scale(deep ? lift : lift * lift);
                 st.l = st.l * lift * lift;
             }
-            union {
-                _Float16 e[8];
-                f16x8 v;
-            } p, p_lo;
+            Weights p;
+            const float unit = __builtin_amdgcn_exp2f(0.5f * (WEIGHT_LIFT - base));  // sigmoid: half of the way to the reference
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const float to = SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(-base) : vs[h];
+            for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const float e = SCORE == ENSI_SCORE_SIGMOID ? u[h][r] : __builtin_amdgcn_exp2f(u[h][r] - base), w = e * to;
-                    st.l += e;
-                    p.e[4 * h + r] = (_Float16)w;
-                    p_lo.e[4 * h + r] = (_Float16)(w - (float)p.e[4 * h + r]);
+                for (int r = 0; r < 4; r += 2) {
+                    if (SCORE == ENSI_SCORE_SIGMOID) {
+                        p.set(4 * h + r, u[h][r] * unit * unit, u[h][r + 1] * unit * unit);
+                    } else {
+                        const float e0 = __builtin_amdgcn_exp2f(u[h][r] - (base - SUM_LIFT)), e1 = __builtin_amdgcn_exp2f(u[h][r + 1] - (base - SUM_LIFT));
+                        st.l += e0 + e1;
+                        p.set(4 * h + r, weight_of(e0, vs[h]), weight_of(e1, vs[h]));
+                    }
                 }
-            }
             u32 nans = 0;
 #pragma unroll
             for (int h = 0; h < 2; h++)
@@ -333,9 +376,9 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
                 for (int b = 0; b < 4; b++) {
                     const int j = 4 * x + b;
                     if (j >= TILES) continue;
-                    const f16x8 v = Wide<ENSI_T_F16>::widen(now.v[0][x][b], now.v[1][x][b]);
-                    st.o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p.v, st.o[j], 0, 0, 0);
-                    if (TYPE == ENSI_T_F16) st.o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p_lo.v, st.o[j], 0, 0, 0);
+                    const bf16x8 v = Wide<ENSI_T_BF16>::widen(now.v[0][x][b], now.v[1][x][b]);
+                    st.o[j] = Wide<ENSI_T_BF16>::mfma16(v, p.hi.v, st.o[j]);
+                    st.o[j] = Wide<ENSI_T_BF16>::mfma16(v, p.lo.v, st.o[j]);
                 }
             }
         }
@@ -368,12 +411,12 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
         __syncthreads();
         if (wave < half) {
             const float om = part_m[wave][lane], m = most_of(st.m, om), base = m == -__builtin_inff() ? 0.0f : m;
-            const float h0 = half_lift(st.m, base), h1 = half_lift(om, base), mine = h0 * h0, other = h1 * h1;
+            const float h0 = half_lift(st.m, base), h1 = half_lift(om, base);
 #pragma unroll
             for (int j = 0; j < TILES; j++) {
                 const f32x4 o = part_o[wave][j][lane];
 #pragma unroll
-                for (int r = 0; r < 4; r++) st.o[j][r] = st.o[j][r] * mine + o[r] * other;
+                for (int r = 0; r < 4; r++) st.o[j][r] = st.o[j][r] * h0 * h0 + o[r] * h1 * h1;
             }
             st.l = st.l * h0 * h0 + part_l[wave][lane] * h1 * h1;
             st.m = m;
@@ -382,7 +425,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
     }
     if (wave != 0 || n >= rt.rows) return;
     const bool whole = rt.tiles <= split_tiles;
-    const float f = !whole ? 1.0f : SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(st.m) : st.l == 0 ? 0.0f : 1.0f / st.l;
+    const Last end = last_of<SCORE>(st.m, st.l);
     float *ws = a.ws + (((int64_t)seq * gridDim.x + blockIdx.x) * a.splits + split) * (16 * DIM + 32);
     T *out = (T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM;
     const auto put = [&](int at, auto first, auto count) {  // registers r of tiles first .. first + count - 1, at place `at` of the row
@@ -390,9 +433,9 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
         for (int r = 0; r < 4; r++)
 #pragma unroll
             for (int j = 0; j < decltype(count)::value; j++) {
-                const float v = st.o[decltype(first)::value + j][r] * f;
+                const float v = st.o[decltype(first)::value + j][r];
                 const int d = at + decltype(count)::value * (4 * g + r) + j;
-                if (whole) out[d] = (T)v;
+                if (whole) out[d] = (T)end(v);
                 else ws[n * DIM + d] = v;
             }
     };
@@ -433,7 +476,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_join(AttentionView a, i
     most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
     if (most == -__builtin_inff()) most = 0;
     const float h = half_lift(m, most);
-    if (t < splits) factor[t] = h * h;
+    if (t < splits) factor[t] = h;
     l = t < splits ? l * h * h : 0;
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) l += __shfl_xor(l, k);
@@ -446,28 +489,29 @@ __global__ __launch_bounds__(256) void k_clear_attention_join(AttentionView a, i
             const f32x4 v = *(const f32x4 *)(ws + (int64_t)s * (16 * DIM + 32) + n * DIM + 4 * quad);
             const float f = factor[s];
 #pragma unroll
-            for (int i = 0; i < 4; i++) o[i] = __builtin_fmaf(v[i], f, o[i]);
+            for (int i = 0; i < 4; i++) o[i] = __builtin_fmaf(v[i] * f, f, o[i]);
         }
         parts[slice][quad] = o;
     }
     __syncthreads();
     if (t >= QUADS) return;
     l = sums[0] + sums[1] + sums[2] + sums[3];
-    const float f = SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(most) : l == 0 ? 0.0f : 1.0f / l;
+    const Last end = last_of<SCORE>(most, l);
     o = (f32x4){0, 0, 0, 0};
     for (int s = 0; s < SLICES; s++) o += parts[s][t];
     const int row = 16 * tile + n, token = part.first + row / a.group, q_head = head * a.group + row % a.group;
     typedef T quad_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     quad_t w;
 #pragma unroll
-    for (int i = 0; i < 4; i++) w[i] = (T)(o[i] * f);
+    for (int i = 0; i < 4; i++) w[i] = (T)end(o[i]);
     *(quad_t *)((T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM + 4 * t) = w;
 }
 
 // Rows split over waves, keys shared: many rows (prompts).  A workgroup has 128 rows of a key head, 32 to a wave, and walks their keys in tiles of 64.
 // A wave fetches one block of 16 keys and values of a tile (the codes of the next tile are under way while one is computed), widens them to 16 bits and puts them into
-// LDS, values transposed and in the order in which the score's registers hold their keys; two buffers, one barrier a tile.  The matrix cores,
-// LDS reads (32 KB a wave and tile at 128 places) and the softmax's vector instructions are about equally busy.
+// LDS, values transposed and in the order in which the score's registers hold their keys; two buffers, one barrier a tile.  Matrix instructions (48 a wave and tile at
+// 128 places, a third of them for the weights' second term: 252 us without it, 310 with it for 2048 + 4096 tokens of 20 over 5 heads) and the softmax's vector
+// instructions (three more a weight for the two terms) decide; LDS reads are 32 KB a wave and tile.
 template <int DIM>
 struct RowsLds {
     static constexpr int KEYS = 64, K_ROW = DIM * 2 + 16, V_ROW = KEYS * 2 + 16;  // bytes; 16 more keep the rows of a fragment on different banks,
@@ -582,7 +626,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
                 transpose4(x[0]);
                 transpose4(x[1]);
 #pragma unroll
-                for (int j = 0; j < 4; j++) *(f16x8 *)(at + L::K_BYTES + (places + j) * L::V_ROW + 16 * ((2 * wave + h) ^ (places / 16 % 4))) = Wide<ENSI_T_F16>::widen(x[0][j], x[1][j]);
+                for (int j = 0; j < 4; j++) *(bf16x8 *)(at + L::K_BYTES + (places + j) * L::V_ROW + 16 * ((2 * wave + h) ^ (places / 16 % 4))) = Wide<ENSI_T_BF16>::widen(x[0][j], x[1][j]);
             }
         }
     };
@@ -671,67 +715,65 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
             const float lift = half_lift(st_m, base);
             st_m = m;
             if (__any(lift != 1.0f)) {
-                const float f = lift * lift;
+                const bool deep = __any(lift < HALF_LIFT_DEEP);
+                const auto scale = [&](float f) {
 #pragma unroll
-                for (int j = 0; j < TILES; j++)
+                    for (int j = 0; j < TILES; j++)
 #pragma unroll
-                    for (int r = 0; r < 16; r++) o[j][r] *= f;
+                        for (int r = 0; r < 16; r++) o[j][r] *= f;
+                };
+                if (deep) scale(lift);
+                scale(deep ? lift : lift * lift);
                 st_l = st_l * lift * lift;
             }
-            // the values of the first block on their way while the weights are formed (those of two would not fit the registers at 128 places)
-            f16x8 vf[2][TILES];
+            // A block of 16 keys at a time: its values are read and its weights formed while the matrix cores have the block before (the weights of all four in two terms
+            // would not fit the registers at 128 places).
+            bf16x8 vf[2][TILES];
             const auto read_values = [&](int b) {
 #pragma unroll
-                for (int j = 0; j < TILES; j++) vf[b % 2][j] = *(const f16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 16 * ((2 * b + half) ^ (2 * (j % 2) + n / 16)));
+                for (int j = 0; j < TILES; j++) vf[b % 2][j] = *(const bf16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 16 * ((2 * b + half) ^ (2 * (j % 2) + n / 16)));
+            };
+            // With all value scales so far between 2^-40 and 2^40 the weight 2^(t + log2 s' - M) can be formed at once and divided by s' for the sum, a block at a
+            // time: a weight is lost below 2^-196 of the largest one, which is below 2^-116 of the sum's largest term.
+            wide |= fmaxf(fmaxf(fabsf(lv[0]), fabsf(lv[1])), fmaxf(fabsf(lv[2]), fabsf(lv[3]))) > 40;
+            const float unit = __builtin_amdgcn_exp2f(0.5f * (WEIGHT_LIFT - base));  // sigmoid: half of the way to the reference
+            Weights p[2];
+            const auto weigh = [&](int b) {
+                Weights &to = p[b % 2];
+                if (SCORE == ENSI_SCORE_SIGMOID) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) to.set(e, u[b][e] * unit * unit, u[b][e + 1] * unit * unit);
+                } else if (!wide) {
+                    const float shift = lv[b] - (base - WEIGHT_LIFT);
+                    float sum = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], shift)), w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e + 1], factor[b], shift));
+                        sum += w0 + w1;
+                        to.set(e, w0, w1);
+                    }
+                    st_l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vs[b] * 0x1p38f), st_l);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], SUM_LIFT - base)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e + 1], factor[b], SUM_LIFT - base));
+                        st_l += e0 + e1;
+                        to.set(e, weight_of(e0, vs[b]), weight_of(e1, vs[b]));
+                    }
+                }
             };
             read_values(0);
             __builtin_amdgcn_sched_barrier(0);
-            union Weights {
-                _Float16 e[8];
-                f16x8 v;
-            } p[4];
-            if (SCORE == ENSI_SCORE_SIGMOID) {
-                const float unit = __builtin_amdgcn_exp2f(-base);
-#pragma unroll
-                for (int b = 0; b < 4; b++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) p[b].e[e] = (_Float16)(u[b][e] * unit);
-            } else {
-                // With all value scales so far between 2^-40 and 2^40 the weight 2^(t + log2 s' - M) can be formed at once and divided by s' for the sum, a block at a
-                // time: what is lost of the sum is below 2^-46 of its largest term.
-                wide |= fmaxf(fmaxf(fabsf(lv[0]), fabsf(lv[1])), fmaxf(fabsf(lv[2]), fabsf(lv[3]))) > 40;
-                if (!wide) {
-#pragma unroll
-                    for (int b = 0; b < 4; b++) {
-                        const float shift = lv[b] - base;
-                        float sum = 0;
-#pragma unroll
-                        for (int e = 0; e < 8; e++) {
-                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], shift));
-                            sum += w;
-                            p[b].e[e] = (_Float16)w;
-                        }
-                        st_l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vs[b]), st_l);
-                    }
-                } else {
-#pragma unroll
-                    for (int b = 0; b < 4; b++)
-#pragma unroll
-                        for (int e = 0; e < 8; e++) {
-                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], -base));
-                            st_l += w;
-                            p[b].e[e] = (_Float16)(w * vs[b]);
-                        }
-                }
-            }
-            read_values(1);
-            __builtin_amdgcn_sched_barrier(0);
+            weigh(0);
 #pragma unroll
             for (int b = 0; b < 4; b++) {
-#pragma unroll
-                for (int j = 0; j < TILES; j++) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[b % 2][j], p[b].v, o[j], 0, 0, 0);
+                if (b + 1 < 4) read_values(b + 1);
                 __builtin_amdgcn_sched_barrier(0);
-                if (b + 2 < 4) read_values(b + 2);
+#pragma unroll
+                for (int j = 0; j < TILES; j++) o[j] = Wide<ENSI_T_BF16>::mfma32(vf[b % 2][j], p[b % 2].hi.v, o[j]);
+#pragma unroll
+                for (int j = 0; j < TILES; j++) o[j] = Wide<ENSI_T_BF16>::mfma32(vf[b % 2][j], p[b % 2].lo.v, o[j]);
+                if (b + 1 < 4) weigh(b + 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -752,7 +794,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
     }
     st_l += __shfl_xor(st_l, 32);
     if (row0 + n >= part.count * a.group) return;
-    const float f = SCORE == ENSI_SCORE_SIGMOID ? __builtin_amdgcn_exp2f(st_m) : st_l == 0 ? 0.0f : 1.0f / st_l;
+    const Last end = last_of<SCORE>(st_m, st_l);
     T *out = (T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM;
 #pragma unroll
     for (int j = 0; j < TILES; j++)
@@ -761,19 +803,19 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
             typedef T quad __attribute__((ext_vector_type(4), aligned(sizeof(T))));
             quad w;
 #pragma unroll
-            for (int i = 0; i < 4; i++) w[i] = (T)(o[j][4 * e + i] * f);
+            for (int i = 0; i < 4; i++) w[i] = (T)end(o[j][4 * e + i]);
             *(quad *)(out + 32 * j + 8 * e + 4 * half) = w;
         }
 }
 
-// Whether rows are split over waves and their keys shared, or keys over waves: microseconds of either as measured (bf16, no cap).  Rows: for a tile of 64 keys 1.4 up to 96
-// places of a head, 1.75 at 128, 2.8 at 192, 3.5 at 256, while two workgroups of 128 rows find room on a CU (one from 192 on); 500 + 1024 tokens of 20 over 5 heads of 128
-// 50, 100 + 2048 73, 2048 + 4096 286.  Keys: 60e6 products of a query, a key and a place in 1: these three 55, 118 and 577; 500 + 512 tokens 28 (rows 35), five prompts of 77
-// behind up to 1500 on 16 heads of 96 21 (45), 1000 + 1000 of 16 over 4 heads of 256 94 (112).
+// Whether rows are split over waves and their keys shared, or keys over waves: microseconds of either as measured (bf16, no cap).  Rows: for a tile of 64 keys 1.8 at 64
+// places of a head, 2.05 at 96, 2.35 at 128, 3.05 at 192, 4.2 at 256, while two workgroups of 128 rows find room on a CU (one from 192 on); 500 + 1024 tokens of 20 over 5
+// heads of 128 61, 100 + 2048 85, 2048 + 4096 317.  Keys: 50e6 to 90e6 products of a query, a key and a place in 1: these three 57, 101 and 504; 500 + 512 tokens 27 (rows 41),
+// five prompts of 77 behind up to 1500 on 16 heads of 96 23 (55), 500 + 2000 of these 78 (86), 1000 + 1000 of 16 over 4 heads of 256 92 (137).
 static bool attention_by_rows(const AttentionView &v, int span) {
     const int dim = v.kv.dim;
     const double blocks = (double)v.s.seqs * v.kv.heads * (((int64_t)v.s.max_new * v.group + 127) / 128);
-    const double rows_us = 4 + (span + 63) / 64 * std::max(1.4, dim / 73.0) * std::max(1.0, blocks / (dim <= 128 ? 400 : 256));
+    const double rows_us = 4 + (span + 63) / 64 * (0.95 + 0.0115 * dim) * std::max(1.0, blocks / (dim <= 128 ? 400 : 256));
     const double pairs = (double)v.s.seqs * v.s.max_new * v.q_heads * (v.window > 0 ? span : std::max(span - v.s.max_new / 2, 1));
     const double keys_us = 6 + pairs * dim / 60e6;
     return v.s.max_new > 1 && rows_us < keys_us;

@@ -1,0 +1,154 @@
+"""Attention on clear activations against 64 bits with bounds for each place of each row: of the row's own keys and of that place's own terms, so that what a row's
+largest contribution would hide is seen where that contribution has no part."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_gpu_clear import CASES, TYPES, U32, Cache, ctx, gen, half_step  # noqa: E402, F401
+
+PAIR = 2.0 ** -16  # weights in two terms of bf16: half a step of one of them, of half a step of the other
+
+
+def definition(c, q, i, h, j, cap, window, score, bias):
+    """Of sequence i and query head j over key head h, in 64 bits: outputs, the sum of their terms' sizes, and what the weights may be off by beside the roundings to 16 bits, relatively."""
+    first, new = int(c.begin[i]), c.news[i]
+    n = c.ctxs[i] + new
+    k, v, x = c.values("k", i, h).cuda(), c.values("v", i, h).cuda(), q[first:first + new, j].cuda().double()
+    root = 1 / math.sqrt(c.dim)
+    t, sizes = x @ k.T * root, x.abs() @ k.abs().T * root
+    at, key = torch.arange(n - new, n, device="cuda")[:, None], torch.arange(n, device="cuda")
+    dark = key > at
+    if window:
+        dark = dark | (key <= at - window)
+    t, sizes = t.masked_fill(dark, 0), sizes.masked_fill(dark, 0)
+    raw = t.abs().amax(1, keepdim=True)
+    if cap:
+        t = cap * torch.tanh(t / cap)
+    p = torch.softmax(t.masked_fill(dark, -math.inf), 1) if score == "softmax" else torch.sigmoid(t + bias).masked_fill(dark, 0)
+    v = v.masked_fill(~(p > 0).any(0)[:, None], 0)  # (NaN where nobody looks)
+    seen = (~dark).sum(1, keepdim=True)
+    # a score: `dim` products added in 32 bits, each addition a whole step of the sum of sizes at most; five roundings of its own (factor, scale, cap); the exponent's argument has four more at the
+    # size of scores, references and lifts in units of log2 e
+    scale = c.scales["v"].nan_to_num(1.0, 1.0, 1.0).clamp(2.0 ** -64, 2.0 ** 120).log2().abs().max()
+    off = 2 * U32 * (c.dim * sizes.amax(1, keepdim=True) + 5 * raw) + 4 * U32 * (1.5 * (t.abs().amax(1, keepdim=True) + abs(bias)) + float(scale) + 70)
+    # the running reference moves once a tile of 32 keys at most, six roundings each time; then sums over the row's keys, of weights and of products; functions to two steps
+    return p @ v, p @ v.abs(), 2 * off + U32 * (6 * seen / 32 + 2 * seen + 32)
+
+
+def check(c, kind, got, q, cap=0.0, window=0, score="softmax", bias=0.0, heads=None):
+    worst = 0.0
+    for i in range(len(c.ctxs)):
+        first, new = int(c.begin[i]), c.news[i]
+        group = q.shape[1] // c.heads
+        for j in () if not new else range(q.shape[1]) if heads is None else heads:
+            out, size, off = definition(c, q, i, j // group, j, cap, window, score, bias)
+            bound = half_step(kind) * (1 + 2.0 ** -7) * out.abs() + (PAIR + off) * size + torch.finfo(TYPES[kind]).smallest_normal * half_step(kind)
+            ratio = ((got[first:first + new, j].cuda().double() - out).abs() / bound).max().item()
+            assert ratio <= 1, (i, j, ratio)  # (also where it is NaN)
+            worst = max(worst, ratio)
+    return worst
+
+
+def longest(c):
+    return {"max_new": max(c.news), "max_length": max(a + b for a, b in zip(c.ctxs, c.news))}
+
+
+PROMPTS = [([70, 0], [1800, 1000], 8, 4, 64, 16, 0.0, 0, "softmax"), ([200], [1500], 8, 4, 128, 64, 0.0, 0, "softmax"), ([33], [1501], 8, 2, 96, 32, 20.0, 300, "softmax"),
+           ([10], [1500], 4, 6, 192, 16, 0.0, 0, "sigmoid"), ([100], [1450], 8, 4, 256, 64, 0.0, 500, "softmax"), ([5, 300, 40], [1500, 0, 911], 8, 2, 64, 48, 9.0, 0, "sigmoid")]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("ctxs, news, heads, group, dim, page, cap, window, score", CASES + PROMPTS)
+def test_every_place(ctx, kind, ctxs, news, heads, group, dim, page, cap, window, score):
+    c = Cache(ctx, ctxs, news, heads, dim, page, sum(ctxs) + 3 * sum(news) + dim)
+    c.fill_new()
+    q = (torch.randn(c.tokens, heads * group, dim, generator=c.g) / 16).to(TYPES[kind])
+    cache = c.wrap(ctx)
+    bias = -math.log(max(ctxs) + max(news)) if score == "sigmoid" else 0.0
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), cap=cap, window=window, score=score, bias=bias, **longest(c))
+    cache.check()
+    check(c, kind, got, q, cap, window, score, bias, None if group * heads < 8 else range(0, heads * group, 3))
+    cache.free()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("news", [[30], [1500, 1200, 700]])
+def test_values_that_cancel(ctx, kind, news):
+    """Neighbouring tokens have opposite values: the outputs are differences of nearly equal weights, whose roundings show.  Early tokens see few keys."""
+    c = Cache(ctx, [0] * len(news), news, 8 if len(news) > 1 else 2, 64, 16, 31)
+    c.fill_new(powers=(-3, -2))
+    for i, n in enumerate(news):
+        for p in range(1, n, 2):
+            one, r = int(c.table[i, p // 16]), p % 16
+            c.codes["v"][one, :, r] = c.codes["v"][one, :, r - 1] ^ 0x80
+    q = (torch.randn(c.tokens, 4 * c.heads, 64, generator=c.g) / 1024).to(TYPES[kind])
+    cache = c.wrap(ctx)
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), **longest(c))
+    check(c, kind, got, q, heads=range(0, 4 * c.heads, 3))
+    cache.free()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("nats", [14, 18, 26, 40])
+@pytest.mark.parametrize("ctxs, news, heads", [([700], [1], 1), ([3000], [1], 2), ([300], [40], 1), ([0], [1800], 16)])
+def test_a_key_that_takes_all_and_gives_nothing(ctx, kind, nats, ctxs, news, heads):
+    """The first token has e^nats times the weight of any other and values of 0 in half of the places: there the others are the result."""
+    c = Cache(ctx, ctxs, news, heads, 64, 16, 100 + nats, powers=(0, 1))
+    c.fill_new(powers=(0, 1))
+    for i in range(len(c.table)):  # score = first element of the key (queries are 8 e_0): small, and `nats` for the first token
+        for p in range(c.ctxs[i] + c.news[i]):
+            c.codes["k"][int(c.table[i, p // 16]), :, p % 16, 0] = (torch.randn(heads, generator=c.g) * 0.3).to(torch.float8_e4m3fn).view(torch.uint8)
+        one = int(c.table[i, 0])
+        c.codes["k"][one, :, 0, 0] = torch.tensor([float(nats)]).to(torch.float8_e4m3fn).view(torch.uint8)
+        c.codes["v"][one, :, 0, :32] = 0
+        for b in range(1, -(-(c.ctxs[i] + c.news[i]) // 16)):
+            c.scales["v"][int(c.table[i, b]), :, 0] = 2.0 ** 8
+    q = torch.zeros(c.tokens, 4 * heads, 64)
+    q[:, :, 0] = 8
+    q = q.to(TYPES[kind])
+    cache = c.wrap(ctx)
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), **longest(c))
+    check(c, kind, got, q, heads=range(0, 4 * heads, 5))
+    cache.free()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("news, heads", [([1], 1), ([90], 2), ([1700], 16)])
+def test_scales_far_apart_and_zeros_beside_the_large_ones(ctx, kind, news, heads):
+    """Value scales from 2^-60 to 2^100 (f16: 2^-4 to 2^6) in one sequence; the block with the largest has values in every other place only."""
+    low, mid, high = (-60, -30, 100) if kind == "bf16" else (-9, -4, 6)
+    c = Cache(ctx, [200], news, heads, 64, 16, 33)
+    c.fill_new()
+    for b in range((200 + news[0]) // 16 + 1):
+        c.scales["v"][int(c.table[0, b]), :, 0] = 2.0 ** (low if b % 2 else mid)
+    one = int(c.table[0, 2])
+    c.scales["v"][one, :, 0] = 2.0 ** high
+    c.codes["v"][one, :, :, ::2] = 0
+    q = (torch.randn(c.tokens, 4 * heads, 64, generator=c.g) / 16).to(TYPES[kind])
+    cache = c.wrap(ctx)
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), **longest(c))
+    check(c, kind, got, q, heads=range(0, 4 * heads, 5))
+    cache.free()
+
+
+@pytest.mark.parametrize("exponent", [120, -64])
+@pytest.mark.parametrize("news, heads", [([1], 1), ([40], 1), ([1700], 16)])
+def test_scales_at_either_end(ctx, exponent, news, heads):
+    """All value scales 2^120, or all 2^-64: the softmax's sum holds terms of e^-20 beside those of the largest score, which belong to a token without values."""
+    c = Cache(ctx, [400], news, heads, 64, 16, 35, powers=(0, 1))
+    c.fill_new(powers=(0, 1))
+    for p in range(400 + news[0]):
+        one, r = int(c.table[0, p // 16]), p % 16
+        c.codes["k"][one, :, r, 0] = torch.tensor([20.0 if p == 5 else 0.25 * (p % 3)]).to(torch.float8_e4m3fn).view(torch.uint8)
+        c.codes["v"][one, :, r] = 0 if p == 5 else torch.tensor([0.5 + p % 2]).to(torch.float8_e4m3fn).view(torch.uint8)
+        c.scales["v"][one, :, r // 16] = 2.0 ** exponent
+    q = torch.zeros(c.tokens, 4 * heads, 64)
+    q[:, :, 0] = 8
+    q = q.to(torch.bfloat16)
+    cache = c.wrap(ctx)
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), **longest(c))
+    check(c, "bf16", got, q, heads=range(0, 4 * heads, 5))
+    cache.free()
