@@ -85,17 +85,51 @@ __device__ __forceinline__ float most_of(float a, float b, float c) { return mos
 // Bit 7 of every byte whose code is NaN
 __device__ __forceinline__ u32 nan_bytes(u32 w) { return (w & 0x7f7f7f7f) + 0x01010101; }
 
-// The score t of a product q c, in units of the exponent: softmax log2 e t, sigmoid t log2 e + bias log2 e
-template <int SCORE, bool CAP>
-__device__ __forceinline__ float score_of(float qc, float scale, const AttentionView &a) {
-    float t = qc * (a.factor * scale);
-    if (CAP) {
-        // cap tanh(t / cap) = cap (1 - 2 / (1 + exp(2 t / cap)))
-        const float e = __builtin_amdgcn_exp2f(t * a.cap_inv);  // cap_inv = 2 log2 e / cap
-        t = a.cap - 2.0f * a.cap * __builtin_amdgcn_rcpf(1.0f + e);
-        t *= LOG2E;
-    }
-    return SCORE == ENSI_SCORE_SIGMOID ? t + a.bias : t;
+// cap tanh(t / cap) of all of a lane's scores.  Below half a cap t (1 + P((t / cap)^2)), the first seven terms of the series (2^-23 of it are left out at one half), beyond
+// cap (1 - 2 / (1 + exp(2 |t| / cap))): that difference would cancel for small scores, by 2^-23 of the cap.  A wave without a score beyond takes the series alone.
+template <int B, int E>
+__device__ __forceinline__ void cap_scores(float (&t)[B][E], float cap, float cap_inv) {
+    float most = 0;
+#pragma unroll
+    for (int b = 0; b < B; b++)
+#pragma unroll
+        for (int e = 0; e < E; e++) most = fmaxf(most, fabsf(t[b][e]));
+    const bool beyond = __any(most * cap_inv >= 0.5f);
+#pragma unroll
+    for (int b = 0; b < B; b++)
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            const float x = t[b][e] * cap_inv, y = x * x;
+            float p = __builtin_fmaf(y, 21844.0f / 6081075, -1382.0f / 155925);
+            p = __builtin_fmaf(y, p, 62.0f / 2835);
+            p = __builtin_fmaf(y, p, -17.0f / 315);
+            p = __builtin_fmaf(y, p, 2.0f / 15);
+            p = __builtin_fmaf(y, p, -1.0f / 3);
+            float capped = __builtin_fmaf(t[b][e] * y, p, t[b][e]);
+            if (beyond) {
+                const float far = cap - 2.0f * cap * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fabsf(x) * (2 * LOG2E)));
+                if (fabsf(x) >= 0.5f) capped = __builtin_copysignf(far, x);
+            }
+            t[b][e] = capped;
+        }
+}
+
+// Products q c to scores t in units of the exponent: softmax log2 e t, sigmoid t log2 e + bias log2 e
+template <int SCORE, bool CAP, int B, int E>
+__device__ __forceinline__ void scores_of(float (&u)[B][E], const float (&scale)[B], const AttentionView &a) {
+#pragma unroll
+    for (int b = 0; b < B; b++)
+#pragma unroll
+        for (int e = 0; e < E; e++) u[b][e] *= a.factor * scale[b];
+    if (CAP) cap_scores(u, a.cap, a.cap_inv);
+    if (CAP || SCORE == ENSI_SCORE_SIGMOID)
+#pragma unroll
+        for (int b = 0; b < B; b++)
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                if (CAP) u[b][e] *= LOG2E;
+                if (SCORE == ENSI_SCORE_SIGMOID) u[b][e] += a.bias;
+            }
 }
 
 // Where the rows of a tile (query tokens times the heads that share a key head, token by token) look: from key lo, rounded down to a tile of 32, to key `last`.
@@ -297,10 +331,13 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    u[h][r] = score_of<SCORE, CAP>(qk[h][r], ks[h], a);
-                    if (SCORE == ENSI_SCORE_SIGMOID) u[h][r] = vs[h] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[h][r]));
-                }
+                for (int r = 0; r < 4; r++) u[h][r] = qk[h][r];
+            scores_of<SCORE, CAP>(u, ks, a);
+            if (SCORE == ENSI_SCORE_SIGMOID)
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) u[h][r] = vs[h] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[h][r]));
             if (masked) {
                 const int reach = pos - key0 - 4 * g;
                 const Seen seen(a, reach);
@@ -684,13 +721,14 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
 #pragma unroll
             for (int b = 0; b < 4; b++)
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    float v = qk[b / 2][8 * (b % 2) + e];
-                    // softmax without a cap: the product itself, its factor enters with the exponent
-                    if (CAP || SCORE == ENSI_SCORE_SIGMOID) v = score_of<SCORE, CAP>(v, ks[b], a);
-                    if (SCORE == ENSI_SCORE_SIGMOID) v = vs[b] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v));
-                    u[b][e] = v;
-                }
+                for (int e = 0; e < 8; e++) u[b][e] = qk[b / 2][8 * (b % 2) + e];
+            // softmax without a cap: the product itself, its factor enters with the exponent
+            if (CAP || SCORE == ENSI_SCORE_SIGMOID) scores_of<SCORE, CAP>(u, ks, a);
+            if (SCORE == ENSI_SCORE_SIGMOID)
+#pragma unroll
+                for (int b = 0; b < 4; b++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) u[b][e] = vs[b] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[b][e]));
             if (masked) {
                 const int reach = pos - key0 - 4 * half;
                 const Seen seen(a, reach);
@@ -882,7 +920,8 @@ void launch_clear_attention(ensi_ctx *ctx, const KvView &kv, const ensi_clear_at
     AttentionView v = {kv, a.s, a.q, a.out, a.q_stride, a.out_stride, a.q_heads, a.q_heads / kv.heads, a.window, a.max_length, a.cap, 0, 0, a.bias * LOG2E, 0, 0, ctx->ws_clear};
     const float root = 1.0f / sqrtf((float)kv.dim);
     v.factor = a.cap > 0 ? root : root * LOG2E;
-    v.cap_inv = a.cap > 0 ? 2.0f * LOG2E / a.cap : 0.0f;
+    if (a.cap > 0) v.cap = std::max(a.cap, 0x1p-120f);  // scores below 2^-120 are as good as 0, and 1 / cap stays finite
+    v.cap_inv = a.cap > 0 ? 1.0f / v.cap : 0.0f;
     if (a.type == ENSI_T_BF16) {
         if (a.score == ENSI_SCORE_SOFTMAX) return attention_dim<ENSI_T_BF16, ENSI_SCORE_SOFTMAX>(ctx, v, st);
         return attention_dim<ENSI_T_BF16, ENSI_SCORE_SIGMOID>(ctx, v, st);

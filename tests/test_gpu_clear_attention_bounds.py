@@ -32,8 +32,12 @@ def definition(c, q, i, h, j, cap, window, score, bias):
     seen = (~dark).sum(1, keepdim=True)
     # a score: `dim` products added in 32 bits, each addition a whole step of the sum of sizes at most; five roundings of its own (factor, scale, cap); the exponent's argument has four more at the
     # size of scores, references and lifts in units of log2 e
+    if cap:  # the exponential, 1 + it, its reciprocal and the difference from 1, of half a cap at least: 5.5 of U32 of the cap; or seven terms of a series
+        off = 12 * U32 * raw
+    else:
+        off = 0
     scale = c.scales["v"].nan_to_num(1.0, 1.0, 1.0).clamp(2.0 ** -64, 2.0 ** 120).log2().abs().max()
-    off = 2 * U32 * (c.dim * sizes.amax(1, keepdim=True) + 5 * raw) + 4 * U32 * (1.5 * (t.abs().amax(1, keepdim=True) + abs(bias)) + float(scale) + 70)
+    off = off + 2 * U32 * (c.dim * sizes.amax(1, keepdim=True) + 5 * raw) + 4 * U32 * (1.5 * (t.abs().amax(1, keepdim=True) + abs(bias)) + float(scale) + 70)
     # the running reference moves once a tile of 32 keys at most, six roundings each time; then sums over the row's keys, of weights and of products; functions to two steps
     return p @ v, p @ v.abs(), 2 * off + U32 * (6 * seen / 32 + 2 * seen + 32)
 
@@ -151,4 +155,20 @@ def test_scales_at_either_end(ctx, exponent, news, heads):
     cache = c.wrap(ctx)
     got = ctx.clear_attention(cache, *c.where, q.cuda(), **longest(c))
     check(c, "bf16", got, q, heads=range(0, 4 * heads, 5))
+    cache.free()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("cap", [1e-40, 1e-3, 1.0, 30.0, 1e4, 1e6, 1e8, 3e38])
+@pytest.mark.parametrize("ctxs, news, heads", [([900, 31], [1, 1], 1), ([0], [1700], 16)])
+def test_caps_of_every_size(ctx, kind, score, cap, ctxs, news, heads):
+    """Scores of deviation 2 under caps far below, near and far above them, where the cap leaves them as they are."""
+    c = Cache(ctx, ctxs, news, heads, 64, 16, 41, powers=(0, 1))
+    c.fill_new(powers=(0, 1))
+    q = (torch.randn(c.tokens, 4 * heads, 64, generator=c.g) / 30).to(TYPES[kind])  # values of deviation 60, divided by 8
+    cache = c.wrap(ctx)
+    bias = -6.0 if score == "sigmoid" else 0.0
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), cap=cap, score=score, bias=bias, **longest(c))
+    check(c, kind, got, q, cap, 0, score, bias, heads=range(0, 4 * heads, 7))
     cache.free()
