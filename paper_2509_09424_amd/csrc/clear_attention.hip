@@ -148,6 +148,8 @@ __device__ __forceinline__ RowTile row_tile(const SeqPart &part, int row0, int m
     r.tiles = (r.last + 1 - r.lo + 31) / 32;
     return r;
 }
+// Whether a row of the tile sees a key of the block that begins at `key`: what lies before a window may have been given back, its page and scales are not looked at.
+__device__ __forceinline__ bool sees_block(const RowTile &r, int key, int window) { return key <= r.last && (window <= 0 || key + KV_BLOCK - 1 > r.first - window); }
 
 // The block of 16 keys that holds a key, as a row of the scales; -1: its page is outside the cache.
 __device__ __forceinline__ int block_of(const AttentionView &a, int seq, int head, int key) {
@@ -266,7 +268,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
         float my_k = 1, my_v = 1;
         {
             const int t = batch + 4 * (lane / 2), key = rt.lo + 32 * t + 16 * (lane % 2);
-            if (t < tile1 && key <= rt.last) {
+            if (t < tile1 && sees_block(rt, key, a.window)) {
                 const int block = block_of(a, seq, head, key);
                 if (block >= 0) {
                     my_block = block;
@@ -597,7 +599,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
         const int key = all.lo + 64 * first + 16 * lane;
         my_block = my_good = 0;
         my_k = my_v = 1;
-        if (key <= all.last) {
+        if (sees_block(all, key, a.window)) {
             const int block = block_of(a, seq, head, key);
             if (block >= 0) {
                 my_block = block;

@@ -172,3 +172,33 @@ def test_caps_of_every_size(ctx, kind, score, cap, ctxs, news, heads):
     got = ctx.clear_attention(cache, *c.where, q.cuda(), cap=cap, score=score, bias=bias, **longest(c))
     check(c, kind, got, q, cap, 0, score, bias, heads=range(0, 4 * heads, 7))
     cache.free()
+
+
+@pytest.mark.parametrize("score, cap", [("softmax", 0.0), ("softmax", 9.0), ("sigmoid", 0.0)])
+@pytest.mark.parametrize("ctxs, news, heads, window", [([300], [1], 1, 50), ([301, 64], [1, 1], 2, 17), ([290], [40], 1, 33), ([300], [1500], 16, 77), ([40], [1600], 16, 16), ([1000], [1], 1, 1)])
+def test_pages_before_a_window_that_were_given_back(ctx, score, cap, ctxs, news, heads, window):
+    """Pages that no row of a tile sees: whatever their place in the table and their scales hold, the results are the same, and nothing is reported."""
+    c = Cache(ctx, ctxs, news, heads, 64, 16, 43 + window)
+    c.fill_new()
+    q = (torch.randn(c.tokens, 4 * heads, 64, generator=c.g) / 16).to(torch.bfloat16)
+    bias = -4.0 if score == "sigmoid" else 0.0
+    call = lambda cache, table: ctx.clear_attention(cache, table, *c.where[1:], q.cuda(), cap=cap, window=window, score=score, bias=bias, **longest(c))  # noqa: E731
+    cache = c.wrap(ctx)
+    clean = call(cache, c.where[0])
+    cache.check()
+    check(c, "bf16", clean, q, cap, window, score, bias, heads=range(0, 4 * heads, 7))
+    given_back = [(i, b) for i, n in enumerate(c.ctxs) for b in range(max(0, (n - window + 1) // 16))]
+    assert given_back
+    spare = next(p for p in range(len(c.codes["k"])) if not (c.table == p).any())
+    for what in (-1, 1 << 30, spare):
+        for k_scale, v_scale in ((0.0, 0.0), (math.nan, math.nan), (math.inf, math.inf), (1.0, math.inf), (math.inf, 1.0)) if what == spare else ((1.0, 1.0),):
+            table = c.table.clone()
+            for i, b in given_back:
+                table[i, b] = what
+            cache.free()
+            cache = c.wrap(ctx)
+            c.dev[2][spare], c.dev[3][spare] = k_scale, v_scale
+            got = call(cache, table.cuda())
+            cache.check()
+            assert torch.equal(got, clean), (what, k_scale, v_scale)
+    cache.free()
