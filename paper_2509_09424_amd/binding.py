@@ -109,6 +109,16 @@ def _torch_types():
     return _torch()[2]
 
 
+def _empty(like, shape, kind, elsewhere, at):
+    """A new tensor for a call to write.  elsewhere: the stream that was given, if one was: its memory then comes from that stream's pool, as work of other streams may
+    still be on a block of theirs."""
+    if elsewhere is None or elsewhere == _TORCH[1](at):
+        return like.new_empty(shape, dtype=kind)
+    import torch
+    with torch.cuda.stream(torch.cuda.ExternalStream(elsewhere, device=at) if elsewhere else torch.cuda.default_stream(at)):
+        return like.new_empty(shape, dtype=kind)
+
+
 def _type(name, kind):
     code = _TORCH[2]["codes"].get(kind)
     if code is None:
@@ -546,7 +556,7 @@ class Context:
                                       ctypes.c_void_p(stream)))
 
     # ---- the decoder layer on clear activations.  Arrays are torch tensors on the context's device; `stream` is torch's current one unless
-    # another is given.  Nothing here waits: what only the device can see (lengths, tables) is reported by ClearCache.check.
+    # another is given (as a number), which then owns what the call makes, as in a `with torch.cuda.stream(...)`.  Nothing here waits: what only the device can see (lengths, tables) is reported by ClearCache.check.
     def _on(self, stream):
         device, current_stream, _ = _TORCH or _torch()
         at = device()
@@ -556,15 +566,16 @@ class Context:
         """h = x + residual; p = h gain; codes = round(p 127 / max |p|) with their scale for each row, out = p / sqrt(mean h^2 + eps), sum_out = h.
         x, residual, sum_out, out: [rows][d] with any stride between rows; codes int8 [rows][d], scales float32 [rows].  Without codes and out, the
         former are made.  Returns (codes, scales)."""
+        elsewhere = stream
         at, stream = self._on(stream)
         kind, shape = x.dtype, x.shape
         if len(shape) != 2:
             raise EnsiError("x must be [rows][d]")
         rows, d = shape
         if codes is None and out is None:
-            codes = x.new_empty((rows, d), dtype=_torch_types()["int8"])
+            codes = _empty(x, (rows, d), _TORCH[2]["int8"], elsewhere, at)
         if codes is not None and scales is None:
-            scales = x.new_empty((rows,), dtype=_torch_types()["float32"])
+            scales = _empty(x, (rows,), _TORCH[2]["float32"], elsewhere, at)
         px, sx = _rows("x", x, shape, kind, at)
         pr, sr = (None, 0) if residual is None else _rows("residual", residual, shape, kind, at)
         ps, ss = (None, 0) if sum_out is None else _rows("sum_out", sum_out, shape, kind, at)
@@ -594,13 +605,14 @@ class Context:
     def clear_matmul(self, weights, codes, scales, out=None, dtype=None, stream=None):
         """out[t] = scales[t] (codes[t] W w_scales); codes int8 [rows][d] with any stride between rows, scales float32 [rows], out [rows][m] of a floating type
         (made with `dtype` if not given)."""
+        elsewhere = stream
         at, stream = self._on(stream)
         shape = codes.shape
         if len(shape) != 2 or shape[1] != weights.d:
             raise EnsiError("codes must be [rows][%d]" % weights.d)
         rows = shape[0]
         if out is None:
-            out = codes.new_empty((rows, weights.m), dtype=dtype)
+            out = _empty(codes, (rows, weights.m), dtype, elsewhere, at)
         kind = out.dtype
         pc, sc = _rows("codes", codes, shape, _TORCH[2]["int8"], at)
         po, so = _rows("out", out, (rows, weights.m), kind, at)
@@ -627,6 +639,7 @@ class Context:
         """Rotates q [tokens][heads][dim] into q_out (made if not given) and k by their positions, and stores k and v [tokens][kv heads][dim] in the cache.
         Sequence i has the tokens begin[i] .. begin[i + 1] - 1 behind lengths[i] cached ones; its pages are table[i] (all int32).  cos, sin: float32
         [positions][rot / 2], or None for no rotation.  max_new: the most new tokens of a sequence (default: all of them).  Returns q_out."""
+        elsewhere = stream
         at, stream = self._on(stream)
         tokens, kind = k.shape[0], k.dtype
         shape = (tokens, cache.heads, cache.dim)
@@ -636,7 +649,7 @@ class Context:
         if q is not None:
             heads = q.shape[1] if len(q.shape) == 3 else 0
             if q_out is None:
-                q_out = q.new_empty(q.shape)
+                q_out = _empty(q, q.shape, q.dtype, elsewhere, at)
             pq, sq = _rows("q", q, (tokens, heads, cache.dim), kind, at)
             po, so = _rows("q_out", q_out, (tokens, heads, cache.dim), kind, at)
         rot = positions = pc = ps = 0
@@ -656,12 +669,13 @@ class Context:
         """Causal attention of the new tokens q [tokens][heads][dim] (stored by clear_append before) over their sequences: scores q k / sqrt(dim), capped by
         cap tanh(. / cap), within a window, through a softmax or as sigmoid(. + bias).  lengths as for clear_append (without the new tokens); max_length: the
         longest sequence with its new tokens (default: what the table holds).  Returns out."""
+        elsewhere = stream
         at, stream = self._on(stream)
         shape, kind = q.shape, q.dtype
         if len(shape) != 3 or shape[2] != cache.dim:
             raise EnsiError("q must be [tokens][heads][%d]" % cache.dim)
         if out is None:
-            out = q.new_empty(shape)
+            out = _empty(q, shape, kind, elsewhere, at)
         pq, sq = _rows("q", q, shape, kind, at)
         po, so = _rows("out", out, shape, kind, at)
         s = _seqs(table, begin, lengths, shape[0], max_new, at)
