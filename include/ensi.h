@@ -521,7 +521,8 @@ int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *
 /* Attention of the new tokens, whose keys and values are in the cache already, over their sequences: token at position p sees the positions up to p, with
  * window > 0 the last `window` of them.  Query head h reads key head h / (q_heads / heads).  t = q k / sqrt(dim), with cap > 0 cap tanh(t / cap);
  * weights: ENSI_SCORE_SOFTMAX softmax(t), ENSI_SCORE_SIGMOID 1 / (1 + exp(-(t + bias))), not normalised.  NaN in places that a token does not see
- * has no part in its result, and pages before every window of the call may have been given back (any number in the table).  q, out: [tokens][q_heads][dim] of ENSI_T_BF16 or ENSI_T_F16.  max_length: no sequence is longer, new tokens included
+ * has no part in its result, and pages before every window of the call may have been given back (any number in the table).
+ * A row without a key in the cache (its pages are all outside it) is 0; one whose scores are all -inf has no softmax and is NaN.  q, out: [tokens][q_heads][dim] of ENSI_T_BF16 or ENSI_T_F16.  max_length: no sequence is longer, new tokens included
  * (up to 2^30). */
 #define ENSI_SCORE_SOFTMAX 0
 #define ENSI_SCORE_SIGMOID 1

@@ -157,6 +157,12 @@ __device__ __forceinline__ int block_of(const AttentionView &a, int seq, int hea
     if (page < 0 || page >= a.kv.pages) return -1;
     return (int)(((page * (int64_t)a.kv.heads + head) * a.kv.page + key % a.kv.page) / KV_BLOCK);
 }
+// Whether any key that the row at `pos` sees is in the cache: for rows whose softmax has a sum of 0, a page after the other.
+__device__ __forceinline__ bool sees_any(const AttentionView &a, int seq, int pos) {
+    for (int key = a.window > 0 ? max(0, pos - a.window + 1) : 0; key <= pos; key = (key / a.kv.page + 1) * a.kv.page)
+        if (block_of(a, seq, 0, key) >= 0) return true;
+    return false;
+}
 __device__ __forceinline__ bool is_nan(unsigned char code) { return (code & 0x7f) == 0x7f; }
 // Which of a lane's keys its row sees, without a branch: places from low + 1 to high behind key0.
 struct Seen {
@@ -216,18 +222,19 @@ struct Weights {
     }
 };
 // What turns a row's sums into its outputs, 2^e f: the reference of sigmoid scores, or the softmax's sum l.  Factor and exponent apart, as their product can leave the range.
+// A sum of 0: the row has no score (all of its pages are outside the cache) and gets 0, or none but -inf, which leaves its softmax undefined: NaN.  `any` tells.
 struct Last {
     float f;
     int e;
     __device__ __forceinline__ float operator()(float o) const { return __builtin_ldexpf(o * f, e); }
 };
-template <int SCORE>
-__device__ __forceinline__ Last last_of(float m, float l) {
+template <int SCORE, class ANY>
+__device__ __forceinline__ Last last_of(float m, float l, const ANY &any) {
     if (SCORE == ENSI_SCORE_SIGMOID) {
         const float whole = floorf(m);
         return {__builtin_amdgcn_exp2f(m - whole), (int)whole - WEIGHT_LIFT};
     }
-    if (l == 0) return {0, 0};
+    if (l == 0) return {any() ? __builtin_nanf("") : 0.0f, 0};
     return {1.0f / __builtin_amdgcn_frexp_mantf(l), SUM_LIFT - WEIGHT_LIFT - __builtin_amdgcn_frexp_expf(l)};
 }
 // 2^(from - to) in two equal factors: references may be 184 apart by their scales alone, which sums have to survive: the factors enter one after the other
@@ -464,7 +471,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
     }
     if (wave != 0 || n >= rt.rows) return;
     const bool whole = rt.tiles <= split_tiles;
-    const Last end = last_of<SCORE>(st.m, st.l);
+    const Last end = last_of<SCORE>(st.m, st.l, [&] { return whole && sees_any(a, seq, pos); });
     float *ws = a.ws + (((int64_t)seq * gridDim.x + blockIdx.x) * a.splits + split) * (16 * DIM + 32);
     T *out = (T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM;
     const auto put = [&](int at, auto first, auto count) {  // registers r of tiles first .. first + count - 1, at place `at` of the row
@@ -535,10 +542,10 @@ __global__ __launch_bounds__(256) void k_clear_attention_join(AttentionView a, i
     __syncthreads();
     if (t >= QUADS) return;
     l = sums[0] + sums[1] + sums[2] + sums[3];
-    const Last end = last_of<SCORE>(most, l);
     o = (f32x4){0, 0, 0, 0};
     for (int s = 0; s < SLICES; s++) o += parts[s][t];
     const int row = 16 * tile + n, token = part.first + row / a.group, q_head = head * a.group + row % a.group;
+    const Last end = last_of<SCORE>(most, l, [&] { return sees_any(a, seq, part.ctx + row / a.group); });
     typedef T quad_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     quad_t w;
 #pragma unroll
@@ -834,7 +841,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
     }
     st_l += __shfl_xor(st_l, 32);
     if (row0 + n >= part.count * a.group) return;
-    const Last end = last_of<SCORE>(st_m, st_l);
+    const Last end = last_of<SCORE>(st_m, st_l, [&] { return sees_any(a, seq, pos); });
     T *out = (T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM;
 #pragma unroll
     for (int j = 0; j < TILES; j++)

@@ -7,7 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_clear import CASES, TYPES, U32, Cache, ctx, gen, half_step  # noqa: E402, F401
+from test_gpu_clear import CASES, TYPES, U32, Cache, ctx, e4m3, half_step  # noqa: E402, F401
 
 PAIR = 2.0 ** -16  # weights in two terms of bf16: half a step of one of them, of half a step of the other
 
@@ -201,4 +201,46 @@ def test_pages_before_a_window_that_were_given_back(ctx, score, cap, ctxs, news,
             got = call(cache, table.cuda())
             cache.check()
             assert torch.equal(got, clean), (what, k_scale, v_scale)
+    cache.free()
+
+
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+@pytest.mark.parametrize("ctxs, news, heads", [([0], [1], 1), ([40], [1], 1), ([3000], [1], 1), ([30], [50], 2), ([0], [1700], 16)])
+def test_scores_of_minus_infinity(ctx, cap, ctxs, news, heads):
+    """Scores that overflow: rows with none but -inf have no softmax and are NaN (a cap turns -inf into minus itself, which is a score like any other), -inf beside finite
+    scores is a weight of 0; a row whose pages are all outside the cache stays 0."""
+    c = Cache(ctx, ctxs, news, heads, 64, 16, 51, powers=(0, 1))
+    c.fill_new(powers=(0, 1))
+    big = torch.tensor([256.0]).to(torch.float8_e4m3fn).view(torch.uint8)
+    n = ctxs[0] + news[0]
+    for p in range(n):
+        c.codes["k"][int(c.table[0, p // 16]), :, p % 16] = 0
+        c.codes["k"][int(c.table[0, p // 16]), :, p % 16, 0] = big
+    group = 4
+    q = torch.zeros(c.tokens, group * heads, 64)
+    q[:, 1::group] = torch.randn(c.tokens, heads, 64, generator=c.g) / 16
+    q[:, 0::group, 0], q[:, 2::group, 0] = -3e38, 3e38
+    q = q.to(torch.bfloat16)
+    cache = c.wrap(ctx)
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), cap=cap, **longest(c)).cpu()
+    cache.check()
+    assert got[:, 1::group].isfinite().all() and got[:, 3::group].isfinite().all()
+    if cap:
+        assert got.isfinite().all()
+        check(c, "bf16", got, torch.where(q.abs() > 1e38, 0.0, q), cap)  # equal scores in either
+        cache.free()
+        return
+    assert got[:, 0::group].isnan().all() and got[:, 2::group].isnan().all()
+    if n > 1:  # the first token's key is 0: its score is 0 for every row, all others are -inf
+        c.codes["k"][int(c.table[0, 0]), :, 0, 0] = 0
+        cache.free()
+        cache = c.wrap(ctx)
+        got = ctx.clear_attention(cache, *c.where, q.cuda(), **longest(c)).cpu()
+        first = e4m3(c.codes["v"][int(c.table[0, 0]), :, 0]) * c.scales["v"][int(c.table[0, 0]), :, 0, None]
+        assert torch.equal(got[:, 0::group].float(), first.to(torch.bfloat16).float().expand(c.tokens, heads, 64))
+    table = torch.full_like(c.table, -1)
+    got = ctx.clear_attention(cache, table.cuda(), *c.where[1:], q.cuda(), **longest(c)).cpu()
+    assert (got == 0).all()
+    with pytest.raises(Exception, match="left out"):
+        cache.check()
     cache.free()
