@@ -453,7 +453,7 @@ int ensi_ccmm_av(ensi_ctx *ctx, const ensi_gk *rk, const ensi_gk *gk, const ensi
  *   h = x + residual, rounded to the type (h = x without a residual); p_i = h_i gain_i; most = max |p_i|
  *   codes_i = p_i (127 (1 / most)) rounded to the nearest whole number, ties to even
  *   scale = most / (127 sqrt(mean h^2 + eps)), so that codes_i scale is the normed value;  out_i = p_i / sqrt(mean h^2 + eps)
- * A row of zeros has codes 0 and scale 0.  A row whose p holds an infinity or NaN, or whose sum of squares leaves the range of 32 bits, has
+ * eps >= 0, finite.  A row of zeros has codes 0, scale 0 and out 0, without an eps too.  A row whose p holds an infinity or NaN, or whose sum of squares leaves the range of 32 bits, has
  * codes 0, scale NaN and out NaN.  sum_out receives h (with a residual only); it may be x or residual itself, out may be x.  At least one of
  * out and codes; codes and scales go together, codes [rows][d] and scales [rows] without gaps. */
 typedef struct ensi_clear_norm_args {

@@ -38,7 +38,7 @@ extern "C" int ensi_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args *a, voi
     if (!size) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: unknown type %d", a->type);
     if (a->d < 1 || a->d > 32768 || a->rows < 0 || a->rows > CLEAR_MAX_NORM_ROWS)
         ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear norm: %lld rows (up to %d) of %d elements (1 to 32768)", (long long)a->rows, CLEAR_MAX_NORM_ROWS, a->d);
-    if (!(a->eps >= 0)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: eps must not be negative");
+    if (!(a->eps >= 0) || isinf(a->eps)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: eps must not be negative or infinite");
     if (a->rows == 0) return ENSI_OK;
     if (!a->x || !a->gain) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: x and gain are needed");
     if (!a->out && !a->codes) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: neither codes nor out are wanted");

@@ -91,7 +91,33 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void k_clear_norm(NormVi
         }
     }
     const bool fine = check == 0 && squares < __builtin_inff();
-    const float root = fine ? rsqrtf(squares / (float)d + a.eps) : __builtin_nanf("");
+    float root = fine ? rsqrtf(squares / (float)d + a.eps) : __builtin_nanf(""), lift = 1;
+    if (fine && squares < 0x1p-100f && a.eps < 0x1p-100f) {
+        // Squares below the range of 32 bits, with no eps to hide them: once more, of h taken 2^100 times (the row's threads agree).  p and the root
+        // take half of that each, which keeps both in range.  A row of zeros without an eps is 0.
+        const T *from = sum ? sum : x, *more = sum ? nullptr : r;  // (x or the residual may be where the sum is)
+        squares = 0;
+        for (int i = 0; i < V; i++)
+            for (int j = 0; j < 8; j++) {
+                const int at = (t + i * LANES) * 8 + j;
+                if (at >= d) break;
+                float h = (float)from[at];
+                if (more) h = (float)(T)(h + (float)more[at]);
+                h *= 0x1p100f;
+                squares = __builtin_fmaf(h, h, squares);
+            }
+        for (int k = 1; k < 64; k *= 2) squares += __shfl_xor(squares, k);
+        if constexpr (LANES > 64) {
+            __shared__ float part[LANES / 64];
+            if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = squares;
+            __syncthreads();
+            squares = 0;
+            for (int w = 0; w < LANES / 64; w++) squares += part[w];
+        }
+        lift = 0x1p50f;
+        const float mean = squares / (float)d + a.eps * 0x1p100f * 0x1p100f;
+        root = mean == 0 ? 0.0f : rsqrtf(mean) * lift;
+    }
     if (a.out) {
         T *out = (T *)a.out + row * a.out_stride;
 #pragma unroll
@@ -99,7 +125,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void k_clear_norm(NormVi
             const int at = (t + i * LANES) * 8;
             float o[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) o[j] = p[i][j] * root;
+            for (int j = 0; j < 8; j++) o[j] = p[i][j] * lift * root;
             if (at + 8 <= d)
                 Chunk<TYPE>::store(out + at, o);
             else
@@ -110,8 +136,8 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void k_clear_norm(NormVi
     }
     if (!a.codes) return;
     // 127 / most would leave the range of 32 bits below 2^-121: there both are taken 2^100 times, which changes no code
-    const float lift = most < 0x1p-100f ? 0x1p100f : 1.0f;
-    const float factor = !fine || most == 0 ? 0.0f : 127.0f * (1.0f / (most * lift));
+    const float up = most < 0x1p-100f ? 0x1p100f : 1.0f;
+    const float factor = !fine || most == 0 ? 0.0f : 127.0f * (1.0f / (most * up));
     signed char *codes = a.codes + row * d;
 #pragma unroll
     for (int i = 0; i < V; i++) {
@@ -119,7 +145,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void k_clear_norm(NormVi
         u32 w[2] = {0, 0};
         if (fine) {
 #pragma unroll
-            for (int j = 0; j < 8; j++) w[j / 4] |= ((u32)(int)__builtin_rintf(p[i][j] * lift * factor) & 255) << (8 * (j % 4));
+            for (int j = 0; j < 8; j++) w[j / 4] |= ((u32)(int)__builtin_rintf(p[i][j] * up * factor) & 255) << (8 * (j % 4));
         }
         if (at + 8 <= d) {
             typedef u32 pair __attribute__((ext_vector_type(2), aligned(1)));
@@ -130,7 +156,8 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void k_clear_norm(NormVi
                 if (at + j < d) codes[at + j] = (signed char)(w[j / 4] >> (8 * (j % 4)));
         }
     }
-    if (t == 0) a.scales[row] = root * (most / 127.0f);
+    most *= lift;
+    if (t == 0) a.scales[row] = most < 0x1p-100f ? root * most / 127.0f : root * (most / 127.0f);  // (most / 127 could leave the range of 32 bits)
 }
 
 template <int TYPE, int LANES, int V>
