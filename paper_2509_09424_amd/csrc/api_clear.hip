@@ -48,10 +48,9 @@ extern "C" int ensi_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args *a, voi
         ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear norm: rows overlap (a stride is below %d)", a->d);
     const Span x(a->x, a->rows, a->x_stride, a->d, size), r(a->residual, a->rows, a->residual_stride, a->d, size), s(a->sum_out, a->rows, a->sum_stride, a->d, size),
         o(a->out, a->rows, a->out_stride, a->d, size), c(a->codes, a->rows, a->d, a->d, 1), w(a->scales, a->rows, 1, 1, 4), g(a->gain, 1, a->d, a->d, size);
-    const bool sum_is_input = (a->sum_out == a->x && (a->rows == 1 || a->sum_stride == a->x_stride) && (!r.meets(s) || a->residual == a->x)) ||
-                              (a->sum_out == a->residual && (a->rows == 1 || a->sum_stride == a->residual_stride) && (!x.meets(s) || a->residual == a->x));
-    const bool out_is_input = a->out == a->x && (a->rows == 1 || a->out_stride == a->x_stride) && !r.meets(o);
-    if (((x.meets(s) || r.meets(s)) && !sum_is_input) || ((x.meets(o) || r.meets(o)) && !out_is_input) || o.meets(s) || c.meets(x) || c.meets(r) || c.meets(s) || c.meets(o) || c.meets(g) ||
+    const auto same = [&](const void *p, int64_t p_stride, const void *q, int64_t q_stride) { return p == q && (a->rows == 1 || p_stride == q_stride); };
+    if ((s.meets(x) && !same(a->sum_out, a->sum_stride, a->x, a->x_stride)) || (s.meets(r) && !same(a->sum_out, a->sum_stride, a->residual, a->residual_stride)) ||
+        (o.meets(x) && !same(a->out, a->out_stride, a->x, a->x_stride)) || o.meets(r) || o.meets(s) || c.meets(x) || c.meets(r) || c.meets(s) || c.meets(o) || c.meets(g) ||
         w.meets(x) || w.meets(r) || w.meets(s) || w.meets(o) || w.meets(c) || w.meets(g) || g.meets(s) || g.meets(o))
         ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: an output overlaps another array (sum may be x or the residual, out may be x)");
     if (int rc = current_device(ctx)) return rc;

@@ -23,3 +23,19 @@ mark("bad")
 norm(BADARG, "eps", eps=float("inf"))
 """)
     assert len(launches(calls)) == 2
+
+
+def test_norm_sum_into_an_input_whose_rows_lie_otherwise(tmp_path):
+    """x and the residual begin at one address, their rows lie apart differently: a sum in place of either is read as the other's rows by other workgroups."""
+    calls = run(tmp_path, NORM + """
+x = at(65536)
+norm(x=x, residual=x, residual_stride=64, sum_out=x, sum_stride=64)
+norm(x=x, residual=x, residual_stride=128, x_stride=64, rows=1, sum_out=x, sum_stride=7)
+mark("bad")
+norm(BADARG, "overlaps", x=x, residual=x, residual_stride=128, sum_out=x, sum_stride=64)
+norm(BADARG, "overlaps", x=x, residual=x, residual_stride=64, x_stride=128, sum_out=x, sum_stride=64)
+norm(BADARG, "overlaps", x=x, residual=x, residual_stride=64, x_stride=128, sum_out=x, sum_stride=128)
+norm(BADARG, "overlaps", x=x, residual=x + 128, residual_stride=64, sum_out=x, sum_stride=64)
+norm(BADARG, "overlaps", x=x, residual=x + 128, residual_stride=64, sum_out=x + 128, sum_stride=64)
+""")
+    assert len(launches(calls)) == 2
