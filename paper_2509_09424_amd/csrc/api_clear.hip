@@ -25,11 +25,20 @@ static int clear_workspace(ensi_ctx *ctx) {
 }
 static int type_size(int type) { return type == ENSI_T_F32 ? 4 : type == ENSI_T_BF16 || type == ENSI_T_F16 ? 2 : 0; }
 
-// Rows of `width` elements, `stride` apart, as a range of addresses
+// Rows of `width` elements, `stride` apart, as addresses.  Two arrays of one stride, slices of a wider one, meet where their columns do; of two strides where the ranges do.
 struct Span {
     uintptr_t from, to;
-    Span(const void *p, int64_t rows, int64_t stride, int64_t width, int size) : from((uintptr_t)p), to(p && rows > 0 ? from + (size_t)(((rows - 1) * stride + width) * size) : from) {}
-    bool meets(const Span &o) const { return from < o.to && o.from < to; }
+    size_t step, row;  // in bytes; step 0: one row
+    Span(const void *p, int64_t rows, int64_t stride, int64_t width, int size)
+        : from((uintptr_t)p), to(p && rows > 0 ? from + (size_t)(((rows - 1) * stride + width) * size) : from), step(rows > 1 ? (size_t)stride * size : 0), row((size_t)width * size) {}
+    bool meets(const Span &o) const {
+        if (from >= o.to || o.from >= to) return false;
+        if (step && o.step && step != o.step) return true;
+        const size_t both = step ? step : o.step;
+        if (!both) return true;
+        const size_t apart = o.from >= from ? (o.from - from) % both : (both - (from - o.from) % both) % both;  // of o's columns behind this one's
+        return apart < row || both - apart < o.row;
+    }
 };
 
 extern "C" int ensi_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args *a, void *stream) {
@@ -203,8 +212,8 @@ extern "C" int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_ap
     const Span q(a->q, t, a->q_stride, qw, size), o(a->q_out, t, a->q_out_stride, qw, size), k(a->k, t, a->k_stride, kw, size), v(a->v, t, a->v_stride, kw, size);
     const bool same = a->q == a->q_out && (t == 1 || a->q_stride == a->q_out_stride);
     if ((o.meets(q) && !same)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: q_out overlaps q without being it");
-    // q, k and v may be slices of one array with gaps between the rows of each: their ranges meet, their rows do not.  The rotated queries go to q's place or apart.
-    if (!same && (o.meets(k) || o.meets(v))) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: q_out overlaps k or v");
+    // (slices of one array with gaps between the rows of each: their ranges meet, their rows do not)
+    if (o.meets(k) || o.meets(v)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: q_out overlaps k or v");
     if (int rc = current_device(ctx)) return rc;
     launch_clear_append(ctx, c, *a, (hipStream_t)stream);
     ENSI_HIP(ctx, hipGetLastError());

@@ -39,3 +39,69 @@ norm(BADARG, "overlaps", x=x, residual=x + 128, residual_stride=64, sum_out=x, s
 norm(BADARG, "overlaps", x=x, residual=x + 128, residual_stride=64, sum_out=x + 128, sum_stride=64)
 """)
     assert len(launches(calls)) == 2
+
+
+SEQS = PROGRAM + CACHE + """
+rc, kv = wrap()
+assert rc == 0
+def seqs(over):
+    s = dict(begin=at(64), lengths=at(64), table=at(4096), table_stride=8, tokens=6, seqs=3, table_width=8, max_new=4)
+    s.update({k: over.pop(k) for k in list(over) if k in s})
+    return list(s.values()) + [0]
+def check(rc, code, text):
+    if code is None:
+        assert rc == 0, lib.ensi_last_error(ctx.h)
+    else:
+        refused(rc, code, text)
+def append(code=None, text="", **over):
+    s = seqs(over)
+    a = dict(q=at(1 << 16), k=at(1 << 16), v=at(1 << 16), q_out=at(1 << 16), cos=at(1 << 16), sin=at(1 << 16), q_stride=256, q_out_stride=256, k_stride=128, v_stride=128,
+             q_heads=4, rot=64, positions=100, pairs=0, type=1)
+    a.update(over)
+    check(lib.ensi_clear_append(ctx.h, kv, binding._APPEND.pack(*s, *a.values(), 0), st), code, text)
+def attention(code=None, text="", **over):
+    s = seqs(over)
+    a = dict(q=at(1 << 16), out=at(1 << 16), q_stride=256, out_stride=256, q_heads=4, type=1, score=0, window=0, max_length=200, cap=0.0, bias=0.0)
+    a.update(over)
+    check(lib.ensi_clear_attention(ctx.h, kv, binding._ATTENTION.pack(*s, *a.values(), 0), st), code, text)
+a = at(1 << 16)
+"""
+
+
+def test_append_rotates_in_place_beside_keys_and_values_only(tmp_path):
+    """Queries of 256 elements, keys and values of 128, of two bytes: slices of one array whose columns meet would be rotated while they are read as keys."""
+    calls = run(tmp_path, SEQS + """
+wide = dict(q_stride=512, q_out_stride=512, k_stride=512, v_stride=512)
+append(q=a, q_out=a, k=a + 512, v=a + 768, **wide)
+append(q=a + 512, q_out=a + 512, k=a, v=a + 256, **wide)
+append(q=a + 256, q_out=a + 256, k=a, v=a + 768, **wide)
+append(q=a, q_out=at(1 << 16), k=a, v=a + 256, q_stride=512, k_stride=512, v_stride=512)     # (queries that are read only)
+append(q=a, q_out=a + 512, k=a + 1024, v=a + 1280, q_stride=1024, q_out_stride=1024, k_stride=1024, v_stride=1024)  # rotated queries beside the others
+append(q=a, q_out=a, k=a + 512, v=a + 768, tokens=1, q_stride=0, q_out_stride=0, k_stride=0, v_stride=0)
+mark("bad")
+append(BADARG, "k or v", q=a, q_out=a, k=a, v=a + 768, **wide)
+append(BADARG, "k or v", q=a, q_out=a, k=a + 510, v=a + 768, **wide)
+append(BADARG, "k or v", q=a, q_out=a, k=a + 512, v=a + 256, **wide)
+append(BADARG, "k or v", q=a + 512, q_out=a + 512, k=a + 768 + 512, v=a, q_stride=384, q_out_stride=384, k_stride=384, v_stride=384)  # wraps round into the next token's queries
+append(BADARG, "k or v", q=a, q_out=a, k=a + 512, v=a + 768, q_stride=512, q_out_stride=512, k_stride=256, v_stride=512)
+append(BADARG, "k or v", q=a, q_out=a, k=a + 510, v=a + 768, tokens=1)
+append(BADARG, "overlaps q", q=a, q_out=a + 510, k=a + 1024, v=a + 1280, q_stride=1024, q_out_stride=1024, k_stride=1024, v_stride=1024)
+""")
+    assert len(launches(calls)) == 6
+
+
+def test_slices_of_one_array_are_apart(tmp_path):
+    """Outputs beside their inputs in rows of one array."""
+    calls = run(tmp_path, SEQS + NORM[len(PROGRAM):] + """
+attention(q=a, out=a + 512, q_stride=512, out_stride=512)
+attention(q=a + 512, out=a, q_stride=512, out_stride=512)
+norm(x=a, x_stride=128, out=a + 128, out_stride=128)
+norm(x=a, x_stride=256, residual=a + 128, residual_stride=256, sum_out=a + 256, sum_stride=256, out=a + 384, out_stride=256)
+mark("bad")
+attention(BADARG, "overlaps", q=a, out=a + 510, q_stride=512, out_stride=512)
+attention(BADARG, "overlaps", q=a + 512, out=a + 2, q_stride=512, out_stride=512)
+attention(BADARG, "overlaps", q=a, out=a + 512, q_stride=512, out_stride=768)
+norm(BADARG, "overlaps", x=a, x_stride=128, out=a + 126, out_stride=128)
+norm(BADARG, "overlaps", x=a, x_stride=256, residual=a + 128, residual_stride=256, sum_out=a + 256, sum_stride=256, out=a + 382, out_stride=256)
+""")
+    assert len(launches(calls)) == 4
