@@ -41,6 +41,15 @@ struct Span {
     }
 };
 
+// The arrays of a cache
+struct CacheSpans {
+    Span part[4];
+    static int64_t blocks(const KvView &c) { return (int64_t)c.pages * c.heads * (c.page / KV_BLOCK); }
+    explicit CacheSpans(const KvView &c)
+        : part{Span(c.k, 1, 0, blocks(c) * KV_BLOCK * c.dim, 1), Span(c.v, 1, 0, blocks(c) * KV_BLOCK * c.dim, 1), Span(c.ks, 1, 0, blocks(c), 4), Span(c.vs, 1, 0, blocks(c), 4)} {}
+    bool meets(const Span &o) const { return part[0].meets(o) || part[1].meets(o) || part[2].meets(o) || part[3].meets(o); }
+};
+
 extern "C" int ensi_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args *a, void *stream) {
     if (!ctx || !a) return ENSI_E_BADARG;
     const int size = type_size(a->type);
@@ -146,17 +155,17 @@ extern "C" int ensi_clear_cache_wrap(ensi_ctx *ctx, void *k, void *v, float *k_s
         (int64_t)pages * ((int64_t)heads * page / KV_BLOCK) > INT32_MAX)
         ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear cache: %d pages of %d heads and %d tokens (pages of whole blocks of 16, fewer than 2^31 of these)", pages, heads, page);
     if (((uintptr_t)k | (uintptr_t)v) & 15 || ((uintptr_t)k_scale | (uintptr_t)v_scale) & 3) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear cache: arrays are not aligned");
-    const int64_t codes = (int64_t)pages * heads * page * dim, blocks = (int64_t)pages * heads * (page / KV_BLOCK);
-    const Span a[4] = {Span(k, 1, codes, codes, 1), Span(v, 1, codes, codes, 1), Span(k_scale, 1, blocks, blocks, 4), Span(v_scale, 1, blocks, blocks, 4)};
+    const KvView view = {(unsigned char *)k, (unsigned char *)v, k_scale, v_scale, pages, heads, page, dim, nullptr};
+    const CacheSpans a(view);
     for (int i = 0; i < 4; i++)
         for (int j = 0; j < i; j++)
-            if (a[i].meets(a[j])) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear cache: its arrays overlap");
+            if (a.part[i].meets(a.part[j])) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear cache: its arrays overlap");
     if (int rc = current_device(ctx)) return rc;
     if (int rc = clear_workspace(ctx)) return rc;
     ensi_kv *kv = new (std::nothrow) ensi_kv();
     if (!kv) ENSI_FAIL(ctx, ENSI_E_NOMEM, "no host memory");
     kv->ctx = ctx;
-    kv->view = {(unsigned char *)k, (unsigned char *)v, k_scale, v_scale, pages, heads, page, dim, nullptr};
+    kv->view = view;
     const int zero = 0;
     hipError_t e = ctx->pool->alloc((void **)&kv->view.status, sizeof(int));
     if (e == hipSuccess) e = hipMemcpy(kv->view.status, &zero, sizeof zero, hipMemcpyHostToDevice);
@@ -214,6 +223,8 @@ extern "C" int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_ap
     if ((o.meets(q) && !same)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: q_out overlaps q without being it");
     // (slices of one array with gaps between the rows of each: their ranges meet, their rows do not)
     if (o.meets(k) || o.meets(v)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: q_out overlaps k or v");
+    const CacheSpans cache(c);
+    if (cache.meets(q) || cache.meets(o) || cache.meets(k) || cache.meets(v)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: q, k, v or q_out overlaps the cache");
     if (int rc = current_device(ctx)) return rc;
     launch_clear_append(ctx, c, *a, (hipStream_t)stream);
     ENSI_HIP(ctx, hipGetLastError());
@@ -235,6 +246,7 @@ extern "C" int ensi_clear_attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear
     if (t > 1 && (a->q_stride < w || a->out_stride < w)) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear attention: tokens overlap");
     const Span q(a->q, t, a->q_stride, w, 2), o(a->out, t, a->out_stride, w, 2);
     if (q.meets(o)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: out overlaps q");
+    if (CacheSpans(c).meets(o)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: out overlaps the cache");
     if ((int64_t)a->s.max_new * a->q_heads > INT32_MAX / 16) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear attention: %d new tokens of %d heads are too many", a->s.max_new, a->q_heads);
     if (int rc = current_device(ctx)) return rc;
     launch_clear_attention(ctx, c, *a, (hipStream_t)stream);

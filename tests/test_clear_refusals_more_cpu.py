@@ -105,3 +105,26 @@ norm(BADARG, "overlaps", x=a, x_stride=128, out=a + 126, out_stride=128)
 norm(BADARG, "overlaps", x=a, x_stride=256, residual=a + 128, residual_stride=256, sum_out=a + 256, sum_stride=256, out=a + 382, out_stride=256)
 """)
     assert len(launches(calls)) == 4
+
+
+def test_arrays_of_a_call_are_not_the_cache_s(tmp_path):
+    """Nothing that a call writes, and nothing that an append reads, may lie in the cache that it writes or reads."""
+    calls = run(tmp_path, SEQS + """
+lib.ensi_clear_cache_free(kv)
+parts = [at(1 << 20) for _ in range(4)]  # 10 pages of 2 heads, 32 tokens, 64 places: codes 40960 bytes, scales 160
+rc, kv = wrap(k=parts[0], v=parts[1], ks=parts[2], vs=parts[3])
+assert rc == 0
+append(q=a, q_out=a)
+attention(q=parts[0])   # (both only read)
+mark("bad")
+for p, size in zip(parts, (40960, 40960, 160, 160)):
+    for at_ in (p, p + size - 2):
+        append(BADARG, "cache", q=a, q_out=at_)
+        append(BADARG, "cache", k=at_)
+        append(BADARG, "cache", v=at_)
+        append(BADARG, "cache", q=at_)
+        attention(BADARG, "cache", out=at_)
+    attention(out=p + size)
+""")
+    got = names(calls)
+    assert sum("append" in n for n in got) == 1 and len([n for n in got if "attention" in n and "join" not in n]) == 5
