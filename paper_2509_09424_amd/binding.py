@@ -131,11 +131,20 @@ def _refuse(name, t, shape, kind, at):
         name, kind, tuple(shape), at, t.dtype, tuple(t.shape), t.stride(), t.get_device()))
 
 
+def _no_gradient(name):
+    """For a tensor that requires a gradient: nothing here is differentiated, and a result without a history would hide that."""
+    import torch
+    if torch.is_grad_enabled():
+        raise EnsiError("%s requires a gradient, which the clear calls do not have: detach it, or call within torch.no_grad()" % name)
+
+
 def _rows(name, t, shape, kind, at):
     """Address and stride between rows of a tensor whose rows have no gaps."""
     strides = t.stride()
     if t.shape != shape or t.dtype is not kind or t.get_device() != at or strides[-1] != 1 and shape[-1] > 1 or len(strides) == 3 and strides[1] != shape[2] and shape[1] > 1:
         _refuse(name, t, shape, kind, at)
+    if t.requires_grad:
+        _no_gradient(name)
     return t.data_ptr(), strides[0]
 
 
@@ -143,6 +152,8 @@ def _whole(name, t, shape, kind, at):
     """Address of a tensor without gaps."""
     if t.shape != shape or t.dtype is not kind or t.get_device() != at or not t.is_contiguous():
         _refuse(name, t, shape, kind, at)
+    if t.requires_grad:
+        _no_gradient(name)
     return t.data_ptr()
 
 

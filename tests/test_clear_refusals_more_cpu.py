@@ -128,3 +128,44 @@ for p, size in zip(parts, (40960, 40960, 160, 160)):
 """)
     got = names(calls)
     assert sum("append" in n for n in got) == 1 and len([n for n in got if "attention" in n and "join" not in n]) == 5
+
+
+BINDING = PROGRAM + """
+import torch
+binding._TORCH = (lambda: -1, lambda at: 0, {**{n: getattr(torch, n) for n in ("int8", "uint8", "int32", "float32", "bfloat16", "float16", "float8_e4m3fn")},
+                  "codes": {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}})   # tensors of the host stand for the device's
+def no(f, text=""):
+    try:
+        f()
+    except binding.EnsiError as e:
+        assert text in str(e), e
+        return
+    raise AssertionError("not refused")
+x, gain = torch.zeros(4, 64), torch.ones(64)
+w = ctx.clear_weights_prepare(np.zeros((64, 16), dtype=np.int8), np.ones(16))
+codes, scales = torch.zeros(3, 64, dtype=torch.int8), torch.ones(3)
+k, s = torch.zeros(5, 2, 32, 64, dtype=torch.uint8), torch.zeros(5, 2, 2)
+cache = ctx.clear_cache(k, k.clone(), s, s.clone())
+where = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+kk, cos, q = torch.zeros(4, 2, 64), torch.zeros(9, 32), torch.zeros(4, 6, 64)
+"""
+
+
+def test_tensors_that_require_a_gradient(tmp_path):
+    """They are refused while gradients are recorded; without that they are tensors like others."""
+    run(tmp_path, BINDING + """
+leaf = lambda t: t.clone().requires_grad_()
+bad = [lambda: ctx.clear_norm(leaf(x), gain), lambda: ctx.clear_norm(x, leaf(gain)), lambda: ctx.clear_norm(x, gain, residual=leaf(x)), lambda: ctx.clear_norm(leaf(x) * 2, gain),
+       lambda: ctx.clear_matmul(w, codes, leaf(scales), dtype=torch.bfloat16),
+       lambda: ctx.clear_append(cache, *where, leaf(kk), kk, cos, cos), lambda: ctx.clear_append(cache, *where, kk, leaf(kk), cos, cos), lambda: ctx.clear_append(cache, *where, kk, kk, cos, leaf(cos)),
+       lambda: ctx.clear_append(cache, *where, kk, kk, cos, cos, q=leaf(q)), lambda: ctx.clear_attention(cache, *where, leaf(q.half())),
+       lambda: ctx.clear_cache(k, k.clone(), leaf(s), s.clone())]
+for f in bad:
+    no(f, "requires a gradient")
+with torch.no_grad():
+    for f in bad:
+        f()
+with torch.inference_mode():
+    for f in bad:
+        f()
+""")
