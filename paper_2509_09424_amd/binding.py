@@ -656,6 +656,8 @@ class Context:
         shape = (tokens, cache.heads, cache.dim)
         pk, sk = _rows("k", k, shape, kind, at)
         pv, sv = _rows("v", v, shape, kind, at)
+        if q is None and q_out is not None or (cos is None) != (sin is None):
+            raise EnsiError("q_out goes with q, cos with sin")
         pq = po = sq = so = heads = 0
         if q is not None:
             heads = q.shape[1] if len(q.shape) == 3 else 0

@@ -169,3 +169,14 @@ with torch.inference_mode():
     for f in bad:
         f()
 """)
+
+
+def test_halves_of_pairs_of_arguments(tmp_path):
+    """A place for rotated queries without queries, and one of cosines and sines, were passed over."""
+    run(tmp_path, BINDING + """
+no(lambda: ctx.clear_append(cache, *where, kk, kk, cos, cos, q_out=q), "q_out goes with q")
+no(lambda: ctx.clear_append(cache, *where, kk, kk, None, cos), "cos with sin")
+no(lambda: ctx.clear_append(cache, *where, kk, kk, cos, None), "cos with sin")
+ctx.clear_append(cache, *where, kk, kk, None, None)
+ctx.clear_append(cache, *where, kk, kk, cos, cos, q=q, q_out=q.clone())
+""")
