@@ -119,6 +119,20 @@ def _empty(like, shape, kind, elsewhere, at):
         return like.new_empty(shape, dtype=kind)
 
 
+def _pack(fields, *values):
+    try:
+        return fields.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise EnsiError("an argument is not a number of its type's range: %s" % e) from None
+
+
+def _code(name, codes, value):
+    code = codes.get(value)
+    if code is None:
+        raise EnsiError("%s must be one of %s, not %r" % (name, ", ".join(codes), value))
+    return code
+
+
 def _type(name, kind):
     code = _TORCH[2]["codes"].get(kind)
     if code is None:
@@ -159,9 +173,9 @@ def _whole(name, t, shape, kind, at):
 
 def _seqs(table, begin, lengths, tokens, max_new, at):
     """The fields of ensi_clear_seqs."""
+    if len(table.shape) != 2 or not lengths.shape:
+        raise EnsiError("table must be [seqs][pages], lengths [seqs]")
     seqs = lengths.shape[0]
-    if len(table.shape) != 2:
-        raise EnsiError("table must be [seqs][pages]")
     kind, width = _TORCH[2]["int32"], table.shape[1]
     pt, st = _rows("table", table, (seqs, width), kind, at)
     return (_whole("begin", begin, (seqs + 1,), kind, at), _whole("lengths", lengths, (seqs,), kind, at), pt, st, tokens, seqs, width,
@@ -591,7 +605,7 @@ class Context:
         pr, sr = (None, 0) if residual is None else _rows("residual", residual, shape, kind, at)
         ps, ss = (None, 0) if sum_out is None else _rows("sum_out", sum_out, shape, kind, at)
         po, so = (None, 0) if out is None else _rows("out", out, shape, kind, at)
-        args = _NORM.pack(px, pr or 0, _whole("gain", gain, (d,), kind, at), ps or 0, po or 0,
+        args = _pack(_NORM, px, pr or 0, _whole("gain", gain, (d,), kind, at), ps or 0, po or 0,
                           0 if codes is None else _whole("codes", codes, shape, _TORCH[2]["int8"], at),
                           0 if scales is None else _whole("scales", scales, (rows,), _TORCH[2]["float32"], at), rows, sx, sr, ss, so, d, _type("x", kind), eps, 0)
         rc = self.lib.ensi_clear_norm(self.h, args, stream)
@@ -652,6 +666,8 @@ class Context:
         [positions][rot / 2], or None for no rotation.  max_new: the most new tokens of a sequence (default: all of them).  Returns q_out."""
         elsewhere = stream
         at, stream = self._on(stream)
+        if len(k.shape) != 3:
+            raise EnsiError("k must be [tokens][heads][dim]")
         tokens, kind = k.shape[0], k.dtype
         shape = (tokens, cache.heads, cache.dim)
         pk, sk = _rows("k", k, shape, kind, at)
@@ -672,7 +688,7 @@ class Context:
             positions, rot = cos.shape[0], 2 * cos.shape[1]
             f32 = _TORCH[2]["float32"]
             pc, ps = _whole("cos", cos, cos.shape, f32, at), _whole("sin", sin, cos.shape, f32, at)
-        args = _APPEND.pack(*_seqs(table, begin, lengths, tokens, max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), _PAIRS[pairs], _type("k", kind), 0)
+        args = _pack(_APPEND, *_seqs(table, begin, lengths, tokens, max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), _code("pairs", _PAIRS, pairs), _type("k", kind), 0)
         rc = self.lib.ensi_clear_append(self.h, cache.h, args, stream)
         if rc:
             self._check(rc)
@@ -694,7 +710,7 @@ class Context:
         s = _seqs(table, begin, lengths, shape[0], max_new, at)
         if max_length is None:
             max_length = min(table.shape[1] * cache.page, 1 << 30)
-        args = _ATTENTION.pack(*s, pq, po, sq, so, shape[1], _type("q", kind), _SCORES[score], window, max_length, cap, bias, 0)
+        args = _pack(_ATTENTION, *s, pq, po, sq, so, shape[1], _type("q", kind), _code("score", _SCORES, score), window, max_length, cap, bias, 0)
         rc = self.lib.ensi_clear_attention(self.h, cache.h, args, stream)
         if rc:
             self._check(rc)

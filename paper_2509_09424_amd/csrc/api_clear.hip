@@ -51,7 +51,8 @@ struct CacheSpans {
 };
 
 extern "C" int ensi_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args *a, void *stream) {
-    if (!ctx || !a) return ENSI_E_BADARG;
+    if (!ctx) return ENSI_E_BADARG;
+    if (!a) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: no arguments");
     const int size = type_size(a->type);
     if (!size) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear norm: unknown type %d", a->type);
     if (a->d < 1 || a->d > 32768 || a->rows < 0 || a->rows > CLEAR_MAX_NORM_ROWS)
@@ -78,7 +79,8 @@ extern "C" int ensi_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args *a, voi
 }
 
 extern "C" int ensi_clear_weights_prepare(ensi_ctx *ctx, const int8_t *W, const float *w_scales, int32_t d, int32_t m, int32_t group, ensi_cw **out) {
-    if (!ctx || !W || !w_scales || !out) return ENSI_E_BADARG;
+    if (!ctx) return ENSI_E_BADARG;
+    if (!W || !w_scales || !out) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear weights: a null argument");
     *out = nullptr;
     if (d < 1 || d > 131072 || m < 1 || m > (1 << 24)) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear weights: %d x %d (up to 131072 x 2^24)", d, m);
     if (group < 0 || group % 64) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear weights: groups of %d rows (a multiple of 64, or 0)", group);
@@ -132,7 +134,8 @@ extern "C" void ensi_clear_weights_free(ensi_cw *cw) {
 
 extern "C" int ensi_clear_matmul(ensi_ctx *ctx, const ensi_cw *cw, const int8_t *codes, int64_t codes_stride, const float *scales, void *out, int64_t out_stride, int64_t rows, int32_t type,
                                  void *stream) {
-    if (!ctx || !cw || cw->ctx != ctx) return ENSI_E_BADARG;
+    if (!ctx) return ENSI_E_BADARG;
+    if (!cw || cw->ctx != ctx) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear matmul: no weights, or those of another context");
     const int size = type_size(type);
     if (!size) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear matmul: unknown type %d", type);
     if (rows < 0 || rows > (1 << 20)) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear matmul: %lld rows (up to 2^20)", (long long)rows);
@@ -148,7 +151,8 @@ extern "C" int ensi_clear_matmul(ensi_ctx *ctx, const ensi_cw *cw, const int8_t 
 }
 
 extern "C" int ensi_clear_cache_wrap(ensi_ctx *ctx, void *k, void *v, float *k_scale, float *v_scale, int32_t pages, int32_t heads, int32_t page, int32_t dim, ensi_kv **out) {
-    if (!ctx || !k || !v || !k_scale || !v_scale || !out) return ENSI_E_BADARG;
+    if (!ctx) return ENSI_E_BADARG;
+    if (!k || !v || !k_scale || !v_scale || !out) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear cache: a null argument");
     *out = nullptr;
     if (dim != 64 && dim != 96 && dim != 128 && dim != 192 && dim != 256) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear cache: heads of %d (64, 96, 128, 192 or 256)", dim);
     if (pages < 1 || heads < 1 || heads > CLEAR_MAX_HEADS || page < KV_BLOCK || page % KV_BLOCK || (int64_t)heads * page > INT32_MAX ||
@@ -184,7 +188,8 @@ extern "C" void ensi_clear_cache_free(ensi_kv *kv) {
 }
 
 extern "C" int ensi_clear_cache_status(ensi_ctx *ctx, ensi_kv *kv, int32_t *bits, void *stream) {
-    if (!ctx || !kv || !bits || kv->ctx != ctx) return ENSI_E_BADARG;
+    if (!ctx) return ENSI_E_BADARG;
+    if (!kv || !bits || kv->ctx != ctx) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear cache: no cache, or that of another context");
     if (int rc = current_device(ctx)) return rc;
     int found = 0;
     const int zero = 0;
@@ -205,7 +210,8 @@ static int check_seqs(ensi_ctx *ctx, const char *who, const ensi_clear_seqs &s) 
 }
 
 extern "C" int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *a, void *stream) {
-    if (!ctx || !kv || !a || kv->ctx != ctx) return ENSI_E_BADARG;
+    if (!ctx) return ENSI_E_BADARG;
+    if (!kv || !a || kv->ctx != ctx) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: no cache, or that of another context, or no arguments");
     const KvView &c = kv->view;
     const int size = type_size(a->type);
     if (!size) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: unknown type %d", a->type);
@@ -232,7 +238,8 @@ extern "C" int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_ap
 }
 
 extern "C" int ensi_clear_attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *a, void *stream) {
-    if (!ctx || !kv || !a || kv->ctx != ctx) return ENSI_E_BADARG;
+    if (!ctx) return ENSI_E_BADARG;
+    if (!kv || !a || kv->ctx != ctx) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: no cache, or that of another context, or no arguments");
     const KvView &c = kv->view;
     if (a->type != ENSI_T_BF16 && a->type != ENSI_T_F16) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: type %d (bf16 or f16)", a->type);
     if (a->score != ENSI_SCORE_SOFTMAX && a->score != ENSI_SCORE_SIGMOID) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: unknown score %d", a->score);

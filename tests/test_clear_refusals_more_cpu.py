@@ -180,3 +180,31 @@ no(lambda: ctx.clear_append(cache, *where, kk, kk, cos, None), "cos with sin")
 ctx.clear_append(cache, *where, kk, kk, None, None)
 ctx.clear_append(cache, *where, kk, kk, cos, cos, q=q, q_out=q.clone())
 """)
+
+
+def test_numbers_names_and_handles_are_refused_as_such(tmp_path):
+    """Numbers outside their type's range, unknown names, handles that are freed or another context's: the library's own error, with a message that is about it."""
+    run(tmp_path, BINDING + """
+h = q.half()
+attend = lambda **over: ctx.clear_attention(cache, *where, h, **over)
+no(lambda: attend(score="maximum"), "score")
+no(lambda: ctx.clear_append(cache, *where, kk, kk, cos, cos, pairs="both"), "pairs")
+for over in (dict(window=1 << 31), dict(window=2.5), dict(max_length=1 << 40), dict(max_new=-(1 << 40)), dict(cap=1e39), dict(bias=-1e39)):
+    no(lambda: attend(**over), "range")
+no(lambda: ctx.clear_append(cache, *where, kk, kk, cos, cos, max_new=1 << 33), "range")
+no(lambda: ctx.clear_norm(x, gain, eps=1e39), "range")
+no(lambda: ctx.clear_attention(cache, where[0], where[1], where[2][0], h), "lengths")
+no(lambda: ctx.clear_append(cache, *where, kk[0, 0, 0], kk, cos, cos), "tokens")
+no(lambda: ctx.clear_append(cache, *where, kk[0], kk, cos, cos), "tokens")
+other = binding.Context(12, 36, 3, 37, 1, 1, 30)
+no(lambda: other.clear_attention(cache, *where, h), "another context")
+no(lambda: other.clear_append(cache, *where, kk, kk, cos, cos), "another context")
+no(lambda: other.clear_matmul(w, codes, scales, dtype=torch.float32), "another context")
+no(lambda: ctx.clear_norm(x, gain, eps=-1.0), "eps")  # (an error of another call before)
+cache.free()
+w.free()
+no(lambda: ctx.clear_attention(cache, *where, h), "no cache")
+no(lambda: ctx.clear_append(cache, *where, kk, kk, cos, cos), "no cache")
+no(lambda: ctx.clear_matmul(w, codes, scales, dtype=torch.float32), "no weights")
+no(lambda: cache.check(), "no cache")
+""")
