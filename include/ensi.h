@@ -437,8 +437,8 @@ int ensi_ccmm_av(ensi_ctx *ctx, const ensi_gk *rk, const ensi_gk *gk, const ensi
                  int32_t baby, int32_t g0, const ensi_pt *mask_head, ensi_ct *out, void *stream);
 
 /* ---- the decoder layer on clear activations ------------------------------------------------------------------
- * The same ternary layer for activations that are not encrypted: what a decrypted result is compared with, what scales and
- * levels are chosen by, and the path of requests that need no encryption.  Activations are device arrays of one ENSI_T_* type;
+ * The same ternary layer for activations that are not encrypted: for requests that need no encryption, and the reference of an
+ * encrypted product of the same 8-bit codes.  Activations are device arrays of one ENSI_T_* type;
  * products, sums, norms and softmax statistics are held in 32 bits and rounded once at the end; the weights of the attention enter
  * their product with the values in 16 bits (two terms of bf16: half a step of 2^-16, and the exponents of 32 bits).  Strides are in elements.
  * These calls only enqueue kernels on the stream, allocate nothing and may be captured into a graph.  Calls of one context must
