@@ -442,7 +442,7 @@ int ensi_ccmm_av(ensi_ctx *ctx, const ensi_gk *rk, const ensi_gk *gk, const ensi
  * products, sums, norms and softmax statistics are held in 32 bits and rounded once at the end; the weights of the attention enter
  * their product with the values in 16 bits (two terms of bf16: half a step of 2^-16, and the exponents of 32 bits).  Strides are in elements.
  * These calls only enqueue kernels on the stream, allocate nothing and may be captured into a graph.  Calls of one context must
- * not overlap on different streams (ensi_clear_attention has a workspace).
+ * not overlap on different streams (the attention and products of many rows of unaligned codes have a workspace).
  * What lies on the device (lengths, tables) cannot be checked by a call that does not wait: the kernels check it,
  * leave out what is wrong and note it in the cache's status (ensi_clear_cache_status). */
 #define ENSI_T_F32 0

@@ -156,23 +156,24 @@ __global__ __launch_bounds__(256) void k_clear_matmul_few(MatmulView a) {
     }
 }
 
-// Many rows: the matrix cores decide.  A workgroup of eight waves has 32 TM rows and 256 columns, a wave 16 TM rows and 64 columns.  Codes and weights reach LDS by
+// Many rows: the matrix cores decide.  A workgroup of eight waves has 128 rows and 256 columns, a wave 64 (TM tiles) and 64.  Codes and weights reach LDS by
 // asynchronous copies, by units of 128 places, two units ahead (three buffers); nothing in the loop loads from memory to registers, as the compiler would then
 // wait for every copy under way.  The codes need rows that begin and end on 16 bytes (others are copied first).  Two workgroups share a CU: one multiplies
-// where the other waits at its barrier or stores.  Weights are widened by the wave that multiplies them: 44 vector instructions for 4 TM matrix
+// where the other waits at its barrier or stores.  Weights are widened by the wave that multiplies them: 44 vector instructions for 16 matrix
 // instructions.  A tile of columns is the instruction's rows, so that a lane ends with neighbouring outputs of a row.
 // The 8 chunks of 16 codes of a row are permuted in LDS with half the row's number: 16 rows of a fragment lie on different banks.
 // Workgroups that follow each other on one XCD have the same rows.
 #define MANY_COLS 256
-template <int TM, bool GROUPED>
+#define MANY_ROWS 128
+template <bool GROUPED>
 struct ManyLds {
-    static constexpr int CODES = 32 * TM * 128, WEIGHTS = MANY_COLS * 32, SCALES = GROUPED ? 2 * MANY_COLS * 4 : 0, BUFFER = CODES + WEIGHTS + SCALES;
+    static constexpr int CODES = MANY_ROWS * 128, WEIGHTS = MANY_COLS * 32, SCALES = GROUPED ? 2 * MANY_COLS * 4 : 0, BUFFER = CODES + WEIGHTS + SCALES;
 };
-template <int TYPE, int TM, bool GROUPED>
+template <int TYPE, bool GROUPED>
 __global__ __launch_bounds__(512, GROUPED ? 2 : 4) void k_clear_matmul_many(MatmulView a) {
     typedef typename Elem<TYPE>::type T;
-    typedef ManyLds<TM, GROUPED> L;
-    constexpr int ROWS = 32 * TM, COPIES = TM / 2;  // copies of 8 rows a wave and unit
+    typedef ManyLds<GROUPED> L;
+    constexpr int ROWS = MANY_ROWS, TM = ROWS / 32, COPIES = TM / 2;  // copies of 8 rows a wave and unit
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, g = lane / 16;
     const int row_tiles = (a.rows + ROWS - 1) / ROWS, col_tiles = (a.m_tiles + 15) / 16, blocks = row_tiles * col_tiles, share = (blocks + 7) / 8;
@@ -299,7 +300,7 @@ __global__ __launch_bounds__(256) void k_clear_align(const signed char *codes, i
 // workgroups have a CU to themselves, then 1 for 230 (120) of them; the copy of unaligned codes 4 on top.
 static bool matmul_is_many(const MatmulView &v, bool aligned) {
     const double few_us = 3 + (double)v.rows * v.d * v.m / (v.group ? 0.30e9 : 0.43e9);
-    const double blocks = (double)((v.rows + 127) / 128) * ((v.m + MANY_COLS - 1) / MANY_COLS);
+    const double blocks = (double)((v.rows + MANY_ROWS - 1) / MANY_ROWS) * ((v.m + MANY_COLS - 1) / MANY_COLS);
     const double many_us = v.units * (v.group ? std::max(1.6, blocks / 120) : std::max(1.0, blocks / 230)) + (aligned ? 0 : 4);
     return many_us < few_us;
 }
@@ -309,12 +310,12 @@ static void matmul_few(const MatmulView &v, hipStream_t st) {
     if (v.group) hipLaunchKernelGGL((k_clear_matmul_few<TYPE, TILES, true>), grid, block, 0, st, v);
     else hipLaunchKernelGGL((k_clear_matmul_few<TYPE, TILES, false>), grid, block, 0, st, v);
 }
-template <int TYPE, int TM, bool GROUPED>
+template <int TYPE, bool GROUPED>
 static void matmul_many(ensi_ctx *ctx, const MatmulView &v, hipStream_t st) {
-    const int blocks = (int)((int64_t)((v.rows + 32 * TM - 1) / (32 * TM)) * ((v.m + MANY_COLS - 1) / MANY_COLS));
-    const int bytes = 3 * ManyLds<TM, GROUPED>::BUFFER;
-    clear_lds(ctx, (const void *)k_clear_matmul_many<TYPE, TM, GROUPED>, bytes);
-    hipLaunchKernelGGL((k_clear_matmul_many<TYPE, TM, GROUPED>), dim3((u32)((blocks + 7) / 8 * 8)), dim3(512), bytes, st, v);
+    const int blocks = (int)((int64_t)((v.rows + MANY_ROWS - 1) / MANY_ROWS) * ((v.m + MANY_COLS - 1) / MANY_COLS));
+    const int bytes = 3 * ManyLds<GROUPED>::BUFFER;
+    clear_lds(ctx, (const void *)k_clear_matmul_many<TYPE, GROUPED>, bytes);
+    hipLaunchKernelGGL((k_clear_matmul_many<TYPE, GROUPED>), dim3((u32)((blocks + 7) / 8 * 8)), dim3(512), bytes, st, v);
 }
 template <int TYPE>
 static void matmul_type(ensi_ctx *ctx, const MatmulView &v, hipStream_t st) {
@@ -322,8 +323,8 @@ static void matmul_type(ensi_ctx *ctx, const MatmulView &v, hipStream_t st) {
     if (matmul_is_many(v, aligned)) {
         const auto many = [&](const MatmulView &u) {
             ScopedTimer timer(ctx, "k_clear_matmul", st);
-            if (u.group) return matmul_many<TYPE, 4, true>(ctx, u, st);
-            matmul_many<TYPE, 4, false>(ctx, u, st);
+            if (u.group) return matmul_many<TYPE, true>(ctx, u, st);
+            matmul_many<TYPE, false>(ctx, u, st);
         };
         if (aligned) return many(v);
         // slices of the rows that the workspace holds

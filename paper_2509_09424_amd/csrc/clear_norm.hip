@@ -171,7 +171,8 @@ static void norm_type(const NormView &v, hipStream_t st) {
     const int chunks = (v.d + 7) / 8;
     // Few chunks to a thread for few rows, whose latency decides (1 x 2560 with a residual: 2.8 us with 512 threads to a row, 3.2 with 256, 5.0 with 64; 512 rows 5.0, 5.0 and
     // 6.6), a wave to a row without a barrier for many (4096 rows: 17.2, 16.8 and 14.6 us; 2048: 10.8, 10.1 and 10.6).  200 x 8192: 5.4 us with 512, 6.4 with 256;
-    // 1024 x 8191 14.5 with either.
+    // 1024 x 8191 14.5 with either.  5 chunks to a thread from 1025 to 2560 wide (4096 rows of 1040, 1536, 2048 and 2560: 10.8, 11.5, 13.0 and 14.3 us; with 8 17.8, 18.1, 19.5
+    // and 21.0, with 256 threads to a row 12.4, 12.5, 15.2 and 16.1).
     if (chunks <= 64) return norm_go<TYPE, 64, 1>(v, st);
     if (v.rows > 2048 && chunks <= 8 * 64) {
         if (chunks <= 2 * 64) return norm_go<TYPE, 64, 2>(v, st);
