@@ -6,7 +6,7 @@
 // softmax's sum adds up, w = e s' <= 1 the weight of the code c'.  The matrix instruction takes weights as two terms of bf16, the nearest one and the nearest to what
 // is left, 16 bits together with the exponents of 32 (f16 would end 2^-40 below the largest weight at best, and where the largest one's values are 0 the small ones
 // are the result).  Both are held lifted: scales are 2^-64 to 2^120, so the largest e 2^32 is 2^-88 to 2^96 and sums of 2^30 of them stay in range,
-// and w 2^70 leaves 2^-196 of the largest weight and sums of 2^30 products with codes in range.
+// and w 2^69 leaves 2^-195 of the largest weight and sums of 2^30 products with codes in range.
 //   sigmoid scores need no sum; w = sigmoid(t) s' 2^-M with the same reference.
 // A tile of scores is held as [key][query]: a lane has one query, so the statistics of a row are per lane, and the weights leave the score's
 // registers in the order in which the second product reads them; the order of its keys is that of the registers, for the values too.
@@ -198,12 +198,13 @@ struct Rows16 {
             for (int r = 0; r < 4; r++) o[j][r] *= f;
     }
 };
-// 2^32 on the terms e of a softmax's sum, 2^70 on the weights
+// 2^62 on a term e (2^64 at most, so that two add up within range), 2^32 on the softmax's sum, 2^69 on the weights: a value's scale, 2^120 at most, takes the 2^7 between
+#define TERM_LIFT 62
 #define SUM_LIFT 32
-#define WEIGHT_LIFT 70
-// The weight of a term e = 2^(t - M + SUM_LIFT) and its value's scale s': 2^31 and 2^7 keep both factors in range whatever s' is.
-__device__ __forceinline__ float weight_of(float e, float scale) { return e * 0x1p31f * (scale * 0x1p7f); }
-static_assert(WEIGHT_LIFT == SUM_LIFT + 31 + 7, "lifts of weight_of");
+#define WEIGHT_LIFT 69
+__device__ __forceinline__ float add_terms(float sum, float e0, float e1) { return __builtin_fmaf(e0 + e1, 0x1p-30f, sum); }
+__device__ __forceinline__ float scale_of_terms(float scale) { return scale * 0x1p7f; }
+static_assert(SUM_LIFT - TERM_LIFT == -30 && WEIGHT_LIFT - TERM_LIFT == 7, "factors between the lifts");
 // Eight weights in two terms of bf16, set in twos: either term of both in one conversion
 struct Weights {
     union {
@@ -385,9 +386,9 @@ __global__ __launch_bounds__(256) void k_clear_attention_keys(AttentionView a, i
                     if (SCORE == ENSI_SCORE_SIGMOID) {
                         p.set(4 * h + r, u[h][r] * unit * unit, u[h][r + 1] * unit * unit);
                     } else {
-                        const float e0 = __builtin_amdgcn_exp2f(u[h][r] - (base - SUM_LIFT)), e1 = __builtin_amdgcn_exp2f(u[h][r + 1] - (base - SUM_LIFT));
-                        st.l += e0 + e1;
-                        p.set(4 * h + r, weight_of(e0, vs[h]), weight_of(e1, vs[h]));
+                        const float e0 = __builtin_amdgcn_exp2f(u[h][r] - (base - TERM_LIFT)), e1 = __builtin_amdgcn_exp2f(u[h][r + 1] - (base - TERM_LIFT)), scale = scale_of_terms(vs[h]);
+                        st.l = add_terms(st.l, e0, e1);
+                        p.set(4 * h + r, e0 * scale, e1 * scale);
                     }
                 }
             u32 nans = 0;
@@ -556,7 +557,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_join(AttentionView a, i
 // Rows split over waves, keys shared: many rows (prompts).  A workgroup has 128 rows of a key head, 32 to a wave, and walks their keys in tiles of 64.
 // A wave fetches one block of 16 keys and values of a tile (the codes of the next tile are under way while one is computed), widens them to 16 bits and puts them into
 // LDS, values transposed and in the order in which the score's registers hold their keys; two buffers, one barrier a tile.  Matrix instructions (48 a wave and tile at
-// 128 places, a third of them for the weights' second term: 252 us without it, 310 with it for 2048 + 4096 tokens of 20 over 5 heads) and the softmax's vector
+// 128 places, a third of them for the weights' second term: 258 us without it, 317 with it for 2048 + 4096 tokens of 20 over 5 heads) and the softmax's vector
 // instructions (three more a weight for the two terms) decide; LDS reads are 32 KB a wave and tile.
 template <int DIM>
 struct RowsLds {
@@ -597,7 +598,6 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
 #pragma unroll
         for (int r = 0; r < 16; r++) o[j][r] = 0;
     float st_m = -__builtin_inff(), st_l = 0;
-    bool wide = false;  // of a wave: value scales outside 2^-40 .. 2^40 were met
     const int tiles = (all.last + 1 - all.lo + 63) / 64;
     // what 16 tiles need to know of their blocks of 16 keys: lane l has block l % 4 of tile l / 4
     int my_block = 0, my_good = 0;
@@ -780,9 +780,6 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
 #pragma unroll
                 for (int j = 0; j < TILES; j++) vf[b % 2][j] = *(const bf16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 16 * ((2 * b + half) ^ (2 * (j % 2) + n / 16)));
             };
-            // With all value scales so far between 2^-40 and 2^40 the weight 2^(t + log2 s' - M) can be formed at once and divided by s' for the sum, a block at a
-            // time: a weight is lost below 2^-196 of the largest one, which is below 2^-116 of the sum's largest term.
-            wide |= fmaxf(fmaxf(fabsf(lv[0]), fabsf(lv[1])), fmaxf(fabsf(lv[2]), fabsf(lv[3]))) > 40;
             const float unit = __builtin_amdgcn_exp2f(0.5f * (WEIGHT_LIFT - base));  // sigmoid: half of the way to the reference
             Weights p[2];
             const auto weigh = [&](int b) {
@@ -790,22 +787,13 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
                 if (SCORE == ENSI_SCORE_SIGMOID) {
 #pragma unroll
                     for (int e = 0; e < 8; e += 2) to.set(e, u[b][e] * unit * unit, u[b][e + 1] * unit * unit);
-                } else if (!wide) {
-                    const float shift = lv[b] - (base - WEIGHT_LIFT);
-                    float sum = 0;
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], shift)), w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e + 1], factor[b], shift));
-                        sum += w0 + w1;
-                        to.set(e, w0, w1);
-                    }
-                    st_l = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vs[b] * 0x1p38f), st_l);
                 } else {
+                    const float scale = scale_of_terms(vs[b]);
 #pragma unroll
                     for (int e = 0; e < 8; e += 2) {
-                        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], SUM_LIFT - base)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e + 1], factor[b], SUM_LIFT - base));
-                        st_l += e0 + e1;
-                        to.set(e, weight_of(e0, vs[b]), weight_of(e1, vs[b]));
+                        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], TERM_LIFT - base)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e + 1], factor[b], TERM_LIFT - base));
+                        st_l = add_terms(st_l, e0, e1);
+                        to.set(e, e0 * scale, e1 * scale);
                     }
                 }
             };
@@ -855,14 +843,14 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_row
         }
 }
 
-// Whether rows are split over waves and their keys shared, or keys over waves: microseconds of either as measured (bf16, no cap).  Rows: for a tile of 64 keys 1.8 at 64
-// places of a head, 2.05 at 96, 2.35 at 128, 3.05 at 192, 4.2 at 256, while two workgroups of 128 rows find room on a CU (one from 192 on); 500 + 1024 tokens of 20 over 5
-// heads of 128 61, 100 + 2048 85, 2048 + 4096 317.  Keys: 50e6 to 90e6 products of a query, a key and a place in 1: these three 57, 101 and 504; 500 + 512 tokens 27 (rows 41),
-// five prompts of 77 behind up to 1500 on 16 heads of 96 23 (55), 500 + 2000 of these 78 (86), 1000 + 1000 of 16 over 4 heads of 256 92 (137).
+// Whether rows are split over waves and their keys shared, or keys over waves: microseconds of either as measured (bf16, no cap).  Rows: for a tile of 64 keys 1.5 at 64
+// places of a head, 1.8 at 96, 2.1 at 128, 2.75 at 192, 3.85 at 256, while two workgroups of 128 rows find room on a CU (one from 192 on); 500 + 1024 tokens of 20 over 5
+// heads of 128 55, 100 + 2048 78, 2048 + 4096 312.  Keys: 50e6 to 90e6 products of a query, a key and a place in 1: these three 56, 101 and 501; 500 + 512 tokens 27 (rows 38),
+// five prompts of 77 behind up to 1500 on 16 heads of 96 22 (49), 500 + 2000 of these 78 (77), 1000 + 1000 of 16 over 4 heads of 256 92 (126).
 static bool attention_by_rows(const AttentionView &v, int span) {
     const int dim = v.kv.dim;
     const double blocks = (double)v.s.seqs * v.kv.heads * (((int64_t)v.s.max_new * v.group + 127) / 128);
-    const double rows_us = 4 + (span + 63) / 64 * (0.95 + 0.0115 * dim) * std::max(1.0, blocks / (dim <= 128 ? 400 : 256));
+    const double rows_us = 4 + (span + 63) / 64 * (0.72 + 0.0115 * dim) * std::max(1.0, blocks / (dim <= 128 ? 400 : 256));
     const double pairs = (double)v.s.seqs * v.s.max_new * v.q_heads * (v.window > 0 ? span : std::max(span - v.s.max_new / 2, 1));
     const double keys_us = 6 + pairs * dim / 60e6;
     return v.s.max_new > 1 && rows_us < keys_us;
