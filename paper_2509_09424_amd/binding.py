@@ -119,18 +119,12 @@ def _empty(like, shape, kind, elsewhere, at):
         return like.new_empty(shape, dtype=kind)
 
 
-def _pack(fields, *values):
-    try:
-        return fields.pack(*values)
-    except (struct.error, OverflowError) as e:
-        raise EnsiError("an argument is not a number of its type's range: %s" % e) from None
+def _unknown(name, codes, value):
+    raise EnsiError("%s must be one of %s, not %r" % (name, ", ".join(codes), value))
 
 
-def _code(name, codes, value):
-    code = codes.get(value)
-    if code is None:
-        raise EnsiError("%s must be one of %s, not %r" % (name, ", ".join(codes), value))
-    return code
+def _no_number(e):
+    raise EnsiError("an argument is not a number of its type's range: %s" % e) from None
 
 
 def _type(name, kind):
@@ -605,9 +599,12 @@ class Context:
         pr, sr = (None, 0) if residual is None else _rows("residual", residual, shape, kind, at)
         ps, ss = (None, 0) if sum_out is None else _rows("sum_out", sum_out, shape, kind, at)
         po, so = (None, 0) if out is None else _rows("out", out, shape, kind, at)
-        args = _pack(_NORM, px, pr or 0, _whole("gain", gain, (d,), kind, at), ps or 0, po or 0,
-                          0 if codes is None else _whole("codes", codes, shape, _TORCH[2]["int8"], at),
-                          0 if scales is None else _whole("scales", scales, (rows,), _TORCH[2]["float32"], at), rows, sx, sr, ss, so, d, _type("x", kind), eps, 0)
+        try:
+            args = _NORM.pack(px, pr or 0, _whole("gain", gain, (d,), kind, at), ps or 0, po or 0,
+                              0 if codes is None else _whole("codes", codes, shape, _TORCH[2]["int8"], at),
+                              0 if scales is None else _whole("scales", scales, (rows,), _TORCH[2]["float32"], at), rows, sx, sr, ss, so, d, _type("x", kind), eps, 0)
+        except (struct.error, OverflowError) as e:
+            _no_number(e)
         rc = self.lib.ensi_clear_norm(self.h, args, stream)
         if rc:
             self._check(rc)
@@ -672,6 +669,9 @@ class Context:
         shape = (tokens, cache.heads, cache.dim)
         pk, sk = _rows("k", k, shape, kind, at)
         pv, sv = _rows("v", v, shape, kind, at)
+        pair_code = _PAIRS.get(pairs)
+        if pair_code is None:
+            _unknown("pairs", _PAIRS, pairs)
         if q is None and q_out is not None or (cos is None) != (sin is None):
             raise EnsiError("q_out goes with q, cos with sin")
         pq = po = sq = so = heads = 0
@@ -688,7 +688,10 @@ class Context:
             positions, rot = cos.shape[0], 2 * cos.shape[1]
             f32 = _TORCH[2]["float32"]
             pc, ps = _whole("cos", cos, cos.shape, f32, at), _whole("sin", sin, cos.shape, f32, at)
-        args = _pack(_APPEND, *_seqs(table, begin, lengths, tokens, max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), _code("pairs", _PAIRS, pairs), _type("k", kind), 0)
+        try:
+            args = _APPEND.pack(*_seqs(table, begin, lengths, tokens, max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), pair_code, _type("k", kind), 0)
+        except (struct.error, OverflowError) as e:
+            _no_number(e)
         rc = self.lib.ensi_clear_append(self.h, cache.h, args, stream)
         if rc:
             self._check(rc)
@@ -701,6 +704,9 @@ class Context:
         elsewhere = stream
         at, stream = self._on(stream)
         shape, kind = q.shape, q.dtype
+        score_code = _SCORES.get(score)
+        if score_code is None:
+            _unknown("score", _SCORES, score)
         if len(shape) != 3 or shape[2] != cache.dim:
             raise EnsiError("q must be [tokens][heads][%d]" % cache.dim)
         if out is None:
@@ -710,7 +716,10 @@ class Context:
         s = _seqs(table, begin, lengths, shape[0], max_new, at)
         if max_length is None:
             max_length = min(table.shape[1] * cache.page, 1 << 30)
-        args = _pack(_ATTENTION, *s, pq, po, sq, so, shape[1], _type("q", kind), _code("score", _SCORES, score), window, max_length, cap, bias, 0)
+        try:
+            args = _ATTENTION.pack(*s, pq, po, sq, so, shape[1], _type("q", kind), score_code, window, max_length, cap, bias, 0)
+        except (struct.error, OverflowError) as e:
+            _no_number(e)
         rc = self.lib.ensi_clear_attention(self.h, cache.h, args, stream)
         if rc:
             self._check(rc)
