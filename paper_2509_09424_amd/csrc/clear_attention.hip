@@ -877,9 +877,9 @@ static void attention_go(ensi_ctx *ctx, AttentionView v, hipStream_t st) {
     v.row_tiles = (int)(((int64_t)v.s.max_new * v.group + 15) / 16);
     const int64_t base = (int64_t)v.s.seqs * heads * v.row_tiles;
     const int tiles = (span + 31) / 32;
-    // Parts of a row's keys.  A decoding step: 8 tiles for a wave, which evens out sequences of different lengths (48 sequences of up to 8192 tokens 66 us, in one part 91).
-    // More where the CUs would stand idle, two workgroups for each of them (one sequence of 32768 tokens: 18.4 us with 102 parts, 19.7 with 128 or 38), unless a wave has no
-    // more than 4 tiles: joining the parts costs 5 us for few rows and 10 for the thousands of a prompt (5 prompts of 77 tokens: 21 us in one part, 27 in two).
+    // Parts of a row's keys.  A decoding step: 8 tiles for a wave, which evens out sequences of different lengths (48 sequences of up to 8192 tokens 66.5 us, in one part 96).
+    // More where the CUs would stand idle, two workgroups for each of them (one sequence of 32768 tokens: 18.7 us with 102 parts, 19.6 with 128 or 38), unless a wave has no
+    // more than 4 tiles: joining the parts costs 5 us for few rows and 10 for the thousands of a prompt (5 prompts of 77 tokens: 17.4 us in one part, 23.9 in two).
     const bool idle = base < (v.s.max_new > 1 ? 128 : 256) && tiles > 16;
     int splits = max(v.s.max_new > 1 ? 1 : (tiles + 31) / 32, idle ? (int)(512 / base) : 1);
     splits = min(splits, min((tiles + 3) / 4, JOIN_MAX));
