@@ -107,7 +107,7 @@ __device__ __forceinline__ void cap_scores(float (&t)[B][E], float cap, float ca
             p = __builtin_fmaf(y, p, -1.0f / 3);
             float capped = __builtin_fmaf(t[b][e] * y, p, t[b][e]);
             if (beyond) {
-                const float far = cap - 2.0f * cap * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fabsf(x) * (2 * LOG2E)));
+                const float far = cap * __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fabsf(x) * (2 * LOG2E))), 1.0f);
                 if (fabsf(x) >= 0.5f) capped = __builtin_copysignf(far, x);
             }
             t[b][e] = capped;
@@ -917,7 +917,8 @@ void launch_clear_attention(ensi_ctx *ctx, const KvView &kv, const ensi_clear_at
     AttentionView v = {kv, a.s, a.q, a.out, a.q_stride, a.out_stride, a.q_heads, a.q_heads / kv.heads, a.window, a.max_length, a.cap, 0, 0, a.bias * LOG2E, 0, 0, ctx->ws_clear};
     const float root = 1.0f / sqrtf((float)kv.dim);
     v.factor = a.cap > 0 ? root : root * LOG2E;
-    if (a.cap > 0) v.cap = std::max(a.cap, 0x1p-120f);  // scores below 2^-120 are as good as 0, and 1 / cap stays finite
+    // 1 / cap and cap log2 e stay finite: scores below 2^-120 are as good as 0, and of scores that a cap beyond 2^126 reaches only which are equal matters
+    if (a.cap > 0) v.cap = std::min(std::max(a.cap, 0x1p-120f), 0x1p126f);
     v.cap_inv = a.cap > 0 ? 1.0f / v.cap : 0.0f;
     if (a.type == ENSI_T_BF16) {
         if (a.score == ENSI_SCORE_SOFTMAX) return attention_dim<ENSI_T_BF16, ENSI_SCORE_SOFTMAX>(ctx, v, st);

@@ -244,3 +244,20 @@ def test_scores_of_minus_infinity(ctx, cap, ctxs, news, heads):
     with pytest.raises(Exception, match="left out"):
         cache.check()
     cache.free()
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("news, heads", [([1], 1), ([1600], 16)])
+def test_scores_near_the_largest_cap(ctx, sign, news, heads):
+    """Scores of 2e38 under a cap of 3e38: all of a row's are equal, so the softmax is a mean."""
+    c = Cache(ctx, [0], news, heads, 64, 16, 53, powers=(0, 1))
+    c.fill_new(powers=(0, 1))
+    for p in range(news[0]):
+        c.codes["k"][int(c.table[0, p // 16]), :, p % 16] = torch.tensor([8.0] + [0.0] * 63).to(torch.float8_e4m3fn).view(torch.uint8)
+    q = torch.zeros(c.tokens, 4 * heads, 64)
+    q[:, :, 0] = sign * 2e38
+    q = q.to(torch.bfloat16)
+    cache = c.wrap(ctx)
+    got = ctx.clear_attention(cache, *c.where, q.cuda(), cap=3e38, **longest(c))
+    check(c, "bf16", got, torch.zeros_like(q), heads=range(0, 4 * heads, 5))  # equal scores
+    cache.free()
