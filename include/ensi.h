@@ -537,6 +537,73 @@ typedef struct ensi_clear_attention_args {
 } ensi_clear_attention_args;
 int ensi_clear_attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *args, void *stream);
 
+/* Drafted decoding: a step gives a sequence several new tokens, drafts of what may follow, of which the longest path that agrees with what is sampled is kept.
+ * parents: device int32 [tokens], for every new token the index of its parent among the new tokens of its sequence, an earlier one, or -1: no parent among
+ * them.  Up to 64 new tokens a sequence.  A tree that is not one (a parent behind its child, or below -1) is left out and noted as ENSI_KV_BAD_TREE.
+ * The two calls above for a tree: new token t is stored at place lengths[i] + t of its sequence; its position, for the rotation and the window, is
+ * lengths[i] + the number of its ancestors; it sees the lengths[i] tokens before, its ancestors and itself, with window > 0 those at the last `window` positions.  `positions`
+ * of the append and max_length of the attention bound positions and places in turn; of the attention's rows without a key in the cache and with nothing but -inf it holds
+ * what is said above. */
+#define ENSI_KV_BAD_TREE 4 /* parents or a path that do not fit: the sequence was left out */
+int ensi_clear_append_tree(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *args, const int32_t *parents, void *stream);
+int ensi_clear_attention_tree(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *args, const int32_t *parents, void *stream);
+
+/* One token for each row of logits [rows][vocab] of an ENSI_T_* type, rows `stride` apart (up to 2^20 rows of up to 2^24).  w_j = exp((x_j - max x) / temperature).  In the order of falling x,
+ * lower indices first among equal ones: the first top_k tokens (all with top_k <= 0); of these the shortest part from the front whose w add up to top_p of theirs
+ * at least (all with top_p >= 1, one with top_p <= 0); of these the ones with w >= min_p (a min_p above 1 counts as 1).  out: the first of them, by index, at which
+ * the running sum of w exceeds uniform times their sum; uniform is in [0, 1), and counts as the nearest of these elsewhere.  temperature 0: the first of the largest.
+ * -1 where there is no distribution: NaN or +inf among the logits, nothing but -inf, a temperature that is negative, infinite or NaN, NaN in one of the others.
+ * Weights are rounded to whole multiples of 2^-S, S = 50 or what sums of vocab of them leave room for in 62 bits, so that the result does not hang on an order
+ * of summation.  uniform: device float [rows]; the others device arrays [rows], or NULL for the number that follows, for all rows. */
+typedef struct ensi_clear_sample_args {
+    const void *logits;
+    const float *uniform, *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    int32_t *out;
+    int64_t rows, stride;
+    int32_t vocab, type;
+    float all_temperature;
+    int32_t all_top_k;
+    float all_top_p, all_min_p;
+} ensi_clear_sample_args;
+int ensi_clear_sample(ensi_ctx *ctx, const ensi_clear_sample_args *args, void *stream);
+
+/* The drafted tokens that agree with what was sampled.  Of each sequence's new tokens (begin as above, up to max_new <= 64) token 0 is given; from it on, the first child of a
+ * node (the next token where parents is NULL) whose token `drafted` is `sampled` at the node, while there is one.  path: device int32 [seqs][max_new], rows path_stride apart: the
+ * indices on the way, ascending, then -1; count: how many; following: what was sampled at the last one (-1 without new tokens, or if they do not fit). */
+typedef struct ensi_clear_accept_args {
+    const int32_t *begin, *parents, *drafted, *sampled;
+    int32_t *path, *count, *following;
+    int64_t tokens, path_stride;
+    int32_t seqs, max_new;
+} ensi_clear_accept_args;
+int ensi_clear_accept(ensi_ctx *ctx, const ensi_clear_accept_args *args, void *stream);
+
+/* Moves the accepted tokens together, in the caches of any number of layers, which have pages of one size: the new token path[i][j] of sequence i, j < count[i], comes to place lengths[i] + j (lengths
+ * and begin are those of the step).  The scale of a block of 16 that tokens come to is the largest scale that its tokens had, those that stay where they are among
+ * them; codes whose scale was smaller are rounded again.  Codes behind the last accepted token that nothing comes to are left as they are.  A path that does not ascend
+ * within the new tokens, or a page outside the cache, leaves the sequence out. */
+typedef struct ensi_clear_keep_args {
+    ensi_clear_seqs s;
+    const int32_t *path, *count;
+    int64_t path_stride;
+} ensi_clear_keep_args;
+int ensi_clear_keep(ensi_ctx *ctx, ensi_kv *const *kv, int32_t caches, const ensi_clear_keep_args *args, void *stream);
+
+/* Rows that continue sequences, in the caches of any number of layers, which have pages of one size: row i has the length of sequence source[i] and the same full pages; a page that is begun
+ * is copied, as far as it is in use, to page fresh[i], which stands in its place (the next append's, where none is begun).  What follows in table_out is -1.  fresh[i] may be the
+ * begun page itself (the row goes on in it), or -1 where no page is begun; other than that it must be a page that none of the sequences has: this is not
+ * checked, but a page given to two rows is, and the later row left out.  A row that is left out has length 0 and no pages.
+ * lengths: device int32 [seqs], table [seqs][table_width], source, fresh: device int32 [rows]; table_out [rows][table_width], lengths_out [rows] may not meet them. */
+typedef struct ensi_clear_fork_args {
+    const int32_t *table, *lengths, *source, *fresh;
+    int32_t *table_out, *lengths_out;
+    int64_t table_stride, out_stride;
+    int32_t seqs, rows, table_width, pad;
+} ensi_clear_fork_args;
+int ensi_clear_fork(ensi_ctx *ctx, ensi_kv *const *kv, int32_t caches, const ensi_clear_fork_args *args, void *stream);
+
 /* ---- transform alone (parity and measurement of the NTT kernels) -------- */
 /* data: device u64[n_limbs][N]; limb r uses prime index prime_idx[r] (host
  * int32[n_limbs]; 0..L-1 = q, L..L+K-1 = p).  In place.  Forward output order

@@ -29,7 +29,8 @@ EXPORTED = [
     "ensi_ct_checksum", "ensi_weights_prepare", "ensi_weights_free", "ensi_ternary_matmul_prepared", "ensi_rescale_ternary_matmul_prepared",
     "ensi_rotate_static", "ensi_matrix_rate_probe",
     "ensi_clear_norm", "ensi_clear_weights_prepare", "ensi_clear_weights_free", "ensi_clear_matmul", "ensi_clear_cache_wrap", "ensi_clear_cache_free",
-    "ensi_clear_cache_status", "ensi_clear_append", "ensi_clear_attention",
+    "ensi_clear_cache_status", "ensi_clear_append", "ensi_clear_attention", "ensi_clear_append_tree", "ensi_clear_attention_tree", "ensi_clear_sample", "ensi_clear_accept",
+    "ensi_clear_keep", "ensi_clear_fork",
 ]
 
 
@@ -66,6 +67,9 @@ def load():
         lib.ensi_clear_norm.argtypes = [p, ctypes.c_char_p, p]
         lib.ensi_clear_matmul.argtypes = [p, p, p, i64, p, p, i64, i64, i32, p]
         lib.ensi_clear_append.argtypes = lib.ensi_clear_attention.argtypes = [p, p, ctypes.c_char_p, p]
+        lib.ensi_clear_append_tree.argtypes = lib.ensi_clear_attention_tree.argtypes = [p, p, ctypes.c_char_p, p, p]
+        lib.ensi_clear_sample.argtypes = lib.ensi_clear_accept.argtypes = [p, ctypes.c_char_p, p]
+        lib.ensi_clear_keep.argtypes = lib.ensi_clear_fork.argtypes = [p, ctypes.c_char_p, i32, ctypes.c_char_p, p]
         _lib = lib
     return _lib
 
@@ -82,10 +86,15 @@ def _i8(a, shape=None):
         raise EnsiError("expected int8 array of shape %s, got %s" % (shape, a.shape))
     return a
 
-# Packed argument structs of include/ensi.h: ensi_clear_norm_args, ensi_clear_append_args and ensi_clear_attention_args (the latter two begin with ensi_clear_seqs)
+# Packed argument structs of include/ensi.h: ensi_clear_norm_args, ensi_clear_append_args, ensi_clear_attention_args, ensi_clear_keep_args (these three begin with ensi_clear_seqs),
+# ensi_clear_sample_args, ensi_clear_accept_args and ensi_clear_fork_args
 _NORM = struct.Struct("<7Q5q2ifi")
 _APPEND = struct.Struct("<3Q2q4i6Q4q6i")
 _ATTENTION = struct.Struct("<3Q2q4i2Q2q5i2fi")
+_KEEP = struct.Struct("<3Q2q4i2Qq")
+_SAMPLE = struct.Struct("<7Q2q2ifi2f")
+_ACCEPT = struct.Struct("<7Q2q2i")
+_FORK = struct.Struct("<6Q2q4i")
 _PAIRS = {"half": 0, "neighbours": 1}
 _SCORES = {"softmax": 0, "sigmoid": 1}
 _TORCH = None
@@ -174,6 +183,16 @@ def _seqs(table, begin, lengths, tokens, max_new, at):
     pt, st = _rows("table", table, (seqs, width), kind, at)
     return (_whole("begin", begin, (seqs + 1,), kind, at), _whole("lengths", lengths, (seqs,), kind, at), pt, st, tokens, seqs, width,
             tokens if max_new is None else max_new, 0)
+
+
+def _handles(caches):
+    """Addresses of a cache's or several caches' handles, packed."""
+    if isinstance(caches, ClearCache):
+        caches = (caches,)
+    try:
+        return struct.pack("%dQ" % len(caches), *[c.h.value for c in caches])
+    except (struct.error, AttributeError, TypeError):
+        raise EnsiError("caches must be a cache that is not freed, or a list of them") from None
 
 
 class Context:
@@ -657,10 +676,11 @@ class Context:
         self._check(self.lib.ensi_clear_cache_wrap(self.h, *(ctypes.c_void_p(p) for p in ptrs), int(pages), int(heads), int(page), int(dim), ctypes.byref(kv)))
         return ClearCache(self, kv, (k, v, k_scale, v_scale))
 
-    def clear_append(self, cache, table, begin, lengths, k, v, cos, sin, q=None, q_out=None, pairs="half", max_new=None, stream=None):
+    def clear_append(self, cache, table, begin, lengths, k, v, cos, sin, q=None, q_out=None, pairs="half", max_new=None, stream=None, parents=None):
         """Rotates q [tokens][heads][dim] into q_out (made if not given) and k by their positions, and stores k and v [tokens][kv heads][dim] in the cache.
         Sequence i has the tokens begin[i] .. begin[i + 1] - 1 behind lengths[i] cached ones; its pages are table[i] (all int32).  cos, sin: float32
-        [positions][rot / 2], or None for no rotation.  max_new: the most new tokens of a sequence (default: all of them).  Returns q_out."""
+        [positions][rot / 2], or None for no rotation.  max_new: the most new tokens of a sequence (default: all of them, up to 64 with parents).  parents int32 [tokens]: the new tokens of a
+        sequence are a tree of drafted ones, token t's parent the earlier one parents[t] or -1; they are rotated by the length and their depth.  Returns q_out."""
         elsewhere = stream
         at, stream = self._on(stream)
         if len(k.shape) != 3:
@@ -689,18 +709,22 @@ class Context:
             f32 = _TORCH[2]["float32"]
             pc, ps = _whole("cos", cos, cos.shape, f32, at), _whole("sin", sin, cos.shape, f32, at)
         try:
-            args = _APPEND.pack(*_seqs(table, begin, lengths, tokens, max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), pair_code, _type("k", kind), 0)
+            args = _APPEND.pack(*_seqs(table, begin, lengths, tokens, min(tokens, 64) if max_new is None and parents is not None else max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), pair_code, _type("k", kind), 0)
         except (struct.error, OverflowError) as e:
             _no_number(e)
-        rc = self.lib.ensi_clear_append(self.h, cache.h, args, stream)
+        if parents is None:
+            rc = self.lib.ensi_clear_append(self.h, cache.h, args, stream)
+        else:
+            rc = self.lib.ensi_clear_append_tree(self.h, cache.h, args, _whole("parents", parents, (tokens,), _TORCH[2]["int32"], at), stream)
         if rc:
             self._check(rc)
         return q_out
 
-    def clear_attention(self, cache, table, begin, lengths, q, out=None, cap=0.0, window=0, score="softmax", bias=0.0, max_new=None, max_length=None, stream=None):
+    def clear_attention(self, cache, table, begin, lengths, q, out=None, cap=0.0, window=0, score="softmax", bias=0.0, max_new=None, max_length=None, stream=None, parents=None):
         """Causal attention of the new tokens q [tokens][heads][dim] (stored by clear_append before) over their sequences: scores q k / sqrt(dim), capped by
         cap tanh(. / cap), within a window, through a softmax or as sigmoid(. + bias).  lengths as for clear_append (without the new tokens); max_length: the
-        longest sequence with its new tokens (default: what the table holds).  Returns out."""
+        longest sequence with its new tokens (default: what the table holds).  parents as for clear_append: a token of a tree sees the cached tokens, its ancestors and itself, a window
+        counts positions (length and depth).  Returns out."""
         elsewhere = stream
         at, stream = self._on(stream)
         shape, kind = q.shape, q.dtype
@@ -713,17 +737,113 @@ class Context:
             out = _empty(q, shape, kind, elsewhere, at)
         pq, sq = _rows("q", q, shape, kind, at)
         po, so = _rows("out", out, shape, kind, at)
-        s = _seqs(table, begin, lengths, shape[0], max_new, at)
+        s = _seqs(table, begin, lengths, shape[0], min(shape[0], 64) if max_new is None and parents is not None else max_new, at)
         if max_length is None:
             max_length = min(table.shape[1] * cache.page, 1 << 30)
         try:
             args = _ATTENTION.pack(*s, pq, po, sq, so, shape[1], _type("q", kind), score_code, window, max_length, cap, bias, 0)
         except (struct.error, OverflowError) as e:
             _no_number(e)
-        rc = self.lib.ensi_clear_attention(self.h, cache.h, args, stream)
+        if parents is None:
+            rc = self.lib.ensi_clear_attention(self.h, cache.h, args, stream)
+        else:
+            rc = self.lib.ensi_clear_attention_tree(self.h, cache.h, args, _whole("parents", parents, shape[:1], _TORCH[2]["int32"], at), stream)
         if rc:
             self._check(rc)
         return out
+
+    def clear_sample(self, logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, stream=None):
+        """One token for each row of logits [rows][vocab] (any stride between rows): of w = exp((x - max) / temperature), in the order of falling x (lower indices first among equal ones), the
+        first top_k (0: all), of these the shortest part that has top_p of their sum, of these the ones with w >= min_p; among them the first by index at which the running sum exceeds
+        uniform (float32 [rows], in [0, 1)) times the whole.  temperature 0: the first of the largest.  temperature, top_p, min_p: numbers, or float32 [rows]; top_k: a number, or int32
+        [rows].  -1 where there is no distribution (NaN, +inf, nothing but -inf, a parameter out of range).  Returns out, int32 [rows]."""
+        elsewhere = stream
+        at, stream = self._on(stream)
+        if len(logits.shape) != 2:
+            raise EnsiError("logits must be [rows][vocab]")
+        shape, kind = logits.shape, logits.dtype
+        rows, f32, i32 = shape[:1], _TORCH[2]["float32"], _TORCH[2]["int32"]
+        if out is None:
+            out = _empty(logits, rows, i32, elsewhere, at)
+        px, sx = _rows("logits", logits, shape, kind, at)
+
+        def one(name, v, kind, off):  # (address, number)
+            return (_whole(name, v, rows, kind, at), off) if hasattr(v, "data_ptr") else (0, v)
+        (pt, t), (pk, k), (pp, p), (pm, m) = one("temperature", temperature, f32, 1.0), one("top_k", top_k, i32, 0), one("top_p", top_p, f32, 1.0), one("min_p", min_p, f32, 0.0)
+        try:
+            args = _SAMPLE.pack(px, _whole("uniform", uniform, rows, f32, at), pt, pk, pp, pm, _whole("out", out, rows, i32, at), rows[0], sx, shape[1], _type("logits", kind), t, k, p, m)
+        except (struct.error, OverflowError) as e:
+            _no_number(e)
+        rc = self.lib.ensi_clear_sample(self.h, args, stream)
+        if rc:
+            self._check(rc)
+        return out
+
+    def clear_accept(self, begin, parents, drafted, sampled, path=None, count=None, following=None, max_new=None, stream=None):
+        """The drafted tokens that agree with what was sampled: from each sequence's token 0 on, the first child (parents as for clear_append, or None: the next token) whose `drafted` is
+        what was `sampled` at its parent (int32 [tokens] each).  Returns path int32 [seqs][max_new] (indices among the sequence's new tokens, ascending, then -1), count and following int32
+        [seqs]: how many, and what was sampled at the last one.  max_new: the most new tokens of a sequence, up to 64 (default: of path, or all of them)."""
+        elsewhere = stream
+        at, stream = self._on(stream)
+        if len(begin.shape) != 1 or begin.shape[0] < 1 or len(drafted.shape) != 1:
+            raise EnsiError("begin must be [seqs + 1], drafted [tokens]")
+        seqs, shape, i32 = begin.shape[0] - 1, drafted.shape, _TORCH[2]["int32"]
+        if max_new is None:
+            max_new = min(shape[0], 64) if path is None or len(path.shape) != 2 else path.shape[1]
+        path = _empty(begin, (seqs, max_new), i32, elsewhere, at) if path is None else path
+        count = _empty(begin, (seqs,), i32, elsewhere, at) if count is None else count
+        following = _empty(begin, (seqs,), i32, elsewhere, at) if following is None else following
+        pp, sp = _rows("path", path, (seqs, max_new), i32, at)
+        try:
+            args = _ACCEPT.pack(_whole("begin", begin, (seqs + 1,), i32, at), 0 if parents is None else _whole("parents", parents, shape, i32, at), _whole("drafted", drafted, shape, i32, at),
+                                _whole("sampled", sampled, shape, i32, at), pp, _whole("count", count, (seqs,), i32, at), _whole("following", following, (seqs,), i32, at), shape[0], sp, seqs, max_new)
+        except (struct.error, OverflowError) as e:
+            _no_number(e)
+        rc = self.lib.ensi_clear_accept(self.h, args, stream)
+        if rc:
+            self._check(rc)
+        return path, count, following
+
+    def clear_keep(self, caches, table, begin, lengths, path, count, max_new=None, stream=None):
+        """Moves the accepted tokens of a step together in a cache, or in those of all layers (a list; pages of one size): new token path[i][j] of sequence i, j < count[i], to place
+        lengths[i] + j.  A block of 16 that tokens come to has the largest scale of its tokens, the others are rounded again.  begin and lengths as for clear_append, from before
+        the step; path int32 [seqs][max_new], count int32 [seqs] as clear_accept makes them."""
+        at, stream = self._on(stream)
+        handles = _handles(caches)
+        if len(path.shape) != 2 or not lengths.shape:
+            raise EnsiError("path must be [seqs][max_new], lengths [seqs]")
+        if max_new is None:
+            max_new = path.shape[1]
+        i32, seqs = _TORCH[2]["int32"], lengths.shape[0]
+        pp, sp = _rows("path", path, (seqs, max_new), i32, at)
+        try:
+            args = _KEEP.pack(*_seqs(table, begin, lengths, seqs * max_new, max_new, at), pp, _whole("count", count, (seqs,), i32, at), sp)
+        except (struct.error, OverflowError) as e:
+            _no_number(e)
+        rc = self.lib.ensi_clear_keep(self.h, handles, len(handles) // 8, args, stream)
+        if rc:
+            self._check(rc)
+
+    def clear_fork(self, caches, table, lengths, source, fresh, table_out=None, lengths_out=None, stream=None):
+        """Rows that continue sequences, in a cache or in those of all layers (a list; pages of one size): row i has the length of sequence source[i] and its full pages; the page that it
+        has begun is copied to page fresh[i], which stands in its place (int32 [rows]; -1 where none is begun, or the begun page itself for a row that goes on in it).  Places behind are
+        -1.  Returns table_out int32 [rows][pages] and lengths_out int32 [rows]."""
+        elsewhere = stream
+        at, stream = self._on(stream)
+        handles = _handles(caches)
+        if len(table.shape) != 2 or len(source.shape) != 1:
+            raise EnsiError("table must be [seqs][pages], source [rows]")
+        (seqs, width), (rows,), i32 = table.shape, source.shape, _TORCH[2]["int32"]
+        table_out = _empty(table, (rows, width), i32, elsewhere, at) if table_out is None else table_out
+        lengths_out = _empty(table, (rows,), i32, elsewhere, at) if lengths_out is None else lengths_out
+        pt, st = _rows("table", table, (seqs, width), i32, at)
+        po, so = _rows("table_out", table_out, (rows, width), i32, at)
+        args = _FORK.pack(pt, _whole("lengths", lengths, (seqs,), i32, at), _whole("source", source, (rows,), i32, at), _whole("fresh", fresh, (rows,), i32, at), po,
+                          _whole("lengths_out", lengths_out, (rows,), i32, at), st, so, seqs, rows, width, 0)
+        rc = self.lib.ensi_clear_fork(self.h, handles, len(handles) // 8, args, stream)
+        if rc:
+            self._check(rc)
+        return table_out, lengths_out
 
     # ---- timers
     def profile_enable(self, on=True):
@@ -817,4 +937,4 @@ class ClearCache(_Handle):
         _, stream = self.ctx._on(stream)
         self.ctx._check(self.ctx.lib.ensi_clear_cache_status(self.ctx.h, self.h, ctypes.byref(bits), ctypes.c_void_p(stream)))
         if bits.value:
-            raise EnsiError("the cache met %s: left out" % " and ".join(t for b, t in ((1, "page numbers outside it"), (2, "sequences that do not fit the arguments")) if bits.value & b))
+            raise EnsiError("the cache met %s: left out" % " and ".join(t for b, t in ((1, "page numbers outside it"), (2, "sequences that do not fit the arguments"), (4, "trees or paths that are none")) if bits.value & b))

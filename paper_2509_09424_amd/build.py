@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libensi_hip.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "api_keys.hip", "api_static.hip", "api_matmul.hip", "api_pmult.hip", "api_ccmm.hip", "ntt.hip", "ntt16.hip", "keyswitch16.hip", "pmult.hip", "ccmm.hip", "kernels.hip",
-           "accumulate_mfma.hip", "client16.hip", "api_clear.hip", "clear_norm.hip", "clear_matmul.hip", "clear_append.hip", "clear_attention.hip"] + ["keyswitch16_ring.hip:%d" % s for s in range(5)]  # file:s -- compiled with -DKS_RING=s
+           "accumulate_mfma.hip", "client16.hip", "api_clear.hip", "clear_norm.hip", "clear_matmul.hip", "clear_append.hip", "clear_attention.hip", "clear_attention_tree.hip", "clear_sample.hip", "clear_pages.hip"] + ["keyswitch16_ring.hip:%d" % s for s in range(5)]  # file:s -- compiled with -DKS_RING=s
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
@@ -18,7 +18,7 @@ FLAGS = [
     "-Wall", "-Wno-unused-function", "-Wno-unused-parameter",
 ]
 # flags of single sources: matrix instructions that keep their sums in ordinary registers, where every tile's softmax works on them
-SOURCE_FLAGS = {"clear_matmul.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "clear_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+SOURCE_FLAGS = {"clear_matmul.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "clear_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "clear_attention_tree.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def compile_one(src, out, extra=(), verbose=False):

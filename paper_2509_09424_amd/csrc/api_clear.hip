@@ -10,6 +10,7 @@
 #define CLEAR_MAX_NORM_ROWS (1 << 21)  // a grid has fewer than 2^32 threads, a row up to 1024 of them
 #define CLEAR_MAX_SEQS 65535      // a grid's third dimension
 #define CLEAR_MAX_NEW (1 << 20)   // its second one, in blocks of 16 tokens
+#define CLEAR_MAX_CACHES 1024     // layers of one call
 
 static int current_device(ensi_ctx *ctx) {
     int cur = -1;
@@ -209,7 +210,13 @@ static int check_seqs(ensi_ctx *ctx, const char *who, const ensi_clear_seqs &s) 
     return ENSI_OK;
 }
 
-extern "C" int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *a, void *stream) {
+// A tree's parents, where a call takes one
+static int check_tree(ensi_ctx *ctx, const char *who, const ensi_clear_seqs &s) {
+    if (s.max_new > TREE_MAX) ENSI_FAIL(ctx, ENSI_E_SHAPE, "%s: trees of up to %d tokens, not %d", who, TREE_MAX, s.max_new);
+    return ENSI_OK;
+}
+
+static int append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *a, const int32_t *parents, void *stream) {
     if (!ctx) return ENSI_E_BADARG;
     if (!kv || !a || kv->ctx != ctx) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: no cache, or that of another context, or no arguments");
     const KvView &c = kv->view;
@@ -220,6 +227,8 @@ extern "C" int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_ap
     if (a->positions < 0 || !a->q != !a->q_out || (a->q && (a->q_heads < 1 || a->q_heads > CLEAR_MAX_HEADS)))
         ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear append: %d positions, %d query heads (up to %d), queries with q_out", a->positions, a->q_heads, CLEAR_MAX_HEADS);
     if (int rc = check_seqs(ctx, "clear append", a->s)) return rc;
+    if (parents)
+        if (int rc = check_tree(ctx, "clear append", a->s)) return rc;
     if (!a->s.seqs || !a->s.tokens || !a->s.max_new) return ENSI_OK;
     if (!a->k || !a->v || (a->rot && (!a->cos || !a->sin))) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: a null array");
     const int64_t kw = (int64_t)c.heads * c.dim, qw = (int64_t)a->q_heads * c.dim, t = a->s.tokens;
@@ -231,13 +240,21 @@ extern "C" int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_ap
     if (o.meets(k) || o.meets(v)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: q_out overlaps k or v");
     const CacheSpans cache(c);
     if (cache.meets(q) || cache.meets(o) || cache.meets(k) || cache.meets(v)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: q, k, v or q_out overlaps the cache");
+    const Span p(parents, 1, 0, t, 4);
+    if (o.meets(p) || cache.meets(p)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: parents overlaps q_out or the cache");
     if (int rc = current_device(ctx)) return rc;
-    launch_clear_append(ctx, c, *a, (hipStream_t)stream);
+    launch_clear_append(ctx, c, *a, parents, (hipStream_t)stream);
     ENSI_HIP(ctx, hipGetLastError());
     return ENSI_OK;
 }
+extern "C" int ensi_clear_append(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *a, void *stream) { return append(ctx, kv, a, nullptr, stream); }
+extern "C" int ensi_clear_append_tree(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *a, const int32_t *parents, void *stream) {
+    if (!ctx) return ENSI_E_BADARG;
+    if (!parents) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear append: a tree needs parents");
+    return append(ctx, kv, a, parents, stream);
+}
 
-extern "C" int ensi_clear_attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *a, void *stream) {
+static int attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *a, const int32_t *parents, void *stream) {
     if (!ctx) return ENSI_E_BADARG;
     if (!kv || !a || kv->ctx != ctx) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: no cache, or that of another context, or no arguments");
     const KvView &c = kv->view;
@@ -247,16 +264,119 @@ extern "C" int ensi_clear_attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear
     if (a->window < 0 || a->max_length < 0 || a->max_length > (1 << 30) || !(a->cap >= 0) || isinf(a->cap) || !isfinite(a->bias))
         ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: window %d, cap %g, bias %g, max_length %d", a->window, a->cap, a->bias, a->max_length);
     if (int rc = check_seqs(ctx, "clear attention", a->s)) return rc;
+    if (parents)
+        if (int rc = check_tree(ctx, "clear attention", a->s)) return rc;
     if (!a->s.seqs || !a->s.tokens || !a->s.max_new) return ENSI_OK;
     if (!a->q || !a->out) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: a null array");
     const int64_t w = (int64_t)a->q_heads * c.dim, t = a->s.tokens;
     if (t > 1 && (a->q_stride < w || a->out_stride < w)) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear attention: tokens overlap");
     const Span q(a->q, t, a->q_stride, w, 2), o(a->out, t, a->out_stride, w, 2);
     if (q.meets(o)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: out overlaps q");
+    if (Span(parents, 1, 0, t, 4).meets(o)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: out overlaps parents");
     if (CacheSpans(c).meets(o)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: out overlaps the cache");
     if ((int64_t)a->s.max_new * a->q_heads > INT32_MAX / 16) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear attention: %d new tokens of %d heads are too many", a->s.max_new, a->q_heads);
     if (int rc = current_device(ctx)) return rc;
-    launch_clear_attention(ctx, c, *a, (hipStream_t)stream);
+    if (parents) launch_clear_attention_tree(ctx, c, *a, parents, (hipStream_t)stream);
+    else launch_clear_attention(ctx, c, *a, (hipStream_t)stream);
+    ENSI_HIP(ctx, hipGetLastError());
+    return ENSI_OK;
+}
+extern "C" int ensi_clear_attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *a, void *stream) { return attention(ctx, kv, a, nullptr, stream); }
+extern "C" int ensi_clear_attention_tree(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *a, const int32_t *parents, void *stream) {
+    if (!ctx) return ENSI_E_BADARG;
+    if (!parents) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear attention: a tree needs parents");
+    return attention(ctx, kv, a, parents, stream);
+}
+
+extern "C" int ensi_clear_sample(ensi_ctx *ctx, const ensi_clear_sample_args *a, void *stream) {
+    if (!ctx) return ENSI_E_BADARG;
+    if (!a) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear sample: no arguments");
+    const int size = type_size(a->type);
+    if (!size) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear sample: unknown type %d", a->type);
+    if (a->rows < 0 || a->rows > (1 << 20) || a->vocab < 1 || a->vocab > (1 << 24))
+        ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear sample: %lld rows (up to 2^20) of %d logits (1 to 2^24)", (long long)a->rows, a->vocab);
+    if (a->rows == 0) return ENSI_OK;
+    if (!a->logits || !a->uniform || !a->out) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear sample: logits, uniform and out are needed");
+    if (a->rows > 1 && a->stride < a->vocab) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear sample: rows overlap (their stride is below %d)", a->vocab);
+    if ((!a->temperature && !(a->all_temperature >= 0 && isfinite(a->all_temperature))) || (!a->top_p && isnan(a->all_top_p)) || (!a->min_p && isnan(a->all_min_p)))
+        ENSI_FAIL(ctx, ENSI_E_BADARG, "clear sample: temperature %g, top_p %g, min_p %g", a->all_temperature, a->all_top_p, a->all_min_p);
+    const Span o(a->out, 1, 0, a->rows, 4);
+    const auto meets = [&](const void *p) { return Span(p, 1, 0, a->rows, 4).meets(o); };
+    if (Span(a->logits, a->rows, a->stride, a->vocab, size).meets(o) || meets(a->uniform) || meets(a->temperature) || meets(a->top_k) || meets(a->top_p) || meets(a->min_p))
+        ENSI_FAIL(ctx, ENSI_E_BADARG, "clear sample: out overlaps an input");
+    if (int rc = current_device(ctx)) return rc;
+    launch_clear_sample(ctx, *a, (hipStream_t)stream);
+    ENSI_HIP(ctx, hipGetLastError());
+    return ENSI_OK;
+}
+
+extern "C" int ensi_clear_accept(ensi_ctx *ctx, const ensi_clear_accept_args *a, void *stream) {
+    if (!ctx) return ENSI_E_BADARG;
+    if (!a) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear accept: no arguments");
+    if (a->seqs < 0 || a->seqs > CLEAR_MAX_SEQS || a->tokens < 0 || a->tokens > INT32_MAX || a->max_new < 0 || a->max_new > TREE_MAX)
+        ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear accept: %d sequences (up to %d) with %lld new tokens, at most %d each (up to %d)", a->seqs, CLEAR_MAX_SEQS, (long long)a->tokens, a->max_new, TREE_MAX);
+    if (a->seqs == 0) return ENSI_OK;
+    if (!a->begin || !a->count || !a->following || (a->max_new && !a->path) || (a->tokens && (!a->drafted || !a->sampled))) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear accept: a null array");
+    if (a->seqs > 1 && a->path_stride < a->max_new) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear accept: paths overlap (their stride is below %d)", a->max_new);
+    const Span in[] = {Span(a->begin, 1, 0, (int64_t)a->seqs + 1, 4), Span(a->parents, 1, 0, a->tokens, 4), Span(a->drafted, 1, 0, a->tokens, 4), Span(a->sampled, 1, 0, a->tokens, 4)};
+    const Span out[] = {Span(a->path, a->seqs, a->path_stride, a->max_new, 4), Span(a->count, 1, 0, a->seqs, 4), Span(a->following, 1, 0, a->seqs, 4)};
+    for (int i = 0; i < 3; i++) {
+        for (const Span &s : in)
+            if (s.meets(out[i])) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear accept: an output overlaps an input");
+        for (int j = 0; j < i; j++)
+            if (out[i].meets(out[j])) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear accept: outputs overlap");
+    }
+    if (int rc = current_device(ctx)) return rc;
+    launch_clear_accept(ctx, *a, (hipStream_t)stream);
+    ENSI_HIP(ctx, hipGetLastError());
+    return ENSI_OK;
+}
+
+// The caches of a call: this context's, with pages of one size, each of them once.
+static int check_caches(ensi_ctx *ctx, const char *who, ensi_kv *const *kv, int caches) {
+    if (!kv || caches < 1 || caches > CLEAR_MAX_CACHES) ENSI_FAIL(ctx, kv ? ENSI_E_SHAPE : ENSI_E_BADARG, "%s: %d caches (1 to %d)", who, caches, CLEAR_MAX_CACHES);
+    for (int i = 0; i < caches; i++) {
+        if (!kv[i] || kv[i]->ctx != ctx) ENSI_FAIL(ctx, ENSI_E_BADARG, "%s: no cache, or that of another context", who);
+        if (kv[i]->view.page != kv[0]->view.page) ENSI_FAIL(ctx, ENSI_E_SHAPE, "%s: caches with pages of %d and of %d tokens", who, kv[0]->view.page, kv[i]->view.page);
+        for (int j = 0; j < i; j++)
+            if (kv[i]->view.k == kv[j]->view.k) ENSI_FAIL(ctx, ENSI_E_BADARG, "%s: a cache is there twice", who);
+    }
+    return ENSI_OK;
+}
+
+extern "C" int ensi_clear_keep(ensi_ctx *ctx, ensi_kv *const *kv, int32_t caches, const ensi_clear_keep_args *a, void *stream) {
+    if (!ctx) return ENSI_E_BADARG;
+    if (!a) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear keep: no arguments");
+    if (int rc = check_caches(ctx, "clear keep", kv, caches)) return rc;
+    if (int rc = check_seqs(ctx, "clear keep", a->s)) return rc;
+    if (int rc = check_tree(ctx, "clear keep", a->s)) return rc;
+    if (!a->s.seqs || !a->s.tokens || !a->s.max_new) return ENSI_OK;
+    if (!a->path || !a->count) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear keep: path and count are needed");
+    if (a->s.seqs > 1 && a->path_stride < a->s.max_new) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear keep: paths overlap (their stride is below %d)", a->s.max_new);
+    if (int rc = current_device(ctx)) return rc;
+    launch_clear_keep(ctx, kv, caches, *a, (hipStream_t)stream);
+    ENSI_HIP(ctx, hipGetLastError());
+    return ENSI_OK;
+}
+
+extern "C" int ensi_clear_fork(ensi_ctx *ctx, ensi_kv *const *kv, int32_t caches, const ensi_clear_fork_args *a, void *stream) {
+    if (!ctx) return ENSI_E_BADARG;
+    if (!a) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear fork: no arguments");
+    if (int rc = check_caches(ctx, "clear fork", kv, caches)) return rc;
+    if (a->seqs < 0 || a->seqs > CLEAR_MAX_SEQS || a->rows < 0 || a->rows > CLEAR_MAX_SEQS || a->table_width < 1)
+        ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear fork: %d sequences and %d rows (up to %d), tables of %d pages", a->seqs, a->rows, CLEAR_MAX_SEQS, a->table_width);
+    if (a->rows == 0) return ENSI_OK;
+    if (!a->source || !a->fresh || !a->table_out || !a->lengths_out || (a->seqs && (!a->table || !a->lengths))) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear fork: a null array");
+    if ((a->seqs > 1 && a->table_stride < a->table_width) || (a->rows > 1 && a->out_stride < a->table_width)) ENSI_FAIL(ctx, ENSI_E_SHAPE, "clear fork: rows of a table overlap");
+    const Span table(a->table, a->seqs, a->table_stride, a->table_width, 4), lengths(a->lengths, 1, 0, a->seqs, 4), source(a->source, 1, 0, a->rows, 4), fresh(a->fresh, 1, 0, a->rows, 4);
+    const Span table_out(a->table_out, a->rows, a->out_stride, a->table_width, 4), lengths_out(a->lengths_out, 1, 0, a->rows, 4);
+    for (const Span *in : {&table, &lengths, &source, &fresh})
+        if (in->meets(table_out) || in->meets(lengths_out)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear fork: an output overlaps an input");
+    if (table_out.meets(lengths_out)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear fork: outputs overlap");
+    for (int i = 0; i < caches; i++)
+        if (CacheSpans(kv[i]->view).meets(table_out) || CacheSpans(kv[i]->view).meets(lengths_out)) ENSI_FAIL(ctx, ENSI_E_BADARG, "clear fork: an output overlaps a cache");
+    if (int rc = current_device(ctx)) return rc;
+    launch_clear_fork(ctx, kv, caches, *a, (hipStream_t)stream);
     ENSI_HIP(ctx, hipGetLastError());
     return ENSI_OK;
 }

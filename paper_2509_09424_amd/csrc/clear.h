@@ -49,6 +49,12 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 #define KV_BLOCK 16  // tokens that share a scale
 
+// Four floats of at most 448 to e4m3, nearest, ties to even.
+__device__ __forceinline__ u32 to_e4m3(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (u32)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
 // A cache as the kernels see it.
 struct KvView {
     unsigned char *k, *v;
@@ -72,6 +78,39 @@ __device__ __forceinline__ SeqPart seq_part(const ensi_clear_seqs &s, int seq, i
     return p;
 }
 
+// A tree of a sequence's new tokens, a wave's width of them at most: each names an earlier one as its parent, or none (-1).  Lane t of a wave gets token t's line, the bits
+// of itself and its ancestors, in as many steps as the number of tokens has bits: every step adds the line of the first ancestor that is not in it yet.
+#define TREE_MAX 64
+struct Tree {
+    u64 line;
+    int depth;   // ancestors
+    bool good;   // of the whole tree: no parent behind its child or below -1 (the status then says so)
+};
+__device__ __forceinline__ Tree tree_of(const int32_t *parents, const SeqPart &part, int *status) {
+    const int lane = threadIdx.x % 64;
+    int up = lane < part.count ? parents[part.first + lane] : -1;
+    Tree t;
+    t.good = !__any(up < -1 || up >= lane);
+    if (!t.good) {
+        if (lane == 0) atomicOr(status, ENSI_KV_BAD_TREE);
+        up = -1;
+    }
+    u32 lo = lane < 32 ? 1u << lane : 0, hi = lane < 32 ? 0 : 1u << (lane - 32);
+    for (int k = 1; k < part.count; k *= 2) {
+        const int from = max(up, 0);
+        const u32 add_lo = __shfl(lo, from), add_hi = __shfl(hi, from);
+        const int next = __shfl(up, from);
+        if (up >= 0) {
+            lo |= add_lo;
+            hi |= add_hi;
+            up = next;
+        }
+    }
+    t.line = (u64)hi << 32 | lo;
+    t.depth = __popcll(t.line) - 1;
+    return t;
+}
+
 // ---- handles
 // Ternary weights of a clear product on the device.
 struct ensi_cw {
@@ -92,8 +131,13 @@ void launch_clear_norm(ensi_ctx *ctx, const ensi_clear_norm_args &a, hipStream_t
 void launch_clear_matmul(ensi_ctx *ctx, const ensi_cw *cw, const int8_t *codes, int64_t codes_stride, const float *scales, void *out,
                          int64_t out_stride, int64_t rows, int type, hipStream_t st);
 void launch_clear_pack(const int8_t *d_W, int d, int m, int units, int m_tiles, u32 *w, int *bad, hipStream_t st);
-void launch_clear_append(ensi_ctx *ctx, const KvView &kv, const ensi_clear_append_args &a, hipStream_t st);
+void launch_clear_append(ensi_ctx *ctx, const KvView &kv, const ensi_clear_append_args &a, const int32_t *parents, hipStream_t st);
 void launch_clear_attention(ensi_ctx *ctx, const KvView &kv, const ensi_clear_attention_args &a, hipStream_t st);
+void launch_clear_attention_tree(ensi_ctx *ctx, const KvView &kv, const ensi_clear_attention_args &a, const int32_t *parents, hipStream_t st);
+void launch_clear_accept(ensi_ctx *ctx, const ensi_clear_accept_args &a, hipStream_t st);
+void launch_clear_keep(ensi_ctx *ctx, const ensi_kv *const *kv, int caches, const ensi_clear_keep_args &a, hipStream_t st);
+void launch_clear_fork(ensi_ctx *ctx, const ensi_kv *const *kv, int caches, const ensi_clear_fork_args &a, hipStream_t st);
+void launch_clear_sample(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStream_t st);
 
 // Raises a kernel's limit of dynamic LDS, once in a context.
 inline void clear_lds(ensi_ctx *ctx, const void *kernel, int bytes) {

@@ -4,7 +4,10 @@
 // not hang on how a compiler joins them.  A block of 16 tokens and a head has one scale, the smallest power of two that brings its largest value to
 // 448: a wave owns the block of a head, whichever of the block's tokens are new, so that nothing is shared and nothing added up in an order of
 // its own.  Every element is read once and written once: prompts are bound by memory (5177 tokens of 16 heads of 96 in f16: 22 us, 3.6 TB/s), a decoding step by the
-// launch and the chain length, page, scale (64 sequences: 5.8 us).
+// launch and the chain length, page, scale (64 sequences: 5.8 us).  Drafted tokens of a tree are stored one behind the other and rotated by the position that they
+// would have if accepted: the length and their depth.
+#include <type_traits>
+
 #include "clear.h"
 
 struct AppendView {
@@ -13,19 +16,14 @@ struct AppendView {
     const void *q, *k, *v;
     void *q_out;
     const float *cos, *sin;
+    const int32_t *parents;  // of a tree of new tokens
     int64_t q_stride, q_out_stride, k_stride, v_stride;
     int q_heads, rot, positions, neighbours;
 };
 
-// Four floats of at most 448 to e4m3, nearest, ties to even.
-__device__ __forceinline__ u32 to_e4m3(float a, float b, float c, float d) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (u32)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-}
-
 // One wave: the tokens of one block of 16 positions, one head of the queries, keys or values.  An item is 16 elements of a token in two chunks of 8:
 // the two halves of 8 pairs, or 16 neighbours where pairs are neighbours or nothing is rotated.  ITEMS = ceil(dim / 64) of them to a lane.
-template <int TYPE, int ITEMS>
+template <int TYPE, int ITEMS, bool TREE>
 __global__ __launch_bounds__(256) void k_clear_append(AppendView a) {
 #pragma clang fp contract(off)
     typedef typename Elem<TYPE>::type T;
@@ -33,7 +31,17 @@ __global__ __launch_bounds__(256) void k_clear_append(AppendView a) {
     int slot = blockIdx.x * 4 + threadIdx.x / 64;
     slot = __builtin_amdgcn_readfirstlane(slot);
     if (slot >= a.q_heads + 2 * a.kv.heads) return;
-    const SeqPart part = seq_part(a.s, seq, a.kv.page, a.rot ? min(a.positions, 1 << 30) : 1 << 30, a.kv.status);
+    const SeqPart part = seq_part(a.s, seq, a.kv.page, a.rot && !TREE ? min(a.positions, 1 << 30) : 1 << 30, a.kv.status);
+    int depth = 0;  // lane t: of new token t
+    if (TREE && part.count > 0) {
+        const Tree tree = tree_of(a.parents, part, a.kv.status);
+        if (!tree.good) return;
+        depth = tree.depth;
+        if (a.rot && __any(lane < part.count && part.ctx + depth >= a.positions)) {
+            if (lane == 0) atomicOr(a.kv.status, ENSI_KV_BAD_LENGTH);
+            return;
+        }
+    }
     const int block = part.ctx / KV_BLOCK + blockIdx.y, start = block * KV_BLOCK;
     if (part.count == 0 || start >= part.ctx + part.count) return;
     const int from = max(part.ctx, start), to = min(part.ctx + part.count, start + KV_BLOCK);  // the new positions in this block
@@ -57,6 +65,7 @@ __global__ __launch_bounds__(256) void k_clear_append(AppendView a) {
     for (int i = 0; i < ITEMS; i++) {
         const int item = lane + 64 * i, unit = item % units;
         pos[i] = start + item / units;
+        const int place = TREE ? part.ctx + __shfl(depth, (pos[i] - part.ctx) & 63) : pos[i];  // (asked for by every lane, used by those with a new token)
         at[i][0] = at[i][1] = 0;
 #pragma unroll
         for (int c = 0; c < 2; c++)
@@ -74,7 +83,7 @@ __global__ __launch_bounds__(256) void k_clear_append(AppendView a) {
         Chunk<TYPE>::load(x[i][1], row + at[i][1]);
         if (turned) {
             float c[8], s[8];
-            const int64_t angle = (int64_t)pos[i] * (rot / 2) + 8 * unit;
+            const int64_t angle = (int64_t)place * (rot / 2) + 8 * unit;
             Chunk<ENSI_T_F32>::load(c, a.cos + angle);
             Chunk<ENSI_T_F32>::load(s, a.sin + angle);
             const auto turn = [](float &u, float &w, float cosine, float sine) {
@@ -164,15 +173,20 @@ static void append_type(const AppendView &v, hipStream_t st) {
     const int slots = v.q_heads + 2 * v.kv.heads;
     // the new tokens of a sequence touch at most this many blocks, wherever they begin
     const dim3 grid((slots + 3) / 4, (v.s.max_new + 2 * KV_BLOCK - 2) / KV_BLOCK, v.s.seqs), block(256);
-    if (v.kv.dim <= 64) hipLaunchKernelGGL((k_clear_append<TYPE, 1>), grid, block, 0, st, v);
-    else if (v.kv.dim <= 128) hipLaunchKernelGGL((k_clear_append<TYPE, 2>), grid, block, 0, st, v);
-    else if (v.kv.dim <= 192) hipLaunchKernelGGL((k_clear_append<TYPE, 3>), grid, block, 0, st, v);
-    else hipLaunchKernelGGL((k_clear_append<TYPE, 4>), grid, block, 0, st, v);
+    const auto go = [&](auto tree) {
+        constexpr bool TREE = decltype(tree)::value;
+        if (v.kv.dim <= 64) hipLaunchKernelGGL((k_clear_append<TYPE, 1, TREE>), grid, block, 0, st, v);
+        else if (v.kv.dim <= 128) hipLaunchKernelGGL((k_clear_append<TYPE, 2, TREE>), grid, block, 0, st, v);
+        else if (v.kv.dim <= 192) hipLaunchKernelGGL((k_clear_append<TYPE, 3, TREE>), grid, block, 0, st, v);
+        else hipLaunchKernelGGL((k_clear_append<TYPE, 4, TREE>), grid, block, 0, st, v);
+    };
+    if (v.parents) go(std::true_type());
+    else go(std::false_type());
 }
 
-void launch_clear_append(ensi_ctx *ctx, const KvView &kv, const ensi_clear_append_args &a, hipStream_t st) {
+void launch_clear_append(ensi_ctx *ctx, const KvView &kv, const ensi_clear_append_args &a, const int32_t *parents, hipStream_t st) {
     ScopedTimer timer(ctx, "k_clear_append", st);
-    const AppendView v = {kv, a.s, a.q, a.k, a.v, a.q_out, a.cos, a.sin, a.q_stride, a.q_out_stride, a.k_stride, a.v_stride, a.q ? a.q_heads : 0, a.rot, a.positions, a.pairs == ENSI_ROT_NEIGHBOURS};
+    const AppendView v = {kv, a.s, a.q, a.k, a.v, a.q_out, a.cos, a.sin, parents, a.q_stride, a.q_out_stride, a.k_stride, a.v_stride, a.q ? a.q_heads : 0, a.rot, a.positions, a.pairs == ENSI_ROT_NEIGHBOURS};
     if (a.type == ENSI_T_F32) return append_type<ENSI_T_F32>(v, st);
     if (a.type == ENSI_T_BF16) return append_type<ENSI_T_BF16>(v, st);
     append_type<ENSI_T_F16>(v, st);

@@ -245,3 +245,13 @@ __device__ __forceinline__ Last last_of(float m, float l, const ANY &any) {
 __device__ __forceinline__ float half_lift(float from, float to) { return from == to ? 1.0f : __builtin_amdgcn_exp2f(0.5f * (from - to)); }
 
 #define JOIN_MAX 256  // parts of a row that a join takes
+
+inline AttentionView attention_view(ensi_ctx *ctx, const KvView &kv, const ensi_clear_attention_args &a) {
+    AttentionView v = {kv, a.s, a.q, a.out, a.q_stride, a.out_stride, a.q_heads, a.q_heads / kv.heads, a.window, a.max_length, a.cap, 0, 0, a.bias * LOG2E, 0, 0, ctx->ws_clear};
+    const float root = 1.0f / sqrtf((float)kv.dim);
+    v.factor = a.cap > 0 ? root : root * LOG2E;
+    // 1 / cap and cap log2 e stay finite: scores below 2^-120 are as good as 0, and of scores that a cap beyond 2^126 reaches only which are equal matters
+    if (a.cap > 0) v.cap = std::min(std::max(a.cap, 0x1p-120f), 0x1p126f);
+    v.cap_inv = a.cap > 0 ? 1.0f / v.cap : 0.0f;
+    return v;
+}

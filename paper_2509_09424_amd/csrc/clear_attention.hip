@@ -671,12 +671,7 @@ static void attention_dim(ensi_ctx *ctx, const AttentionView &v, hipStream_t st)
 }
 
 void launch_clear_attention(ensi_ctx *ctx, const KvView &kv, const ensi_clear_attention_args &a, hipStream_t st) {
-    AttentionView v = {kv, a.s, a.q, a.out, a.q_stride, a.out_stride, a.q_heads, a.q_heads / kv.heads, a.window, a.max_length, a.cap, 0, 0, a.bias * LOG2E, 0, 0, ctx->ws_clear};
-    const float root = 1.0f / sqrtf((float)kv.dim);
-    v.factor = a.cap > 0 ? root : root * LOG2E;
-    // 1 / cap and cap log2 e stay finite: scores below 2^-120 are as good as 0, and of scores that a cap beyond 2^126 reaches only which are equal matters
-    if (a.cap > 0) v.cap = std::min(std::max(a.cap, 0x1p-120f), 0x1p126f);
-    v.cap_inv = a.cap > 0 ? 1.0f / v.cap : 0.0f;
+    const AttentionView v = attention_view(ctx, kv, a);
     if (a.type == ENSI_T_BF16) {
         if (a.score == ENSI_SCORE_SOFTMAX) return attention_dim<ENSI_T_BF16, ENSI_SCORE_SOFTMAX>(ctx, v, st);
         return attention_dim<ENSI_T_BF16, ENSI_SCORE_SIGMOID>(ctx, v, st);

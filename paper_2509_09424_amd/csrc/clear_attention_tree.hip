@@ -1,0 +1,440 @@
+// Attention of trees of drafted tokens over a paged cache (the mathematics: clear_attention.h).  New token t of a sequence sees the cached tokens, itself and its ancestors; its
+// position is the length and its depth.
+//
+// A sequence has up to 64 new tokens, so one word of 64 bits holds what a row sees of them, and 64 rows or fewer read the same long cache: a wave takes RT tiles of 16 rows
+// at once, widens a tile of 32 keys and values once for all of them, and the keys are split over the waves and over workgroups.
+#include "clear_attention.h"
+
+// Which of the 32 keys from key0 on a row sees: cached ones within the window of its place, and those of its line.
+__device__ __forceinline__ u32 seen_keys(const SeqPart &part, int window, u64 line, int place, int key0) {
+    const int old = part.ctx - key0;  // keys of the tile that are cached ones
+    u32 seen = old >= 32 ? ~0u : old > 0 ? (1u << old) - 1 : 0;
+    if (window > 0) {
+        const int dark = place - window + 1 - key0;  // of its first keys lie before the window
+        if (dark > 0) seen = dark >= 32 ? 0 : seen & (~0u << dark);
+    }
+    if (old <= 0) {
+        if (old > -64) seen |= (u32)(line >> -old);
+    } else if (old < 32)
+        seen |= (u32)line << old;
+    return seen;
+}
+// Whether any key that a row sees is in the cache.
+__device__ __forceinline__ bool sees_any_of(const AttentionView &a, int seq, const SeqPart &part, u64 line, int place) {
+    for (int key = a.window > 0 ? max(0, place - a.window + 1) : 0; key < part.ctx; key = (key / a.kv.page + 1) * a.kv.page)
+        if (block_of(a, seq, 0, key) >= 0) return true;
+    for (int t = 0; t < part.count; t++)
+        if ((line >> t & 1) && block_of(a, seq, 0, part.ctx + t) >= 0) return true;
+    return false;
+}
+// The keys that a sequence's trees look at, in tiles of 32.
+struct TreeKeys {
+    int lo, last, tiles;
+};
+__device__ __forceinline__ TreeKeys tree_keys(const SeqPart &part, int window) {
+    TreeKeys k;
+    k.lo = window > 0 ? max(0, part.ctx - window + 1) & ~31 : 0;
+    k.last = part.ctx + part.count - 1;
+    k.tiles = (k.last + 1 - k.lo + 31) / 32;
+    return k;
+}
+// The part of a line within the window: ancestors come before their children, so the nearest ones are its highest bits.
+__device__ __forceinline__ u64 near_line(u64 line, int window) {
+    if (window > 0)
+        for (int more = __popcll(line) - window; more > 0; more--) line &= line - 1;
+    return line;
+}
+
+template <int TYPE, int DIM, int SCORE, int RT>
+__global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, const int32_t *parents, int split_tiles) {
+    typedef typename Elem<TYPE>::type T;
+    typedef Wide<TYPE> W;
+    typedef typename W::vec vec;
+    constexpr int STEPS = DIM / 32, TILES = DIM / 16, PIECE = Split<DIM>::PIECE, REST = Split<DIM>::REST, MAIN = Split<DIM>::MAIN;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, g = lane / 16;
+    const int blocks = (a.row_tiles + RT - 1) / RT;
+    const int seq = blockIdx.z, head = blockIdx.x / blocks, row0 = 16 * RT * (blockIdx.x % blocks), split = blockIdx.y;
+    const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
+    const int rows = part.count * a.group;
+    const TreeKeys keys = tree_keys(part, a.window);
+    const int tile0 = split * split_tiles, tile1 = min(tile0 + split_tiles, keys.tiles);
+    if (row0 >= rows || tile0 >= tile1) return;
+    __shared__ u64 lines[TREE_MAX];
+    __shared__ int places[TREE_MAX];
+    {
+        const Tree tree = tree_of(parents, part, a.kv.status);
+        if (!tree.good) return;
+        if (wave == 0) {
+            lines[lane] = near_line(tree.line, a.window);
+            places[lane] = part.ctx + tree.depth;
+        }
+    }
+    __syncthreads();
+    int index[RT];  // of the row's token among the new ones
+    vec q[RT][STEPS];
+    Rows16<DIM> st[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        const int row = min(row0 + 16 * rt + n, rows - 1);
+        index[rt] = row / a.group;
+        typedef vec loose __attribute__((aligned(2)));
+        const T *p = (const T *)a.q + (int64_t)(part.first + index[rt]) * a.q_stride + (int64_t)(head * a.group + row % a.group) * DIM + g * (DIM / 4);
+#pragma unroll
+        for (int s = 0; s < STEPS; s++) q[rt][s] = *(const loose *)(p + 8 * s);
+        st[rt].clear();
+    }
+    int nan_from = INT32_MAX, nan_to = -1;  // keys between which values had NaN
+    for (int batch = tile0 + wave; batch < tile1; batch += 4 * 32) {
+        // 32 tiles of this wave at once: lane l looks up the block of 16 keys of half l % 2 of tile l / 2
+        int my_block = 0, my_good = 0;
+        float my_k = 1, my_v = 1;
+        {
+            const int t = batch + 4 * (lane / 2), key = keys.lo + 32 * t + 16 * (lane % 2);
+            if (t < tile1 && key <= keys.last && (a.window <= 0 || key + KV_BLOCK - 1 > part.ctx - a.window)) {
+                const int block = block_of(a, seq, head, key);
+                if (block >= 0) {
+                    my_block = block;
+                    my_good = 1;
+                    my_k = a.kv.ks[block];
+                    my_v = fmaxf(a.kv.vs[block], 0x1p-64f);
+                } else
+                    atomicOr(a.kv.status, ENSI_KV_BAD_PAGE);
+            }
+        }
+        const int turns = min(32, (tile1 - batch + 3) / 4);
+        // keys: lane (n, g) has places DIM / 4 g .. of key n; values: places PIECE n .. of keys 4 g .. 4 g + 3 of either half
+        constexpr int WORDS = (PIECE + REST + 3) / 4;
+        struct Codes {
+            u32x2 k[2][STEPS];
+            u32 v[2][WORDS][4];
+        };
+        const int k_at = n * DIM + g * (DIM / 4), v_at = 4 * g * DIM + PIECE * n, rest_at = 4 * g * DIM + MAIN + REST * n;
+        const auto fetch = [&](Codes &to, int i) {
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                // a wave's base and a lane's offset of 32 bits: no registers for 64-bit addresses
+                const unsigned char *p = a.kv.k + (int64_t)__builtin_amdgcn_readlane(my_block, 2 * i + h) * (KV_BLOCK * DIM);
+#pragma unroll
+                for (int s = 0; s < STEPS; s++) to.k[h][s] = *(const u32x2 *)(p + (u32)(k_at + 8 * s));
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const unsigned char *p = a.kv.v + (int64_t)__builtin_amdgcn_readlane(my_block, 2 * i + h) * (KV_BLOCK * DIM);
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    typedef u32 piece __attribute__((ext_vector_type(PIECE / 4)));
+                    const piece v = *(const piece *)(p + (u32)(v_at + r * DIM));
+#pragma unroll
+                    for (int w = 0; w < PIECE / 4; w++) to.v[h][w][r] = v[w];
+                    if (REST == 4) to.v[h][WORDS - 1][r] = *(const u32 *)(p + (u32)(rest_at + r * DIM));
+                    if (REST == 2) to.v[h][WORDS - 1][r] = *(const unsigned short *)(p + (u32)(rest_at + r * DIM));
+                }
+            }
+        };
+        for (int i = 0; i < turns; i++) {
+            const int key0 = keys.lo + 32 * (batch + 4 * i);
+            int good[2];
+            float ks[2], vs[2], lv[2];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                good[h] = __builtin_amdgcn_readlane(my_good, 2 * i + h);
+                ks[h] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), 2 * i + h));
+                vs[h] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 2 * i + h));
+                lv[h] = SCORE == ENSI_SCORE_SIGMOID ? 0 : __builtin_amdgcn_logf(vs[h]);
+            }
+            Codes now;
+            fetch(now, i);
+            const bool masked = key0 + 31 >= part.ctx || (a.window > 0 && key0 <= keys.last - a.window) || !good[0] || !good[1];
+            vec k[2][STEPS];
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int s = 0; s < STEPS; s++) k[h][s] = W::widen(now.k[h][s][0], now.k[h][s][1]);
+            Weights p[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) {
+                f32x4 qk[2];
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    qk[h] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+                    for (int s = 0; s < STEPS; s++) qk[h] = W::mfma16(k[h][s], q[rt][s], qk[h]);
+                }
+                float u[2][4];
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) u[h][r] = qk[h][r];
+                if (a.cap > 0) scores_of<SCORE, true>(u, ks, a);
+                else scores_of<SCORE, false>(u, ks, a);
+                if (SCORE == ENSI_SCORE_SIGMOID)
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) u[h][r] = vs[h] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[h][r]));
+                if (masked) {
+                    u32 seen = seen_keys(part, a.window, lines[index[rt]], places[index[rt]], key0);
+                    seen &= (good[0] ? 0xffffu : 0) | (good[1] ? 0xffff0000u : 0);
+                    seen >>= 4 * g;
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) u[h][r] = seen >> (16 * h + r) & 1 ? u[h][r] : SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+                }
+                float most = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+#pragma unroll
+                for (int h = 0; h < 2; h++) most = most_of(most, most_of(most_of(u[h][0], u[h][1], u[h][2]), u[h][3]) + lv[h]);
+                most = most_of(most, __shfl_xor(most, 16));
+                most = most_of(most, __shfl_xor(most, 32));
+                if (SCORE == ENSI_SCORE_SIGMOID) most = most_of(__builtin_amdgcn_logf(most), -120.0f);
+                const float m = most_of(st[rt].m, most), base = m == -__builtin_inff() ? 0.0f : m;
+                const float lift = half_lift(st[rt].m, base);
+                st[rt].m = m;
+                if (__any(lift != 1.0f)) {
+                    const bool deep = __any(lift < HALF_LIFT_DEEP);
+                    if (deep) st[rt].scale(lift);
+                    st[rt].scale(deep ? lift : lift * lift);
+                    st[rt].l = st[rt].l * lift * lift;
+                }
+                const float unit = __builtin_amdgcn_exp2f(0.5f * (WEIGHT_LIFT - base));  // sigmoid: half of the way to the reference
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int r = 0; r < 4; r += 2) {
+                        if (SCORE == ENSI_SCORE_SIGMOID) {
+                            p[rt].set(4 * h + r, u[h][r] * unit * unit, u[h][r + 1] * unit * unit);
+                        } else {
+                            const float e0 = __builtin_amdgcn_exp2f(u[h][r] - (base - TERM_LIFT)), e1 = __builtin_amdgcn_exp2f(u[h][r + 1] - (base - TERM_LIFT)), scale = scale_of_terms(vs[h]);
+                            st[rt].l = add_terms(st[rt].l, e0, e1);
+                            p[rt].set(4 * h + r, e0 * scale, e1 * scale);
+                        }
+                    }
+            }
+            u32 nans = 0;
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int x = 0; x < WORDS; x++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) nans |= nan_bytes(now.v[h][x][r]);
+            if (__any((nans & 0x80808080) != 0)) {
+                bool inside = false;  // of a token of the sequence, not of what lies behind its end
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int x = 0; x < WORDS; x++)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) {
+                            const u32 hit = nan_bytes(now.v[h][x][r]) & 0x80808080;
+                            inside |= hit && key0 + 16 * h + 4 * g + r <= keys.last;
+                            now.v[h][x][r] &= ~((hit >> 7) * 0xff);
+                        }
+                if (__any(inside)) {
+                    nan_from = min(nan_from, key0);
+                    nan_to = key0 + 31;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < WORDS; x++) {
+#pragma unroll
+                for (int h = 0; h < 2; h++) transpose4(now.v[h][x]);
+#pragma unroll
+                for (int b = 0; b < 4; b++) {
+                    const int j = 4 * x + b;
+                    if (j >= TILES) continue;
+                    const bf16x8 v = Wide<ENSI_T_BF16>::widen(now.v[0][x][b], now.v[1][x][b]);
+#pragma unroll
+                    for (int rt = 0; rt < RT; rt++) {
+                        st[rt].o[j] = Wide<ENSI_T_BF16>::mfma16(v, p[rt].hi.v, st[rt].o[j]);
+                        st[rt].o[j] = Wide<ENSI_T_BF16>::mfma16(v, p[rt].lo.v, st[rt].o[j]);
+                    }
+                }
+            }
+        }
+    }
+    for (int key = nan_from; key <= min(nan_to, keys.last); key++) {
+        // rare, and of this wave's tiles only
+        const int block = (key - keys.lo) / 32 % 4 == (tile0 + wave) % 4 ? block_of(a, seq, head, key) : -1;
+        if (block < 0) continue;
+        const unsigned char *v = a.kv.v + ((int64_t)block * KV_BLOCK + key % KV_BLOCK) * DIM;
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            if (!(seen_keys(part, a.window, lines[index[rt]], places[index[rt]], key) & 1)) continue;
+#pragma unroll
+            for (int j = 0; j < TILES; j++)
+#pragma unroll
+                for (int r = 0; r < 4; r++)
+                    if (is_nan(v[j < PIECE ? PIECE * (4 * g + r) + j : MAIN + REST * (4 * g + r) + j - PIECE])) st[rt].o[j][r] = __builtin_nanf("");
+        }
+    }
+    const bool whole = keys.tiles <= split_tiles;
+    __shared__ f32x4 part_o[2][TILES][64];
+    __shared__ float part_m[2][64], part_l[2][64];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        Rows16<DIM> &s = st[rt];
+        // a lane has the sum of its keys only
+        s.l += __shfl_xor(s.l, 16);
+        s.l += __shfl_xor(s.l, 32);
+        // waves 2 and 3 into 0 and 1, wave 1 into 0
+#pragma unroll
+        for (int half = 2; half >= 1; half /= 2) {
+            if (wave >= half && wave < 2 * half) {
+#pragma unroll
+                for (int j = 0; j < TILES; j++) part_o[wave - half][j][lane] = s.o[j];
+                part_m[wave - half][lane] = s.m;
+                part_l[wave - half][lane] = s.l;
+            }
+            __syncthreads();
+            if (wave < half) {
+                const float om = part_m[wave][lane], m = most_of(s.m, om), base = m == -__builtin_inff() ? 0.0f : m;
+                const float h0 = half_lift(s.m, base), h1 = half_lift(om, base);
+#pragma unroll
+                for (int j = 0; j < TILES; j++) {
+                    const f32x4 o = part_o[wave][j][lane];
+#pragma unroll
+                    for (int r = 0; r < 4; r++) s.o[j][r] = s.o[j][r] * h0 * h0 + o[r] * h1 * h1;
+                }
+                s.l = s.l * h0 * h0 + part_l[wave][lane] * h1 * h1;
+                s.m = m;
+            }
+            __syncthreads();
+        }
+        if (wave == 0 && row0 + 16 * rt + n < rows) {
+            const Last end = last_of<SCORE>(s.m, s.l, [&] { return whole && sees_any_of(a, seq, part, lines[index[rt]], places[index[rt]]); });
+            float *ws = a.ws + (((int64_t)seq * a.kv.heads + head) * a.row_tiles + row0 / 16 + rt) * a.splits * (16 * DIM + 32) + (int64_t)split * (16 * DIM + 32);
+            T *out = (T *)a.out + (int64_t)(part.first + index[rt]) * a.out_stride + (int64_t)(head * a.group + (row0 + 16 * rt + n) % a.group) * DIM;
+            const auto put = [&](int at, auto first, auto count) {  // registers r of tiles first .. first + count - 1, at place `at` of the row
+#pragma unroll
+                for (int r = 0; r < 4; r++)
+#pragma unroll
+                    for (int j = 0; j < decltype(count)::value; j++) {
+                        const float v = s.o[decltype(first)::value + j][r];
+                        const int d = at + decltype(count)::value * (4 * g + r) + j;
+                        if (whole) out[d] = (T)end(v);
+                        else ws[n * DIM + d] = v;
+                    }
+            };
+            put(0, std::integral_constant<int, 0>(), std::integral_constant<int, PIECE>());
+            if constexpr (REST > 0) put(MAIN, std::integral_constant<int, PIECE>(), std::integral_constant<int, REST>());
+            if (!whole && g == 0) {
+                ws[16 * DIM + n] = s.m;
+                ws[16 * DIM + 16 + n] = s.l;
+            }
+        }
+    }
+}
+
+// Joins the parts of a row: a workgroup to a row.  The references first, a thread to a part, then the outputs: DIM / 4 threads to a part, as many
+// parts side by side as there are threads, added in LDS.
+template <int TYPE, int DIM, int SCORE>
+__global__ __launch_bounds__(256) void k_clear_attention_tree_join(AttentionView a, const int32_t *parents, int split_tiles) {
+    typedef typename Elem<TYPE>::type T;
+    constexpr int QUADS = DIM / 4, SLICES = 256 / QUADS;
+    const int seq = blockIdx.z, head = blockIdx.x / a.row_tiles, tile = blockIdx.x % a.row_tiles, n = blockIdx.y, t = threadIdx.x, row = 16 * tile + n;
+    const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
+    const TreeKeys keys = tree_keys(part, a.window);
+    if (row >= part.count * a.group || keys.tiles <= split_tiles) return;
+    const Tree tree = tree_of(parents, part, a.kv.status);
+    if (!tree.good) return;
+    const int splits = (keys.tiles + split_tiles - 1) / split_tiles, index = row / a.group;
+    const float *ws = a.ws + ((int64_t)seq * gridDim.x + blockIdx.x) * a.splits * (16 * DIM + 32);
+    __shared__ float factor[JOIN_MAX], top[4], sums[4];
+    __shared__ f32x4 parts[SLICES][QUADS];
+    const int quad = t % QUADS, slice = t / QUADS;
+    float m = -__builtin_inff(), l = 0;
+    if (t < splits) {
+        m = ws[(int64_t)t * (16 * DIM + 32) + 16 * DIM + n];
+        l = ws[(int64_t)t * (16 * DIM + 32) + 16 * DIM + 16 + n];
+    }
+    float most = m;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
+    if (t % 64 == 0) top[t / 64] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    if (most == -__builtin_inff()) most = 0;
+    const float h = half_lift(m, most);
+    if (t < splits) factor[t] = h;
+    l = t < splits ? l * h * h : 0;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) l += __shfl_xor(l, k);
+    if (t % 64 == 0) sums[t / 64] = l;
+    __syncthreads();
+    f32x4 o = {0, 0, 0, 0};
+    if (slice < SLICES) {
+#pragma unroll 4
+        for (int s = slice; s < splits; s += SLICES) {
+            const f32x4 v = *(const f32x4 *)(ws + (int64_t)s * (16 * DIM + 32) + n * DIM + 4 * quad);
+            const float f = factor[s];
+#pragma unroll
+            for (int i = 0; i < 4; i++) o[i] = __builtin_fmaf(v[i] * f, f, o[i]);
+        }
+        parts[slice][quad] = o;
+    }
+    const u32 lo = __shfl((u32)tree.line, index), hi = __shfl((u32)(tree.line >> 32), index);
+    const int depth = __shfl(tree.depth, index);
+    __syncthreads();
+    if (t >= QUADS) return;
+    l = sums[0] + sums[1] + sums[2] + sums[3];
+    o = (f32x4){0, 0, 0, 0};
+    for (int s = 0; s < SLICES; s++) o += parts[s][t];
+    const int token = part.first + index, q_head = head * a.group + row % a.group;
+    const Last end = last_of<SCORE>(most, l, [&] { return sees_any_of(a, seq, part, near_line((u64)hi << 32 | lo, a.window), part.ctx + depth); });
+    typedef T quad_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    quad_t w;
+#pragma unroll
+    for (int i = 0; i < 4; i++) w[i] = (T)end(o[i]);
+    *(quad_t *)((T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM + 4 * t) = w;
+}
+
+template <int TYPE, int DIM, int SCORE>
+static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipStream_t st) {
+    const int heads = v.kv.heads;
+    const int span = v.window > 0 ? (int)min((int64_t)v.max_length, (int64_t)v.window + v.s.max_new - 1 + 31) : v.max_length;
+    v.row_tiles = (v.s.max_new * v.group + 15) / 16;
+    const int tiles = (span + 31) / 32;
+    const int rt = v.row_tiles == 1 ? 1 : v.row_tiles == 2 || DIM > 128 ? 2 : 4;
+    const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + rt - 1) / rt);
+    int splits = max((tiles + 31) / 32, base < 256 && tiles > 16 ? (int)(512 / base) : 1);
+    splits = min(splits, min((tiles + 3) / 4, JOIN_MAX));
+    splits = max(splits, 1);
+    const int64_t room = (int64_t)CLEAR_WS_FLOATS / ((int64_t)v.s.seqs * heads * v.row_tiles * (16 * DIM + 32));
+    if (splits > room) splits = (int)max((int64_t)1, room);
+    int split_tiles = (tiles + splits - 1) / splits;
+    split_tiles = max((split_tiles + 3) & ~3, 4);  // a tile for every wave
+    splits = max((tiles + split_tiles - 1) / split_tiles, 1);
+    v.splits = splits;
+    {
+        ScopedTimer timer(ctx, "k_clear_attention_tree", st);
+        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(heads * ((v.row_tiles + rt - 1) / rt), splits, v.s.seqs), dim3(256), 0, st, v, parents, split_tiles); };
+        if (rt == 1) go(k_clear_attention_tree<TYPE, DIM, SCORE, 1>);
+        else if (rt == 2) go(k_clear_attention_tree<TYPE, DIM, SCORE, 2>);
+        else if constexpr (DIM <= 128) go(k_clear_attention_tree<TYPE, DIM, SCORE, 4>);
+    }
+    if (splits == 1) return;
+    ScopedTimer timer(ctx, "k_clear_attention_tree_join", st);
+    const int rows = min(16, v.s.max_new * v.group);
+    hipLaunchKernelGGL((k_clear_attention_tree_join<TYPE, DIM, SCORE>), dim3(heads * v.row_tiles, rows, v.s.seqs), dim3(256), 0, st, v, parents, split_tiles);
+}
+
+template <int TYPE, int SCORE>
+static void tree_dim(ensi_ctx *ctx, const AttentionView &v, const int32_t *parents, hipStream_t st) {
+    switch (v.kv.dim) {
+    case 64: return tree_go<TYPE, 64, SCORE>(ctx, v, parents, st);
+    case 96: return tree_go<TYPE, 96, SCORE>(ctx, v, parents, st);
+    case 128: return tree_go<TYPE, 128, SCORE>(ctx, v, parents, st);
+    case 192: return tree_go<TYPE, 192, SCORE>(ctx, v, parents, st);
+    default: return tree_go<TYPE, 256, SCORE>(ctx, v, parents, st);
+    }
+}
+
+void launch_clear_attention_tree(ensi_ctx *ctx, const KvView &kv, const ensi_clear_attention_args &a, const int32_t *parents, hipStream_t st) {
+    const AttentionView v = attention_view(ctx, kv, a);
+    if (a.type == ENSI_T_BF16) {
+        if (a.score == ENSI_SCORE_SOFTMAX) return tree_dim<ENSI_T_BF16, ENSI_SCORE_SOFTMAX>(ctx, v, parents, st);
+        return tree_dim<ENSI_T_BF16, ENSI_SCORE_SIGMOID>(ctx, v, parents, st);
+    }
+    if (a.score == ENSI_SCORE_SOFTMAX) return tree_dim<ENSI_T_F16, ENSI_SCORE_SOFTMAX>(ctx, v, parents, st);
+    tree_dim<ENSI_T_F16, ENSI_SCORE_SIGMOID>(ctx, v, parents, st);
+}
