@@ -28,23 +28,46 @@ struct SampleLds {
     u64 sum[SAMPLE_BINS];  // of the bins, of the segments of a row, or the candidates' weights
     u32 count[SAMPLE_BINS];
     u64 list[SAMPLE_LIST];  // bits of the value in their order, and inverted index: the order of the filters is the falling one of these
-    u64 part[2 * SAMPLE_WAVES];
+    u64 part[SAMPLE_WAVES];
     u32 low[SAMPLE_WAVES], high[SAMPLE_WAVES];
-    int found, listed;
+    int found, listed, few;
     u64 found_before;
+    u64 order[64], load[64];  // of the elements of one bin, for a wave to put in order
 };
 
 // What the workgroups of a row leave for each other, in the workspace
-struct SamplePart {
-    u64 bins[SAMPLE_BINS];
-    u64 list[SAMPLE_LIST];
-    int listed, first;
-    float most;
-    int pad;
-};
 struct SampleShared {
-    u64 sum[SAMPLE_SEGMENTS];
+    u64 bins[SAMPLE_BINS], sum[SAMPLE_SEGMENTS], list[SAMPLE_LIST];
+    float most[SAMPLE_PARTS];
+    int first[SAMPLE_PARTS];
+    int listed, pad;
 };
+
+// Values of other lanes, within a row of 16 and from the rows before: a scan takes 6 of them, a twentieth of what it takes through LDS.  Lanes without a source get `none`.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ u32 from_lane(u32 none, u32 v) {
+    return (u32)__builtin_amdgcn_update_dpp((int)none, (int)v, CONTROL, ROWS, 0xf, false);
+}
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ u64 from_lane(u64 none, u64 v) {
+    return (u64)from_lane<CONTROL, ROWS>((u32)(none >> 32), (u32)(v >> 32)) << 32 | from_lane<CONTROL, ROWS>((u32)none, (u32)v);
+}
+// Inclusive, over a wave of which all lanes are here; `none` is what changes nothing
+template <class V, class OP>
+__device__ __forceinline__ V wave_scan(V v, V none, const OP &op) {
+    v = op(v, from_lane<0x111, 0xf>(none, v));  // one lane up, then two, four and eight
+    v = op(v, from_lane<0x112, 0xf>(none, v));
+    v = op(v, from_lane<0x114, 0xf>(none, v));
+    v = op(v, from_lane<0x118, 0xf>(none, v));
+    v = op(v, from_lane<0x142, 0xa>(none, v));  // the last lane of rows 0 and 2 into rows 1 and 3
+    v = op(v, from_lane<0x143, 0xc>(none, v));  // and that of row 1 into rows 2 and 3
+    return v;
+}
+__device__ __forceinline__ u64 wave_scan(u64 v) {
+    return wave_scan(v, (u64)0, [](u64 a, u64 b) { return a + b; });
+}
+__device__ __forceinline__ u64 wave_last(u64 v) { return (u64)(u32)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (u32)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ u64 wave_sum(u64 v) { return wave_last(wave_scan(v)); }
 
 // Numbers in their order as unsigned ones; both zeros are one
 __device__ __forceinline__ u32 key_of(float x) {
@@ -59,10 +82,17 @@ __device__ __forceinline__ u64 part_of(u64 w, float f, bool up) {
     const int e = (int)(b >> 23);
     const u64 m = e ? (b & 0x7fffff) | 0x800000 : b & 0x7fffff;
     const int shift = 150 - max(e, 1);  // f = m 2^-shift, 24 to 149
-    const unsigned __int128 p = (unsigned __int128)w * m;
-    if (shift >= 128) return up && p ? 1 : 0;
-    const u64 whole = (u64)(p >> shift);
-    return up && (p & (((unsigned __int128)1 << shift) - 1)) ? whole + 1 : whole;
+    const u64 low = w * m, high = __umul64hi(w, m);
+    u64 whole, rest;  // of (high, low) 2^-shift, and what is left
+    if (shift < 64) {
+        whole = high << (64 - shift) | low >> shift;
+        rest = low << (64 - shift);
+    } else {
+        const int s = min(shift - 64, 63);  // (high is below 2^24)
+        whole = high >> s;
+        rest = low | (high & (((u64)1 << s) - 1));
+    }
+    return whole + (up && rest ? 1 : 0);
 }
 // The running sum at which top_p's part ends, and the one that the random number exceeds by less than a token
 __device__ __forceinline__ u64 part_target(u64 sum, float p) { return p > 0 ? max(part_of(sum, p, true), (u64)1) : 1; }
@@ -70,7 +100,10 @@ __device__ __forceinline__ u64 draw_target(u64 sum, float u) { return !(u > 0) ?
 
 enum SampleMode { SAMPLE_NONE, SAMPLE_FIRST, SAMPLE_TOP, SAMPLE_PART, SAMPLE_ALL, SAMPLE_SLOW };
 
-template <int TYPE>
+__device__ __forceinline__ u32 larger(u32 a, u32 b) { return __builtin_bit_cast(u32, __builtin_elementwise_maximum(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b))); }
+
+// HELD: a row of up to 64 tiles stays in registers, four tiles to a wave
+template <int TYPE, bool HELD>
 struct SampleRow {
     typedef typename Elem<TYPE>::type T;
     static constexpr int E = TYPE == ENSI_T_F32 ? 4 : 8, TILE = 64 * E, AHEAD = 4;  // elements of a lane and of a wave; tiles under way
@@ -89,6 +122,7 @@ struct SampleRow {
     // kept so far: values above `edge`, and of the equal ones those up to index `last`
     float edge, small;     // small: the smallest value that min_p leaves
     int last;
+    vec held[HELD ? AHEAD : 1];
 
     __device__ SampleRow(const ensi_clear_sample_args &a, int64_t row, SampleLds &l) : lds(l) {
         x = (const T *)a.logits + row * a.stride;
@@ -102,6 +136,9 @@ struct SampleRow {
         m = a.min_p ? a.min_p[row] : a.all_min_p;
         k = a.top_k ? a.top_k[row] : a.all_top_k;
         u = a.uniform[row];
+        if (HELD)
+#pragma unroll
+            for (int i = 0; i < AHEAD; i++) held[HELD ? i : 0] = fetch(wave + SAMPLE_WAVES * i);
     }
     // With the row's largest value (NaN where it has one): what is to be done, and the constants for it
     __device__ __forceinline__ SampleMode begin(float most) {
@@ -114,7 +151,7 @@ struct SampleRow {
         const int bits = 32 - __clz(vocab);
         shift = min(50, 62 - bits);
         rate = 512 / LN2 / (double)t;
-        bins = (float)fmin(SAMPLE_BINS / (LN2 * (shift + 2)) / (double)t, 3e38);
+        bins = fminf((float)rate * (SAMPLE_BINS / 512) / (float)(shift + 2), 3e38f);  // 2^-(S + 2) after the last
         if (m > 0) {
             // min_p keeps values from some place on: found by all lanes, a 64th of what is left at a time
             const double least = 512 * log2((double)fminf(m, 1.0f));
@@ -136,16 +173,18 @@ struct SampleRow {
         if (threadIdx.x < 512) lds.roots[threadIdx.x] = exp2(threadIdx.x / 512.0);
     }
 
-    __device__ __forceinline__ void load(float (&f)[E], int tile) const {
+    // A lane's part of a tile, -inf behind the row's end
+    __device__ __forceinline__ vec fetch(int tile) const {
         const int at = tile * TILE + lane * E;
-        if (at + E <= vocab) {
-            const vec v = *(const vec *)(x + at);
+        if (at + E <= vocab) return *(const vec *)(x + at);
+        vec v;
 #pragma unroll
-            for (int i = 0; i < E; i++) f[i] = (float)v[i];
-        } else {
+        for (int i = 0; i < E; i++) v[i] = at + i < vocab ? x[at + i] : (T)-__builtin_inff();
+        return v;
+    }
+    static __device__ __forceinline__ void widen(float (&f)[E], const vec &v) {
 #pragma unroll
-            for (int i = 0; i < E; i++) f[i] = at + i < vocab ? (float)x[at + i] : -__builtin_inff();
-        }
+        for (int i = 0; i < E; i++) f[i] = (float)v[i];
     }
     // todo(values, index of the first) for the tiles that `step` apart follow `first`, up to `end`: little work, AHEAD whole tiles at a time ...
     template <class TODO>
@@ -159,39 +198,44 @@ struct SampleRow {
 #pragma unroll
             for (int a = 0; a < AHEAD; a++) {
                 float f[E];
-#pragma unroll
-                for (int i = 0; i < E; i++) f[i] = (float)v[a][i];
+                widen(f, v[a]);
                 todo(f, (tile + a * step) * TILE + lane * E);
             }
         }
-        for (; tile < end; tile += step) {
-            float f[E];
-            load(f, tile);
-            todo(f, tile * TILE + lane * E);
-        }
+        walk_slowly(tile, end, step, todo);
     }
     // ... or much: the next tile is under way while one is worked on
     template <class TODO>
     __device__ __forceinline__ void walk_slowly(int first, int end, int step, const TODO &todo) const {
-        const int whole = min(end, vocab / TILE);
-        int tile = first;
-        if (tile < whole) {
-            vec now = *(const vec *)(x + tile * TILE + lane * E);
-            for (; tile < whole; tile += step) {
-                vec next = now;
-                if (tile + step < whole) next = *(const vec *)(x + (tile + step) * TILE + lane * E);
-                float f[E];
-#pragma unroll
-                for (int i = 0; i < E; i++) f[i] = (float)now[i];
-                todo(f, tile * TILE + lane * E);
-                now = next;
-            }
-        }
-        for (; tile < end; tile += step) {
+        if (first >= end) return;
+        vec now = fetch(first);
+        for (int tile = first; tile < end; tile += step) {
+            vec next = now;
+            if (tile + step < end) next = fetch(tile + step);
             float f[E];
-            load(f, tile);
+            widen(f, now);
             todo(f, tile * TILE + lane * E);
+            now = next;
         }
+    }
+    // Of a part, all waves
+    template <class TODO>
+    __device__ __forceinline__ void walk_part(int first, int end, const TODO &todo) const {
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; i++)
+                if (wave + SAMPLE_WAVES * i < tiles) {
+                    float f[E];
+                    widen(f, held[i]);
+                    todo(f, (wave + SAMPLE_WAVES * i) * TILE + lane * E);
+                }
+        } else
+            walk(first + wave, end, SAMPLE_WAVES, todo);
+    }
+    template <class TODO>
+    __device__ __forceinline__ void walk_part_slowly(int first, int end, const TODO &todo) const {
+        if constexpr (HELD) walk_part(first, end, todo);
+        else walk_slowly(first + wave, end, SAMPLE_WAVES, todo);
     }
     __device__ __forceinline__ bool kept(float f, int index) const { return (f > edge) | ((f == edge) & (index <= last)); }
     __device__ __forceinline__ double place(float f) const { return ((double)f - (double)top) * rate; }
@@ -231,8 +275,7 @@ struct SampleRow {
 
     // ---- over the workgroup
     __device__ __forceinline__ u64 total(u64 v) const {
-#pragma unroll
-        for (int k = 1; k < 64; k *= 2) v += (u64)__shfl_xor((unsigned long long)v, k);
+        v = wave_sum(v);
         __syncthreads();
         if (lane == 0) lds.part[wave] = v;
         __syncthreads();
@@ -242,40 +285,44 @@ struct SampleRow {
         return sum;
     }
     template <class OP>
-    __device__ __forceinline__ u32 reduce(u32 v, u32 (&each)[SAMPLE_WAVES], const OP &op) const {  // (a barrier before `each` is written again is the caller's)
-#pragma unroll
-        for (int k = 1; k < 64; k *= 2) v = op(v, (u32)__shfl_xor(v, k));
+    __device__ __forceinline__ u32 reduce(u32 v, u32 none, u32 (&each)[SAMPLE_WAVES], const OP &op) const {  // (a barrier before `each` is written again is the caller's)
+        v = (u32)__builtin_amdgcn_readlane((int)wave_scan(v, none, op), 63);
         if (lane == 0) each[wave] = v;
         __syncthreads();
+#pragma unroll
         for (int w = 0; w < SAMPLE_WAVES; w++) v = op(v, each[w]);
         return v;
     }
-    __device__ __forceinline__ u64 scan(u64 v) const {  // inclusive, over the wave
-#pragma unroll
-        for (int k = 1; k < 64; k *= 2) {
-            const u64 o = (u64)__shfl_up((unsigned long long)v, k);
-            if (lane >= k) v += o;
-        }
-        return v;
-    }
-    // The first of lds.sum[0 .. n) (or of lds.count, by COUNTS) at which the running sum reaches `target` >= 1: into lds.found, with the sum before it; n if none does.  Two to a thread
-    template <bool COUNTS>
-    __device__ __forceinline__ void find(int n, u64 target) const {
+    // The first of lds.sum[0 .. n) (or of lds.count, by COUNTS) at which the running sum reaches target(the whole sum) >= 1: into lds.found, with the sum before it; n if none does.
+    // Two to a thread; returns that target
+    template <bool COUNTS, class TARGET>
+    __device__ __forceinline__ u64 find(int n, const TARGET &target_of) const {
         __syncthreads();
         const int at = 2 * threadIdx.x;
         const u64 v0 = at < n ? (COUNTS ? (u64)lds.count[at] : lds.sum[at]) : 0, v1 = at + 1 < n ? (COUNTS ? (u64)lds.count[at + 1] : lds.sum[at + 1]) : 0;
-        const u64 s = scan(v0 + v1);
-        if (lane == 63) lds.part[SAMPLE_WAVES + wave] = s;
+        const u64 s = wave_scan(v0 + v1);
+        if (lane == 63) lds.part[wave] = s;
         if (threadIdx.x == 0) lds.found = n;
         __syncthreads();
-        u64 before = s - v0 - v1;
-        for (int w = 0; w < wave; w++) before += lds.part[SAMPLE_WAVES + w];
+        u64 before = s - v0 - v1, sum = 0;
+#pragma unroll
+        for (int w = 0; w < SAMPLE_WAVES; w++) {
+            const u64 one = lds.part[w];
+            sum += one;
+            before += w < wave ? one : 0;
+        }
+        const u64 target = target_of(sum);
         if (before < target && before + v0 + v1 >= target) {  // (of one thread)
             const bool second = before + v0 < target;
             lds.found = at + second;
             lds.found_before = before + (second ? v0 : 0);
         }
         __syncthreads();
+        return target;
+    }
+    template <bool COUNTS>
+    __device__ __forceinline__ void find_at(int n, u64 target) const {
+        find<COUNTS>(n, [=](u64) { return target; });
     }
     __device__ __forceinline__ void clear_bins() const {
         __syncthreads();
@@ -299,7 +346,7 @@ struct SampleRow {
                     if (!COUNTS) atomicAdd((unsigned long long *)&lds.sum[b], (unsigned long long)weight());
                 }
             });
-            find<COUNTS>(SAMPLE_BINS, target);
+            find_at<COUNTS>(SAMPLE_BINS, target);
             const u32 b = lds.found, first = high - (b << step);
             target -= lds.found_before;
             ties = (int)lds.count[b];
@@ -312,7 +359,7 @@ struct SampleRow {
     // ---- in the tiles from `first` to `end`
     __device__ __forceinline__ float largest(int first, int end) const {  // of a thread; NaN where it has one
         float most = -__builtin_inff();
-        walk(first + wave, end, SAMPLE_WAVES, [&](const float (&f)[E], int) {
+        walk_part(first, end, [&](const float (&f)[E], int) {
 #pragma unroll
             for (int i = 0; i < E; i++) most = __builtin_elementwise_maximum(most, f[i]);
         });
@@ -320,16 +367,16 @@ struct SampleRow {
     }
     __device__ __forceinline__ int first_largest(int first, int end) const {
         int index = INT32_MAX;
-        walk(first + wave, end, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
+        walk_part(first, end, [&](const float (&f)[E], int at) {
 #pragma unroll
             for (int i = 0; i < E; i++)
                 if (f[i] == top) index = min(index, at + i);
         });
-        return (int)reduce((u32)index, lds.high, [](u32 a, u32 b) { return min(a, b); });
+        return (int)reduce((u32)index, ~0u, lds.high, [](u32 a, u32 b) { return min(a, b); });
     }
     __device__ __forceinline__ void count_bins(int first, int end) const {
         clear_bins();
-        walk(first + wave, end, SAMPLE_WAVES, [&](const float (&f)[E], int) {
+        walk_part(first, end, [&](const float (&f)[E], int) {
 #pragma unroll
             for (int i = 0; i < E; i++) {
                 const int b = bin(f[i]);
@@ -340,7 +387,7 @@ struct SampleRow {
     }
     __device__ __forceinline__ void sum_bins(int first, int end) const {
         clear_bins();
-        walk_slowly(first + wave, end, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
+        walk_part_slowly(first, end, [&](const float (&f)[E], int at) {
             u64 w[E];
             bool in[E];
 #pragma unroll
@@ -354,13 +401,16 @@ struct SampleRow {
         });
         __syncthreads();
     }
-    // Puts what `in` holds for into the list
-    template <class IN>
-    __device__ __forceinline__ void gather(int first, int end, const IN &in) const {
-        walk(first + wave, end, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
+    // Puts the values of the bins from `low` to `high` into the list
+    __device__ __forceinline__ void gather(int first, int end, int low, int high) const {
+        walk_part(first, end, [&](const float (&f)[E], int at) {
+            float most = f[0];
+#pragma unroll
+            for (int i = 1; i < E; i++) most = fmaxf(most, f[i]);
+            if (bin(most) > high) return;
 #pragma unroll
             for (int i = 0; i < E; i++)
-                if (in(f[i])) {
+                if (bin(f[i]) >= low && bin(f[i]) <= high) {
                     const int n = atomicAdd(&lds.listed, 1);
                     if (n < SAMPLE_LIST) lds.list[n] = (u64)key_of(f[i]) << 32 | ~(u32)(at + i);
                 }
@@ -370,39 +420,49 @@ struct SampleRow {
     // Weights of what `in` holds for, summed over each segment
     template <class IN>
     __device__ __forceinline__ void sums(int first_segment, int end_segment, u64 *into, const IN &in) const {
-        for (int segment = first_segment + wave; segment < end_segment; segment += SAMPLE_WAVES) {
-            u64 s = 0;
-            walk_slowly(segment * per, min((segment + 1) * per, tiles), 1, [&](const float (&f)[E], int at) {
-                u64 w[E];
-                bool is[E], any = false;
+        u64 s = 0;
+        const auto add = [&](const float (&f)[E], int at) {
+            u64 w[E];
+            bool is[E], any = false;
 #pragma unroll
-                for (int i = 0; i < E; i++) any |= is[i] = in(f[i], at + i);
-                if (!__any(any)) return;
-                weights<E>(w, f, is);
+            for (int i = 0; i < E; i++) any |= is[i] = in(f[i], at + i);
+            if (!__any(any)) return;
+            weights<E>(w, f, is);
 #pragma unroll
-                for (int i = 0; i < E; i++) s += w[i];
-                s -= E * NO_WEIGHT;
+            for (int i = 0; i < E; i++) s += w[i];
+            s -= E * NO_WEIGHT;
+        };
+        if constexpr (HELD) {  // (a segment is a tile)
+            walk_part(0, tiles, [&](const float (&f)[E], int at) {
+                s = 0;
+                add(f, at);
+                s = wave_sum(s);
+                if (lane == 0) into[at / TILE] = s;
             });
-#pragma unroll
-            for (int k = 1; k < 64; k *= 2) s += (u64)__shfl_xor((unsigned long long)s, k);
-            if (lane == 0) into[segment] = s;
-        }
+        } else
+            for (int segment = first_segment + wave; segment < end_segment; segment += SAMPLE_WAVES) {
+                s = 0;
+                walk_slowly(segment * per, min((segment + 1) * per, tiles), 1, add);
+                s = wave_sum(s);
+                if (lane == 0) into[segment] = s;
+            }
     }
-    // The first index at which the running sum of `of`, whose sums over segments are in lds.sum, reaches `target` >= 1, which it does
-    template <class OF>
-    __device__ __forceinline__ int pick(const OF &of, u64 target) const {
-        find<false>((tiles + per - 1) / per, target);
+    // The first index at which the running sum of of(weights, values, index of the first), whose sums over segments are in lds.sum, reaches target(the whole sum) >= 1
+    template <class OF, class TARGET>
+    __device__ __forceinline__ int pick(const OF &of, const TARGET &target_of) const {
+        const u64 target = find<false>((tiles + per - 1) / per, target_of);
         const int segment = lds.found;
         u64 before = lds.found_before;
         __syncthreads();
         if (wave == 0) {
             for (int tile = segment * per; tile < min((segment + 1) * per, tiles); tile++) {
                 float f[E];
-                load(f, tile);
+                widen(f, fetch(tile));
                 u64 w[E], mine = 0;
+                of(w, f, tile * TILE + lane * E);
 #pragma unroll
-                for (int i = 0; i < E; i++) mine += w[i] = of(f[i], tile * TILE + lane * E + i);
-                const u64 s = scan(mine), reached = __ballot(before + s >= target);
+                for (int i = 0; i < E; i++) mine += w[i];
+                const u64 s = wave_scan(mine), reached = __ballot(before + s >= target);
                 if (reached) {
                     if (lane == __ffsll((unsigned long long)reached) - 1) {
                         u64 run = before + s - mine;
@@ -416,7 +476,7 @@ struct SampleRow {
                     }
                     break;
                 }
-                before += (u64)__shfl((unsigned long long)s, 63);
+                before += wave_last(s);
             }
         }
         __syncthreads();
@@ -424,11 +484,16 @@ struct SampleRow {
     }
     // The token, once the bound is known and the sums of the segments are in lds.sum
     __device__ __forceinline__ int draw() const {
-        __syncthreads();
-        u64 sum = 0;
-        for (int i = threadIdx.x; i * per < tiles; i += SAMPLE_THREADS) sum += lds.sum[i];
-        sum = total(sum);
-        return pick([&](float f, int at) { return kept(f, at) ? weight(f) : (u64)0; }, draw_target(sum, u) + 1);
+        return pick(
+            [&](u64(&w)[E], const float (&f)[E], int at) {
+                bool is[E];
+#pragma unroll
+                for (int i = 0; i < E; i++) is[i] = kept(f[i], at + i);
+                weights<E>(w, f, is);
+#pragma unroll
+                for (int i = 0; i < E; i++) w[i] -= NO_WEIGHT;
+            },
+            [&](u64 sum) { return draw_target(sum, u) + 1; });
     }
     // min_p leaves the front part of what is kept
     __device__ __forceinline__ void keep_small() {
@@ -441,7 +506,7 @@ struct SampleRow {
     template <bool COUNTS>
     __device__ __forceinline__ void bound(u64 target) {
         const auto each = [&](const auto &todo) {
-            walk(wave, tiles, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
+            walk_part(0, tiles, [&](const float (&f)[E], int at) {
 #pragma unroll 1
                 for (int i = 0; i < E; i++) {
                     float v = f[0];
@@ -453,13 +518,13 @@ struct SampleRow {
         };
         if (COUNTS) count_bins(0, tiles);  // (nothing is cut before)
         else sum_bins(0, tiles);
-        find<COUNTS>(SAMPLE_BINS, target);
+        find_at<COUNTS>(SAMPLE_BINS, target);
         const int border = lds.found;
         if (border == SAMPLE_BINS) return;
         target -= lds.found_before;
         // the values in that bin
         u32 low = ~0u, high = 0;
-        walk(wave, tiles, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
+        walk_part(0, tiles, [&](const float (&f)[E], int at) {
 #pragma unroll
             for (int i = 0; i < E; i++)
                 if (bin(f[i]) == border && kept(f[i], at + i)) {
@@ -467,8 +532,8 @@ struct SampleRow {
                     high = max(high, key_of(f[i]));
                 }
         });
-        low = reduce(low, lds.low, [](u32 a, u32 b) { return min(a, b); });
-        high = reduce(high, lds.high, [](u32 a, u32 b) { return max(a, b); });
+        low = reduce(low, ~0u, lds.low, [](u32 a, u32 b) { return min(a, b); });
+        high = reduce(high, 0, lds.high, [](u32 a, u32 b) { return max(a, b); });
         int ties;
         const float at = of_key(select<COUNTS>(low, high, target, ties, each));
         if (edge != at) last = INT32_MAX;  // (equal ones may have been cut before)
@@ -491,14 +556,19 @@ struct SampleRow {
             for (int k = 1; k < 64; k *= 2) n += __shfl_xor(n, k);
             if (lane == 0) lds.sum[segment] = n;
         }
-        last = pick([&](float f, int) { return (u64)(f == at ? 1 : 0); }, needed);
+        last = pick(
+            [&](u64(&w)[E], const float (&f)[E], int) {
+#pragma unroll
+                for (int i = 0; i < E; i++) w[i] = f[i] == at ? 1 : 0;
+            },
+            [=](u64) { return needed; });
     }
     __device__ __forceinline__ int slowly() {
         if (k) bound<true>(k);
         if (p < 1) {
             u64 sum = 0;
             if (k) {
-                walk_slowly(wave, tiles, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
+                walk_part_slowly(0, tiles, [&](const float (&f)[E], int at) {
                     u64 w[E];
                     bool is[E];
 #pragma unroll
@@ -518,6 +588,40 @@ struct SampleRow {
         sums(0, (tiles + per - 1) / per, lds.sum, [&](float f, int at) { return kept(f, at); });
         return draw();
     }
+    // The same in one step where the elements, each(todo) with todo(bin, order, weight), are spread over the bins: the order (a falling one) of the element at which the running sum reaches
+    // `target`; 0 where a bin has too many.  `wave` 0 puts the elements of the bin in order.
+    template <bool COUNTS, class EACH>
+    __device__ __forceinline__ u64 select_spread(u64 target, const EACH &each) const {
+        clear_bins();
+        if (threadIdx.x == 0) lds.few = 0;
+        each([&](int b, u64, const auto &weight) {
+            atomicAdd(&lds.count[b], 1u);
+            if (!COUNTS) atomicAdd((unsigned long long *)&lds.sum[b], (unsigned long long)weight());
+        });
+        find_at<COUNTS>(SAMPLE_BINS, target);
+        const int border = lds.found;
+        if (lds.count[border] > 64) return 0;
+        target -= lds.found_before;
+        each([&](int b, u64 order, const auto &weight) {
+            if (b == border) {
+                const int i = atomicAdd(&lds.few, 1);
+                lds.order[i] = order;
+                lds.load[i] = COUNTS ? 1 : weight();
+            }
+        });
+        __syncthreads();
+        if (wave == 0) {
+            const int n = lds.few;
+            const u64 mine = lane < n ? lds.order[lane] : 0, w = lane < n ? lds.load[lane] : 0;
+            u64 before = 0;
+            for (int i = 0; i < n; i++) before += lds.order[i] > mine ? lds.load[i] : 0;
+            if (before < target && before + w >= target) lds.found_before = mine;  // (of one lane: the orders differ)
+        }
+        __syncthreads();
+        const u64 order = lds.found_before;
+        __syncthreads();
+        return order;
+    }
     // ---- in the list of candidates
     template <class TODO>
     __device__ __forceinline__ void each_listed(const TODO &todo) const {
@@ -526,9 +630,18 @@ struct SampleRow {
             if (kept(of_key((u32)(e >> 32)), (int)~(u32)e)) todo((u32)(e >> 32), ~(u32)e);
         }
     }
-    // Moves the bound as above, to one among the candidates.
+    // Moves the bound as above, to one among the candidates, which are in the bins from `from` to `to`.
     template <bool COUNTS>
-    __device__ __forceinline__ void bound_listed(u64 target) {
+    __device__ __forceinline__ void bound_listed(u64 target, int from, int to) {
+        const float finer = (float)SAMPLE_BINS / (to + 1 - from);
+        const u64 spread = select_spread<COUNTS>(target, [&](const auto &todo) {
+            each_listed([&](u32 key, u32 i) { todo(max(0, min((int)(((top - of_key(key)) * bins - from) * finer), SAMPLE_BINS - 1)), (u64)key << 32 | ~i, [&] { return weight(of_key(key)); }); });
+        });
+        if (spread) {
+            edge = of_key((u32)(spread >> 32));
+            last = (int)~(u32)spread;
+            return;
+        }
         int ties;
         u32 low = ~0u, high = 0;
         each_listed([&](u32 key, u32) {
@@ -536,8 +649,8 @@ struct SampleRow {
             high = max(high, key);
         });
         __syncthreads();
-        low = reduce(low, lds.low, [](u32 a, u32 b) { return min(a, b); });
-        high = reduce(high, lds.high, [](u32 a, u32 b) { return max(a, b); });
+        low = reduce(low, ~0u, lds.low, [](u32 a, u32 b) { return min(a, b); });
+        high = reduce(high, 0, lds.high, [](u32 a, u32 b) { return max(a, b); });
         const u32 key = select<COUNTS>(low, high, target, ties, [&](const auto &todo) { each_listed([&](u32 key, u32) { todo(key, [&] { return weight(of_key(key)); }); }); });
         const float value = of_key(key);
         u64 needed = target;
@@ -555,65 +668,74 @@ struct SampleRow {
         edge = value;
         last = index;
     }
-    // The token of a row whose top k are among the candidates
-    __device__ __forceinline__ int finish_listed() {
-        const int n = lds.listed;
-        if (n <= SAMPLE_PAIRS) {
-            // four threads to a candidate: how many come before it and what they weigh
-            const int mine = threadIdx.x / 4, sub = threadIdx.x % 4;
-            const bool there = mine < n;
-            const u64 e = there ? lds.list[mine] : 0;
-            const float f = of_key((u32)(e >> 32));
-            u64 w = 0;
-            if (there) w = weight(f);
-            if (sub == 0) lds.sum[mine] = w;
-            __syncthreads();
-            int rank = 0;
-            u64 before = 0;
-            for (int i = sub; i < n; i += 4) {
-                const bool ahead = lds.list[i] > e;
-                rank += ahead;
-                before += ahead ? lds.sum[i] : 0;
-            }
-#pragma unroll
-            for (int s = 1; s < 4; s *= 2) {
-                rank += __shfl_xor(rank, s);
-                before += (u64)__shfl_xor((unsigned long long)before, s);
-            }
-            bool in = there && rank < k;
-            if (p < 1) {
-                const u64 target = part_target(total(sub == 0 && in ? w : 0), p);
-                in = in && before < target;
-            }
-            in = in && f >= small;
-            if (!in) w = 0;
-            __syncthreads();
-            if (sub == 0) lds.sum[mine] = w;
-            if (threadIdx.x == 0) lds.found = 0;
-            const u64 at = draw_target(total(sub == 0 ? w : 0), u);
-            before = 0;
-            for (int i = sub; i < n; i += 4) before += (u32)lds.list[i] > (u32)e ? lds.sum[i] : 0;  // (indices are inverted)
-#pragma unroll
-            for (int s = 1; s < 4; s *= 2) before += (u64)__shfl_xor((unsigned long long)before, s);
-            if (sub == 0 && before <= at && at < before + w) lds.found = (int)~(u32)e;
-            __syncthreads();
-            return lds.found;
+    // The token of a row whose top k are among few candidates, four threads to each; waves without one are done.  -1 in threads that do not have it.
+    __device__ __forceinline__ int finish_pairs(int n) const {
+        if (16 * wave >= n) return -1;
+        const int mine = threadIdx.x / 4, sub = threadIdx.x % 4;
+        const bool there = mine < n;
+        u64 *const w_of = lds.sum, *const run_of = lds.sum + SAMPLE_PAIRS, *const sorted_w = lds.sum + 2 * SAMPLE_PAIRS, *const sorted = lds.list + SAMPLE_PAIRS;
+        const auto quad = [](auto v) {  // sum over the four
+            v += from_lane<0xb1, 0xf>((decltype(v))0, v);
+            v += from_lane<0x4e, 0xf>((decltype(v))0, v);
+            return v;
+        };
+        const u64 e = there ? lds.list[mine] : 0;
+        u64 w = weight(of_key((u32)(e >> 32)));
+        if (sub == 0 && there) w_of[mine] = w;
+        __syncthreads();
+        // how many come before it, and what they weigh
+        u32 rank = 0;
+        u64 before = 0;
+        for (int i = sub; i < n; i += 4) {
+            const bool ahead = lds.list[i] > e;
+            rank += ahead;
+            before += ahead ? w_of[i] : 0;
         }
+        rank = quad(rank);
+        before = quad(before);
+        if (sub == 0 && there) {
+            sorted[rank] = e;
+            sorted_w[rank] = w;
+            run_of[rank] = before + w;
+        }
+        __syncthreads();
+        // how many the filters leave: each leaves the front ones
+        const int most = min(k, n);
+        const u64 target = p < 1 ? part_target(run_of[most - 1], p) : ~(u64)0;
+        int left = 0;
+        for (int at = 0; at < most; at += 64) {
+            const int i = at + lane;
+            const bool in = i < most && (i == 0 || run_of[max(i, 1) - 1] < target) && of_key((u32)(sorted[min(i, most - 1)] >> 32)) >= small;
+            left += __popcll(__ballot(in));
+        }
+        const u64 at = draw_target(run_of[left - 1], u);
+        before = 0;
+        for (int i = sub; i < left; i += 4) before += (u32)sorted[i] > (u32)e ? sorted_w[i] : 0;  // (indices are inverted)
+        before = quad(before);
+        return there && (int)rank < left && before <= at && at < before + w ? (int)~(u32)e : -1;
+    }
+    // The token of a row whose top k are among the candidates
+    __device__ __forceinline__ int finish_listed(int limit) {
+        const int n = lds.listed;
+        if (n <= SAMPLE_PAIRS) return finish_pairs(n);
         const auto sum = [&] {
             u64 s = 0;
             each_listed([&](u32 key, u32) { s += weight(of_key(key)); });
             return total(s);
         };
-        if (k < n) bound_listed<true>(k);
-        if (p < 1) bound_listed<false>(part_target(sum(), p));
+        if (k < n) bound_listed<true>(k, 0, limit);
+        if (p < 1) bound_listed<false>(part_target(sum(), p), 0, limit);
         keep_small();
         u64 target = draw_target(sum(), u) + 1;
+        const int shift_index = max(0, 21 - __clz(vocab - 1));  // 2048 bins of indices
+        const u64 spread = select_spread<false>(target, [&](const auto &todo) { each_listed([&](u32 key, u32 i) { todo((int)(i >> shift_index), ~(u64)i, [&] { return weight(of_key(key)); }); }); });
+        if (spread) return (int)~(u32)spread;
         int ties;
         return (int)~select<false>(~(u32)(vocab - 1), ~0u, target, ties, [&](const auto &todo) { each_listed([&](u32 key, u32 i) { todo(~i, [&] { return weight(of_key(key)); }); }); });
     }
     // The token of a row whose bound by top_p is among the candidates, where it leaves `rest` of the sum; the segments' sums of what is above are in lds.sum
-    __device__ __forceinline__ int finish_part(u64 rest, u64 *sums) {
-        bound_listed<false>(rest);  // (it works in lds.sum)
+    __device__ __forceinline__ int finish_part(u64 rest, int border, u64 *sums) {
+        bound_listed<false>(rest, border, border);  // (it works in lds.sum)
         keep_small();
         __syncthreads();
         for (int i = threadIdx.x; i * per < tiles; i += SAMPLE_THREADS) lds.sum[i] = sums[i];
@@ -624,16 +746,15 @@ struct SampleRow {
 };
 
 // A workgroup to a row
-template <int TYPE>
+template <int TYPE, bool HELD>
 __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample(ensi_clear_sample_args a) {
     __shared__ SampleLds lds;
     __shared__ u64 above[SAMPLE_SEGMENTS];
-    SampleRow<TYPE> r(a, blockIdx.x, lds);
+    SampleRow<TYPE, HELD> r(a, blockIdx.x, lds);
     r.set_roots();
     if (threadIdx.x == 0) lds.listed = 0;
     const float mine = r.largest(0, r.tiles);
-    const auto larger = [](u32 a, u32 b) { return __builtin_bit_cast(u32, __builtin_elementwise_maximum(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b))); };
-    SampleMode mode = r.begin(__builtin_bit_cast(float, r.reduce(__builtin_bit_cast(u32, mine), lds.low, larger)));
+    SampleMode mode = r.begin(__builtin_bit_cast(float, r.reduce(__builtin_bit_cast(u32, mine), __builtin_bit_cast(u32, -__builtin_inff()), lds.low, larger)));
     const int tiles = r.tiles, segments = (tiles + r.per - 1) / r.per;
     int token = -1;
     if (mode == SAMPLE_FIRST) token = r.first_largest(0, tiles);
@@ -646,27 +767,32 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample(ensi_clear_samp
                 if (b < SAMPLE_BINS) atomicAdd(&lds.count[b], 1u);
             } else
                 r.count_bins(0, tiles);
-            r.template find<true>(SAMPLE_BINS, r.k);
+            r.template find_at<true>(SAMPLE_BINS, r.k);
             limit = min(lds.found, limit);
         }
-        r.gather(0, tiles, [&](float f) { return r.bin(f) <= limit; });
-        if (lds.listed <= SAMPLE_LIST) token = r.finish_listed();
+        r.gather(0, tiles, 0, limit);
+        if (lds.listed <= SAMPLE_PAIRS) {
+            token = r.finish_pairs(lds.listed);
+            if (token >= 0) a.out[blockIdx.x] = token;
+            return;
+        }
+        if (lds.listed <= SAMPLE_LIST) token = r.finish_listed(limit);
         else mode = SAMPLE_SLOW;
     }
     if (mode == SAMPLE_PART) {
         r.sum_bins(0, tiles);
-        const u64 target = part_target(r.total(lds.sum[threadIdx.x] + lds.sum[threadIdx.x + SAMPLE_THREADS]), r.p);
-        r.template find<false>(SAMPLE_BINS, target);
+        const u64 target = r.template find<false>(SAMPLE_BINS, [&](u64 sum) { return part_target(sum, r.p); });
         const int border = lds.found;
         const u64 rest = target - lds.found_before;
-        r.gather(0, tiles, [&](float f) { return r.bin(f) == border; });
+        r.gather(0, tiles, border, border);
         if (lds.listed <= SAMPLE_LIST) {
             r.sums(0, segments, above, [&](float f, int) { return r.bin(f) < border && f >= r.small; });
-            token = r.finish_part(rest, above);
+            token = r.finish_part(rest, border, above);
         } else
             mode = SAMPLE_SLOW;
     }
     if (mode == SAMPLE_ALL) {
+        __syncthreads();
         r.sums(0, segments, lds.sum, [&](float f, int at) { return r.kept(f, at); });
         token = r.draw();
     }
@@ -674,10 +800,163 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample(ensi_clear_samp
     if (threadIdx.x == 0) a.out[blockIdx.x] = token;
 }
 
-void launch_clear_sample(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStream_t st) {
+// ---- Several workgroups to a row, for rows that are fewer than the CUs: the same in four launches, which leave in the workspace what the next one needs.  All sums are exact, so
+// the token is the same, and neither the order in which bins are added up nor that of the list matters.
+struct SampleParts {
+    ensi_clear_sample_args a;
+    SampleShared *row;
+    int parts;
+};
+// The segments and tiles of a part
+template <class ROW>
+struct SampleRange {
+    int segment0, segment1, tile0, tile1;
+    __device__ SampleRange(const ROW &r, int parts, int i) {
+        const int segments = (r.tiles + r.per - 1) / r.per, each = (segments + parts - 1) / parts;
+        segment0 = min(i * each, segments);
+        segment1 = min(segment0 + each, segments);
+        tile0 = segment0 * r.per;
+        tile1 = min(segment1 * r.per, r.tiles);
+    }
+};
+template <class ROW>
+__device__ __forceinline__ SampleMode begin_part(ROW &r, const SampleShared &row, int parts) {
+    static_assert(SAMPLE_PARTS == 8, "one of them to a lane of each eight");
+    const u32 most = __builtin_bit_cast(u32, row.most[min((int)threadIdx.x % 8, parts - 1)]);
+    return r.begin(__builtin_bit_cast(float, __builtin_amdgcn_readlane((int)wave_scan(most, __builtin_bit_cast(u32, -__builtin_inff()), larger), 63)));
+}
+// The bin with the bound into lds.found; what is left there of the target
+template <class ROW>
+__device__ __forceinline__ u64 find_part(const ROW &r, const SampleShared &row, SampleMode mode) {
+    const u64 b0 = row.bins[threadIdx.x], b1 = row.bins[threadIdx.x + SAMPLE_THREADS];
+    r.lds.sum[threadIdx.x] = b0;
+    r.lds.sum[threadIdx.x + SAMPLE_THREADS] = b1;
+    const u64 target = r.template find<false>(SAMPLE_BINS, [&](u64 sum) { return mode == SAMPLE_TOP ? (u64)r.k : part_target(sum, r.p); });
+    return target - r.lds.found_before;
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_most(SampleParts s) {
+    __shared__ SampleLds lds;
+    SampleShared &row = s.row[blockIdx.y];
+    const SampleRow<TYPE, false> r(s.a, blockIdx.y, lds);
+    const SampleRange<SampleRow<TYPE, false>> g(r, s.parts, blockIdx.x);
+    for (int i = blockIdx.x * SAMPLE_THREADS + threadIdx.x; i < SAMPLE_BINS; i += s.parts * SAMPLE_THREADS) row.bins[i] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) row.listed = 0;
+    const u32 most = r.reduce(__builtin_bit_cast(u32, r.largest(g.tile0, g.tile1)), __builtin_bit_cast(u32, -__builtin_inff()), lds.low, larger);
+    if (threadIdx.x == 0) row.most[blockIdx.x] = __builtin_bit_cast(float, most);
+}
+template <int TYPE>
+__global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_bins(SampleParts s) {
+    __shared__ SampleLds lds;
+    SampleShared &row = s.row[blockIdx.y];
+    SampleRow<TYPE, false> r(s.a, blockIdx.y, lds);
+    const SampleRange<SampleRow<TYPE, false>> g(r, s.parts, blockIdx.x);
+    const SampleMode mode = begin_part(r, row, s.parts);
+    if (mode == SAMPLE_FIRST) {
+        const int first = r.first_largest(g.tile0, g.tile1);
+        if (threadIdx.x == 0) row.first[blockIdx.x] = first;
+    } else if (mode == SAMPLE_TOP) {
+        r.count_bins(g.tile0, g.tile1);
+        for (int i = threadIdx.x; i < SAMPLE_BINS; i += SAMPLE_THREADS)
+            if (lds.count[i]) atomicAdd((unsigned long long *)&row.bins[i], (unsigned long long)lds.count[i]);
+    } else if (mode == SAMPLE_PART) {
+        r.set_roots();
+        r.sum_bins(g.tile0, g.tile1);
+        for (int i = threadIdx.x; i < SAMPLE_BINS; i += SAMPLE_THREADS)
+            if (lds.sum[i]) atomicAdd((unsigned long long *)&row.bins[i], (unsigned long long)lds.sum[i]);
+    } else if (mode == SAMPLE_ALL) {
+        r.set_roots();
+        __syncthreads();
+        r.sums(g.segment0, g.segment1, row.sum, [&](float f, int at) { return r.kept(f, at); });
+    }
+}
+template <int TYPE>
+__global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_gather(SampleParts s) {
+    __shared__ SampleLds lds;
+    __shared__ int at;
+    SampleShared &row = s.row[blockIdx.y];
+    SampleRow<TYPE, false> r(s.a, blockIdx.y, lds);
+    const SampleRange<SampleRow<TYPE, false>> g(r, s.parts, blockIdx.x);
+    const SampleMode mode = begin_part(r, row, s.parts);
+    if (mode != SAMPLE_TOP && mode != SAMPLE_PART) return;
+    if (threadIdx.x == 0) lds.listed = 0;
+    if (mode == SAMPLE_PART) r.set_roots();
+    find_part(r, row, mode);
+    const int border = lds.found;
+    r.gather(g.tile0, g.tile1, mode == SAMPLE_TOP ? 0 : border, min(border, SAMPLE_BINS - 1));
+    const int listed = lds.listed;
+    if (threadIdx.x == 0) at = atomicAdd(&row.listed, listed);  // (past the list's end where there are too many)
+    __syncthreads();
+    for (int i = threadIdx.x; i < min(listed, SAMPLE_LIST) && at + i < SAMPLE_LIST; i += SAMPLE_THREADS) row.list[at + i] = lds.list[i];
+    if (mode == SAMPLE_PART) r.sums(g.segment0, g.segment1, row.sum, [&](float f, int) { return r.bin(f) < border && f >= r.small; });
+}
+template <int TYPE>
+__global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_finish(SampleParts s) {
+    __shared__ SampleLds lds;
+    SampleShared &row = s.row[blockIdx.x];
+    SampleRow<TYPE, false> r(s.a, blockIdx.x, lds);
+    SampleMode mode = begin_part(r, row, s.parts);
+    int token = -1;
+    r.set_roots();
+    if (mode == SAMPLE_FIRST) {
+        token = INT32_MAX;
+        for (int i = 0; i < s.parts; i++) token = min(token, row.first[i]);
+    }
+    if (mode == SAMPLE_TOP || mode == SAMPLE_PART) {
+        const int listed = row.listed;
+        if (listed <= SAMPLE_LIST) {
+            for (int i = threadIdx.x; i < listed; i += SAMPLE_THREADS) lds.list[i] = row.list[i];
+            if (threadIdx.x == 0) lds.listed = listed;
+            if (mode == SAMPLE_TOP && listed <= SAMPLE_PAIRS) {
+                __syncthreads();
+                token = r.finish_pairs(listed);
+                if (token >= 0) s.a.out[blockIdx.x] = token;
+                return;
+            }
+            const u64 rest = find_part(r, row, mode);
+            const int border = min(lds.found, SAMPLE_BINS - 1);
+            token = mode == SAMPLE_TOP ? r.finish_listed(border) : r.finish_part(rest, border, row.sum);
+        } else {
+            mode = SAMPLE_SLOW;
+            __syncthreads();
+        }
+    }
+    if (mode == SAMPLE_ALL) {
+        for (int i = threadIdx.x; i * r.per < r.tiles; i += SAMPLE_THREADS) lds.sum[i] = row.sum[i];
+        token = r.draw();
+    }
+    if (mode == SAMPLE_SLOW) {
+        __syncthreads();
+        token = r.slowly();
+    }
+    if (threadIdx.x == 0) s.a.out[blockIdx.x] = token;
+}
+
+template <int TYPE>
+static void sample_type(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStream_t st) {
+    constexpr int E = SampleRow<TYPE, false>::E, TILE = SampleRow<TYPE, false>::TILE;
+    const dim3 block(SAMPLE_THREADS);
+    // As many workgroups to a row as give the CUs two each, while a thread has two tiles' worth of a row
+    int parts = (int)min((int64_t)SAMPLE_PARTS, 512 / a.rows);
+    parts = min(parts, a.vocab / (2 * SAMPLE_THREADS * E));
+    if (a.rows * sizeof(SampleShared) > CLEAR_WS_FLOATS * 4) parts = 1;
     ScopedTimer timer(ctx, "k_clear_sample", st);
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((u32)a.rows), dim3(SAMPLE_THREADS), 0, st, a); };
-    if (a.type == ENSI_T_F32) go(k_clear_sample<ENSI_T_F32>);
-    else if (a.type == ENSI_T_BF16) go(k_clear_sample<ENSI_T_BF16>);
-    else go(k_clear_sample<ENSI_T_F16>);
+    if (parts < 2 || !ctx->ws_clear) {
+        if (a.vocab <= 64 * TILE) hipLaunchKernelGGL((k_clear_sample<TYPE, true>), dim3((u32)a.rows), block, 0, st, a);
+        else hipLaunchKernelGGL((k_clear_sample<TYPE, false>), dim3((u32)a.rows), block, 0, st, a);
+        return;
+    }
+    const SampleParts s = {a, (SampleShared *)ctx->ws_clear, parts};
+    const dim3 grid(parts, (u32)a.rows);
+    hipLaunchKernelGGL(k_clear_sample_most<TYPE>, grid, block, 0, st, s);
+    hipLaunchKernelGGL(k_clear_sample_bins<TYPE>, grid, block, 0, st, s);
+    if (a.top_k || a.top_p || a.all_top_k > 0 || a.all_top_p < 1) hipLaunchKernelGGL(k_clear_sample_gather<TYPE>, grid, block, 0, st, s);
+    hipLaunchKernelGGL(k_clear_sample_finish<TYPE>, dim3((u32)a.rows), block, 0, st, s);
+}
+
+void launch_clear_sample(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStream_t st) {
+    if (a.type == ENSI_T_F32) sample_type<ENSI_T_F32>(ctx, a, st);
+    else if (a.type == ENSI_T_BF16) sample_type<ENSI_T_BF16>(ctx, a, st);
+    else sample_type<ENSI_T_F16>(ctx, a, st);
 }
