@@ -122,9 +122,9 @@ struct SampleRow {
     // kept so far: values above `edge`, and of the equal ones those up to index `last`
     float edge, small;     // small: the smallest value that min_p leaves
     int last;
-    vec held[HELD ? AHEAD : 1];
+    vec held0, held1, held2, held3;
 
-    __device__ SampleRow(const ensi_clear_sample_args &a, int64_t row, SampleLds &l) : lds(l) {
+    __device__ __forceinline__ SampleRow(const ensi_clear_sample_args &a, int64_t row, SampleLds &l) : lds(l) {
         x = (const T *)a.logits + row * a.stride;
         vocab = a.vocab;
         tiles = (vocab + TILE - 1) / TILE;
@@ -136,9 +136,12 @@ struct SampleRow {
         m = a.min_p ? a.min_p[row] : a.all_min_p;
         k = a.top_k ? a.top_k[row] : a.all_top_k;
         u = a.uniform[row];
-        if (HELD)
-#pragma unroll
-            for (int i = 0; i < AHEAD; i++) held[HELD ? i : 0] = fetch(wave + SAMPLE_WAVES * i);
+        if constexpr (HELD) {
+            held0 = fetch(wave);
+            held1 = fetch(wave + SAMPLE_WAVES);
+            held2 = fetch(wave + 2 * SAMPLE_WAVES);
+            held3 = fetch(wave + 3 * SAMPLE_WAVES);
+        }
     }
     // With the row's largest value (NaN where it has one): what is to be done, and the constants for it
     __device__ __forceinline__ SampleMode begin(float most) {
@@ -222,20 +225,22 @@ struct SampleRow {
     template <class TODO>
     __device__ __forceinline__ void walk_part(int first, int end, const TODO &todo) const {
         if constexpr (HELD) {
-#pragma unroll
-            for (int i = 0; i < AHEAD; i++)
-                if (wave + SAMPLE_WAVES * i < tiles) {
-                    float f[E];
-                    widen(f, held[i]);
-                    todo(f, (wave + SAMPLE_WAVES * i) * TILE + lane * E);
-                }
+            const auto one = [&](const vec &v, int tile) {
+                if (tile >= tiles) return;
+                float f[E];
+                widen(f, v);
+                todo(f, tile * TILE + lane * E);
+            };
+            one(held0, wave);
+            one(held1, wave + SAMPLE_WAVES);
+            one(held2, wave + 2 * SAMPLE_WAVES);
+            one(held3, wave + 3 * SAMPLE_WAVES);
         } else
             walk(first + wave, end, SAMPLE_WAVES, todo);
     }
     template <class TODO>
     __device__ __forceinline__ void walk_part_slowly(int first, int end, const TODO &todo) const {
-        if constexpr (HELD) walk_part(first, end, todo);
-        else walk_slowly(first + wave, end, SAMPLE_WAVES, todo);
+        walk_slowly(first + wave, end, SAMPLE_WAVES, todo);
     }
     __device__ __forceinline__ bool kept(float f, int index) const { return (f > edge) | ((f == edge) & (index <= last)); }
     __device__ __forceinline__ double place(float f) const { return ((double)f - (double)top) * rate; }
@@ -432,20 +437,12 @@ struct SampleRow {
             for (int i = 0; i < E; i++) s += w[i];
             s -= E * NO_WEIGHT;
         };
-        if constexpr (HELD) {  // (a segment is a tile)
-            walk_part(0, tiles, [&](const float (&f)[E], int at) {
-                s = 0;
-                add(f, at);
-                s = wave_sum(s);
-                if (lane == 0) into[at / TILE] = s;
-            });
-        } else
-            for (int segment = first_segment + wave; segment < end_segment; segment += SAMPLE_WAVES) {
-                s = 0;
-                walk_slowly(segment * per, min((segment + 1) * per, tiles), 1, add);
-                s = wave_sum(s);
-                if (lane == 0) into[segment] = s;
-            }
+        for (int segment = first_segment + wave; segment < end_segment; segment += SAMPLE_WAVES) {
+            s = 0;
+            walk_slowly(segment * per, min((segment + 1) * per, tiles), 1, add);
+            s = wave_sum(s);
+            if (lane == 0) into[segment] = s;
+        }
     }
     // The first index at which the running sum of of(weights, values, index of the first), whose sums over segments are in lds.sum, reaches target(the whole sum) >= 1
     template <class OF, class TARGET>
@@ -506,14 +503,10 @@ struct SampleRow {
     template <bool COUNTS>
     __device__ __forceinline__ void bound(u64 target) {
         const auto each = [&](const auto &todo) {
-            walk_part(0, tiles, [&](const float (&f)[E], int at) {
-#pragma unroll 1
-                for (int i = 0; i < E; i++) {
-                    float v = f[0];
+            walk(wave, tiles, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
 #pragma unroll
-                    for (int j = 1; j < E; j++) v = j == i ? f[j] : v;
-                    if (kept(v, at + i)) todo(key_of(v), [&] { return weight(v); });
-                }
+                for (int i = 0; i < E; i++)
+                    if (kept(f[i], at + i)) todo(key_of(f[i]), [&] { return weight(f[i]); });
             });
         };
         if (COUNTS) count_bins(0, tiles);  // (nothing is cut before)
@@ -524,7 +517,7 @@ struct SampleRow {
         target -= lds.found_before;
         // the values in that bin
         u32 low = ~0u, high = 0;
-        walk_part(0, tiles, [&](const float (&f)[E], int at) {
+        walk(wave, tiles, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
 #pragma unroll
             for (int i = 0; i < E; i++)
                 if (bin(f[i]) == border && kept(f[i], at + i)) {
@@ -568,7 +561,7 @@ struct SampleRow {
         if (p < 1) {
             u64 sum = 0;
             if (k) {
-                walk_part_slowly(0, tiles, [&](const float (&f)[E], int at) {
+                walk_slowly(wave, tiles, SAMPLE_WAVES, [&](const float (&f)[E], int at) {
                     u64 w[E];
                     bool is[E];
 #pragma unroll
@@ -811,7 +804,7 @@ struct SampleParts {
 template <class ROW>
 struct SampleRange {
     int segment0, segment1, tile0, tile1;
-    __device__ SampleRange(const ROW &r, int parts, int i) {
+    __device__ __forceinline__ SampleRange(const ROW &r, int parts, int i) {
         const int segments = (r.tiles + r.per - 1) / r.per, each = (segments + parts - 1) / parts;
         segment0 = min(i * each, segments);
         segment1 = min(segment0 + each, segments);
