@@ -38,7 +38,7 @@ struct SampleLds {
 // What the workgroups of a row leave for each other, in the workspace
 struct SampleShared {
     u64 bins[SAMPLE_BINS], sum[SAMPLE_SEGMENTS], list[SAMPLE_LIST];
-    float most[SAMPLE_PARTS];
+    float most[SAMPLE_PARTS], threads[SAMPLE_PARTS * SAMPLE_THREADS];  // the largest values of the parts, and of their threads
     int first[SAMPLE_PARTS];
     int listed, pad;
 };
@@ -407,30 +407,35 @@ struct SampleRow {
         __syncthreads();
     }
     // Puts the values of the bins from `low` to `high` into the list
-    __device__ __forceinline__ void gather(int first, int end, int low, int high) const {
+    __device__ __forceinline__ void enlist(const float (&f)[E], int at, int low, int high) const {
+#pragma unroll
+        for (int i = 0; i < E; i++) {
+            const int b = bin(f[i]);
+            if (b >= low && b <= high) {
+                const int n = atomicAdd(&lds.listed, 1);
+                if (n < SAMPLE_LIST) lds.list[n] = (u64)key_of(f[i]) << 32 | ~(u32)(at + i);
+            }
+        }
+    }
+    __device__ __forceinline__ void gather(int first, int end, int high) const {
         walk_part(first, end, [&](const float (&f)[E], int at) {
             float most = f[0];
 #pragma unroll
             for (int i = 1; i < E; i++) most = fmaxf(most, f[i]);
-            if (bin(most) > high) return;
-#pragma unroll
-            for (int i = 0; i < E; i++)
-                if (bin(f[i]) >= low && bin(f[i]) <= high) {
-                    const int n = atomicAdd(&lds.listed, 1);
-                    if (n < SAMPLE_LIST) lds.list[n] = (u64)key_of(f[i]) << 32 | ~(u32)(at + i);
-                }
+            if (bin(most) <= high) enlist(f, at, 0, high);
         });
         __syncthreads();
     }
-    // Weights of what `in` holds for, summed over each segment
-    template <class IN>
-    __device__ __forceinline__ void sums(int first_segment, int end_segment, u64 *into, const IN &in) const {
+    // Weights of what `in` holds for, summed over each segment; look(values, index of the first) sees all
+    template <class IN, class LOOK>
+    __device__ __forceinline__ void sums(int first_segment, int end_segment, u64 *into, const IN &in, const LOOK &look) const {
         u64 s = 0;
         const auto add = [&](const float (&f)[E], int at) {
             u64 w[E];
             bool is[E], any = false;
 #pragma unroll
             for (int i = 0; i < E; i++) any |= is[i] = in(f[i], at + i);
+            look(f, at);
             if (!__any(any)) return;
             weights<E>(w, f, is);
 #pragma unroll
@@ -443,6 +448,14 @@ struct SampleRow {
             s = wave_sum(s);
             if (lane == 0) into[segment] = s;
         }
+    }
+    __device__ __forceinline__ void kept_sums(int first_segment, int end_segment, u64 *into) const {
+        sums(first_segment, end_segment, into, [&](float f, int at) { return kept(f, at); }, [](const float (&)[E], int) {});
+    }
+    // Those above a bin, which goes into the list
+    __device__ __forceinline__ void sums_above(int first_segment, int end_segment, u64 *into, int border) const {
+        sums(first_segment, end_segment, into, [&](float f, int) { return bin(f) < border && f >= small; }, [&](const float (&f)[E], int at) { enlist(f, at, border, border); });
+        __syncthreads();
     }
     // The first index at which the running sum of of(weights, values, index of the first), whose sums over segments are in lds.sum, reaches target(the whole sum) >= 1
     template <class OF, class TARGET>
@@ -578,13 +591,13 @@ struct SampleRow {
         }
         keep_small();
         __syncthreads();
-        sums(0, (tiles + per - 1) / per, lds.sum, [&](float f, int at) { return kept(f, at); });
+        kept_sums(0, (tiles + per - 1) / per, lds.sum);
         return draw();
     }
-    // The same in one step where the elements, each(todo) with todo(bin, order, weight), are spread over the bins: the order (a falling one) of the element at which the running sum reaches
-    // `target`; 0 where a bin has too many.  `wave` 0 puts the elements of the bin in order.
+    // The same for few elements that are spread over the bins, each(todo) with todo(bin, order, weight).  First the bin where the running sum reaches `target`: into lds.found, how many
+    // there are in lds.count; returns what is left of the target
     template <bool COUNTS, class EACH>
-    __device__ __forceinline__ u64 select_spread(u64 target, const EACH &each) const {
+    __device__ __forceinline__ u64 find_spread(u64 target, const EACH &each) const {
         clear_bins();
         if (threadIdx.x == 0) lds.few = 0;
         each([&](int b, u64, const auto &weight) {
@@ -592,9 +605,12 @@ struct SampleRow {
             if (!COUNTS) atomicAdd((unsigned long long *)&lds.sum[b], (unsigned long long)weight());
         });
         find_at<COUNTS>(SAMPLE_BINS, target);
+        return target - lds.found_before;
+    }
+    // then, for up to 64 of them, the order (a falling one, never 0) of the element: a wave compares each with each
+    template <bool COUNTS, class EACH>
+    __device__ __forceinline__ u64 order_spread(u64 target, const EACH &each) const {
         const int border = lds.found;
-        if (lds.count[border] > 64) return 0;
-        target -= lds.found_before;
         each([&](int b, u64 order, const auto &weight) {
             if (b == border) {
                 const int i = atomicAdd(&lds.few, 1);
@@ -611,9 +627,7 @@ struct SampleRow {
             if (before < target && before + w >= target) lds.found_before = mine;  // (of one lane: the orders differ)
         }
         __syncthreads();
-        const u64 order = lds.found_before;
-        __syncthreads();
-        return order;
+        return lds.found_before;  // (a barrier before it is written again is clear_bins')
     }
     // ---- in the list of candidates
     template <class TODO>
@@ -623,28 +637,35 @@ struct SampleRow {
             if (kept(of_key((u32)(e >> 32)), (int)~(u32)e)) todo((u32)(e >> 32), ~(u32)e);
         }
     }
+    __device__ __forceinline__ int index_bin(u32 i) const { return (int)(i >> max(0, 21 - __clz(vocab - 1))); }  // 2048 bins of indices
     // Moves the bound as above, to one among the candidates, which are in the bins from `from` to `to`.
     template <bool COUNTS>
     __device__ __forceinline__ void bound_listed(u64 target, int from, int to) {
         const float finer = (float)SAMPLE_BINS / (to + 1 - from);
-        const u64 spread = select_spread<COUNTS>(target, [&](const auto &todo) {
-            each_listed([&](u32 key, u32 i) { todo(max(0, min((int)(((top - of_key(key)) * bins - from) * finer), SAMPLE_BINS - 1)), (u64)key << 32 | ~i, [&] { return weight(of_key(key)); }); });
-        });
-        if (spread) {
-            edge = of_key((u32)(spread >> 32));
-            last = (int)~(u32)spread;
+        const auto bin_of = [&](u32 key) { return max(0, min((int)(((top - of_key(key)) * bins - from) * finer), SAMPLE_BINS - 1)); };
+        const auto by_value = [&](const auto &todo) {
+            each_listed([&](u32 key, u32 i) { todo(bin_of(key), (u64)key << 32 | ~i, [&] { return weight(of_key(key)); }); });
+        };
+        target = find_spread<COUNTS>(target, by_value);
+        const int border = lds.found;
+        int ties = (int)lds.count[border];
+        if (ties <= 64) {
+            const u64 order = order_spread<COUNTS>(target, by_value);
+            edge = of_key((u32)(order >> 32));
+            last = (int)~(u32)order;
             return;
         }
-        int ties;
+        // many: 16 bits leave few values to a bin
         u32 low = ~0u, high = 0;
         each_listed([&](u32 key, u32) {
+            if (bin_of(key) != border) return;
             low = min(low, key);
             high = max(high, key);
         });
-        __syncthreads();
         low = reduce(low, ~0u, lds.low, [](u32 a, u32 b) { return min(a, b); });
         high = reduce(high, 0, lds.high, [](u32 a, u32 b) { return max(a, b); });
-        const u32 key = select<COUNTS>(low, high, target, ties, [&](const auto &todo) { each_listed([&](u32 key, u32) { todo(key, [&] { return weight(of_key(key)); }); }); });
+        if (low != high) high = select<COUNTS>(low, high, target, ties, [&](const auto &todo) { each_listed([&](u32 key, u32) { todo(key, [&] { return weight(of_key(key)); }); }); });
+        const u32 key = high;
         const float value = of_key(key);
         u64 needed = target;
         if (!COUNTS) {
@@ -652,14 +673,26 @@ struct SampleRow {
             needed = w ? (target + w - 1) / w : ties;
         }
         int index = edge == value ? last : INT32_MAX;
-        if (needed < (u64)ties)
-            index = (int)~select<true>(~(u32)(vocab - 1), ~0u, needed, ties, [&](const auto &todo) {
-                each_listed([&](u32 k, u32 i) {
-                    if (k == key) todo(~i, [] { return 1; });
-                });
-            });
+        if (needed < (u64)ties) index = index_listed<true>(needed, [=](u32 k) { return k == key; });
         edge = value;
         last = index;
+    }
+    // The index at which the running sum of the candidates `in` holds for, by index, reaches `target`
+    template <bool COUNTS, class IN>
+    __device__ __forceinline__ int index_listed(u64 target, const IN &in) const {
+        const auto by_index = [&](const auto &todo) {
+            each_listed([&](u32 key, u32 i) {
+                if (in(key)) todo(index_bin(i), ~(u64)i, [&] { return weight(of_key(key)); });
+            });
+        };
+        u64 rest = find_spread<COUNTS>(target, by_index);
+        if (lds.count[lds.found] <= 64) return (int)~(u32)order_spread<COUNTS>(rest, by_index);
+        int ties;
+        return (int)~select<COUNTS>(~(u32)(vocab - 1), ~0u, target, ties, [&](const auto &todo) {
+            each_listed([&](u32 key, u32 i) {
+                if (in(key)) todo(~i, [&] { return weight(of_key(key)); });
+            });
+        });
     }
     // The token of a row whose top k are among few candidates, four threads to each; waves without one are done.  -1 in threads that do not have it.
     __device__ __forceinline__ int finish_pairs(int n) const {
@@ -719,12 +752,7 @@ struct SampleRow {
         if (k < n) bound_listed<true>(k, 0, limit);
         if (p < 1) bound_listed<false>(part_target(sum(), p), 0, limit);
         keep_small();
-        u64 target = draw_target(sum(), u) + 1;
-        const int shift_index = max(0, 21 - __clz(vocab - 1));  // 2048 bins of indices
-        const u64 spread = select_spread<false>(target, [&](const auto &todo) { each_listed([&](u32 key, u32 i) { todo((int)(i >> shift_index), ~(u64)i, [&] { return weight(of_key(key)); }); }); });
-        if (spread) return (int)~(u32)spread;
-        int ties;
-        return (int)~select<false>(~(u32)(vocab - 1), ~0u, target, ties, [&](const auto &todo) { each_listed([&](u32 key, u32 i) { todo(~i, [&] { return weight(of_key(key)); }); }); });
+        return index_listed<false>(draw_target(sum(), u) + 1, [](u32) { return true; });
     }
     // The token of a row whose bound by top_p is among the candidates, where it leaves `rest` of the sum; the segments' sums of what is above are in lds.sum
     __device__ __forceinline__ int finish_part(u64 rest, int border, u64 *sums) {
@@ -763,7 +791,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample(ensi_clear_samp
             r.template find_at<true>(SAMPLE_BINS, r.k);
             limit = min(lds.found, limit);
         }
-        r.gather(0, tiles, 0, limit);
+        r.gather(0, tiles, limit);
         if (lds.listed <= SAMPLE_PAIRS) {
             token = r.finish_pairs(lds.listed);
             if (token >= 0) a.out[blockIdx.x] = token;
@@ -777,16 +805,13 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample(ensi_clear_samp
         const u64 target = r.template find<false>(SAMPLE_BINS, [&](u64 sum) { return part_target(sum, r.p); });
         const int border = lds.found;
         const u64 rest = target - lds.found_before;
-        r.gather(0, tiles, border, border);
-        if (lds.listed <= SAMPLE_LIST) {
-            r.sums(0, segments, above, [&](float f, int) { return r.bin(f) < border && f >= r.small; });
-            token = r.finish_part(rest, border, above);
-        } else
-            mode = SAMPLE_SLOW;
+        r.sums_above(0, segments, above, border);
+        if (lds.listed <= SAMPLE_LIST) token = r.finish_part(rest, border, above);
+        else mode = SAMPLE_SLOW;
     }
     if (mode == SAMPLE_ALL) {
         __syncthreads();
-        r.sums(0, segments, lds.sum, [&](float f, int at) { return r.kept(f, at); });
+        r.kept_sums(0, segments, lds.sum);
         token = r.draw();
     }
     if (mode == SAMPLE_SLOW) token = r.slowly();
@@ -836,7 +861,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_most(SamplePart
     const SampleRange<SampleRow<TYPE, false>> g(r, s.parts, blockIdx.x);
     for (int i = blockIdx.x * SAMPLE_THREADS + threadIdx.x; i < SAMPLE_BINS; i += s.parts * SAMPLE_THREADS) row.bins[i] = 0;
     if (blockIdx.x == 0 && threadIdx.x == 0) row.listed = 0;
-    const u32 most = r.reduce(__builtin_bit_cast(u32, r.largest(g.tile0, g.tile1)), __builtin_bit_cast(u32, -__builtin_inff()), lds.low, larger);
+    const float mine = r.largest(g.tile0, g.tile1);
+    row.threads[blockIdx.x * SAMPLE_THREADS + threadIdx.x] = mine;
+    const u32 most = r.reduce(__builtin_bit_cast(u32, mine), __builtin_bit_cast(u32, -__builtin_inff()), lds.low, larger);
     if (threadIdx.x == 0) row.most[blockIdx.x] = __builtin_bit_cast(float, most);
 }
 template <int TYPE>
@@ -849,7 +876,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_bins(SamplePart
     if (mode == SAMPLE_FIRST) {
         const int first = r.first_largest(g.tile0, g.tile1);
         if (threadIdx.x == 0) row.first[blockIdx.x] = first;
-    } else if (mode == SAMPLE_TOP) {
+    } else if (mode == SAMPLE_TOP && r.k > SAMPLE_FEW * s.parts) {
         r.count_bins(g.tile0, g.tile1);
         for (int i = threadIdx.x; i < SAMPLE_BINS; i += SAMPLE_THREADS)
             if (lds.count[i]) atomicAdd((unsigned long long *)&row.bins[i], (unsigned long long)lds.count[i]);
@@ -861,7 +888,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_bins(SamplePart
     } else if (mode == SAMPLE_ALL) {
         r.set_roots();
         __syncthreads();
-        r.sums(g.segment0, g.segment1, row.sum, [&](float f, int at) { return r.kept(f, at); });
+        r.kept_sums(g.segment0, g.segment1, row.sum);
     }
 }
 template <int TYPE>
@@ -874,15 +901,26 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_gather(SamplePa
     const SampleMode mode = begin_part(r, row, s.parts);
     if (mode != SAMPLE_TOP && mode != SAMPLE_PART) return;
     if (threadIdx.x == 0) lds.listed = 0;
-    if (mode == SAMPLE_PART) r.set_roots();
-    find_part(r, row, mode);
-    const int border = lds.found;
-    r.gather(g.tile0, g.tile1, mode == SAMPLE_TOP ? 0 : border, min(border, SAMPLE_BINS - 1));
+    if (mode == SAMPLE_TOP) {
+        if (r.k <= SAMPLE_FEW * s.parts) {
+            r.clear_bins();
+            for (int i = threadIdx.x; i < s.parts * SAMPLE_THREADS; i += SAMPLE_THREADS) {
+                const int b = r.bin(row.threads[i]);
+                if (b < SAMPLE_BINS) atomicAdd(&lds.count[b], 1u);
+            }
+            r.template find_at<true>(SAMPLE_BINS, r.k);
+        } else
+            find_part(r, row, mode);
+        r.gather(g.tile0, g.tile1, min(lds.found, SAMPLE_BINS - 1));
+    } else {
+        r.set_roots();
+        find_part(r, row, mode);
+        r.sums_above(g.segment0, g.segment1, row.sum, lds.found);
+    }
     const int listed = lds.listed;
     if (threadIdx.x == 0) at = atomicAdd(&row.listed, listed);  // (past the list's end where there are too many)
     __syncthreads();
     for (int i = threadIdx.x; i < min(listed, SAMPLE_LIST) && at + i < SAMPLE_LIST; i += SAMPLE_THREADS) row.list[at + i] = lds.list[i];
-    if (mode == SAMPLE_PART) r.sums(g.segment0, g.segment1, row.sum, [&](float f, int) { return r.bin(f) < border && f >= r.small; });
 }
 template <int TYPE>
 __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_finish(SampleParts s) {
@@ -907,9 +945,13 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_finish(SamplePa
                 if (token >= 0) s.a.out[blockIdx.x] = token;
                 return;
             }
-            const u64 rest = find_part(r, row, mode);
-            const int border = min(lds.found, SAMPLE_BINS - 1);
-            token = mode == SAMPLE_TOP ? r.finish_listed(border) : r.finish_part(rest, border, row.sum);
+            if (mode == SAMPLE_TOP) {
+                __syncthreads();
+                token = r.finish_listed(SAMPLE_BINS - 1);
+            } else {
+                const u64 rest = find_part(r, row, mode);
+                token = r.finish_part(rest, lds.found, row.sum);
+            }
         } else {
             mode = SAMPLE_SLOW;
             __syncthreads();
@@ -931,7 +973,7 @@ static void sample_type(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStrea
     constexpr int E = SampleRow<TYPE, false>::E, TILE = SampleRow<TYPE, false>::TILE;
     const dim3 block(SAMPLE_THREADS);
     // As many workgroups to a row as give the CUs two each, while a thread has two tiles' worth of a row
-    int parts = (int)min((int64_t)SAMPLE_PARTS, 512 / a.rows);
+    int parts = (int)min((int64_t)SAMPLE_PARTS, 1024 / a.rows);
     parts = min(parts, a.vocab / (2 * SAMPLE_THREADS * E));
     if (a.rows * sizeof(SampleShared) > CLEAR_WS_FLOATS * 4) parts = 1;
     ScopedTimer timer(ctx, "k_clear_sample", st);
