@@ -904,8 +904,12 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_gather(SamplePa
     if (mode == SAMPLE_TOP) {
         if (r.k <= SAMPLE_FEW * s.parts) {
             r.clear_bins();
-            for (int i = threadIdx.x; i < s.parts * SAMPLE_THREADS; i += SAMPLE_THREADS) {
-                const int b = r.bin(row.threads[i]);
+            float most[SAMPLE_PARTS];
+#pragma unroll
+            for (int i = 0; i < SAMPLE_PARTS; i++) most[i] = i < s.parts ? row.threads[i * SAMPLE_THREADS + threadIdx.x] : -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < SAMPLE_PARTS; i++) {
+                const int b = r.bin(most[i]);
                 if (b < SAMPLE_BINS) atomicAdd(&lds.count[b], 1u);
             }
             r.template find_at<true>(SAMPLE_BINS, r.k);
