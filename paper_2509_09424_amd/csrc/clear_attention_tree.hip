@@ -45,12 +45,23 @@ __device__ __forceinline__ u64 near_line(u64 line, int window) {
     return line;
 }
 
+template <int DIM, int RT>
+struct TreeLds {
+    static constexpr int ROWS = 16 * RT, ROW = DIM + 4;  // floats of a row; 4 more put the rows that are written at once on different banks
+    static constexpr int BYTES = 4 * ROWS * (ROW + 2) * 4;
+};
+
 template <int TYPE, int DIM, int SCORE, int RT>
 __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, const int32_t *parents, int split_tiles) {
     typedef typename Elem<TYPE>::type T;
     typedef Wide<TYPE> W;
     typedef typename W::vec vec;
+    typedef TreeLds<DIM, RT> L;
     constexpr int STEPS = DIM / 32, TILES = DIM / 16, PIECE = Split<DIM>::PIECE, REST = Split<DIM>::REST, MAIN = Split<DIM>::MAIN;
+    constexpr bool VALUES_AHEAD = RT == 4;  // one wave to a SIMD in any case
+    extern __shared__ __align__(16) float tree_lds[];
+    __shared__ u64 lines[TREE_MAX];
+    __shared__ int places[TREE_MAX];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, g = lane / 16;
     const int blocks = (a.row_tiles + RT - 1) / RT;
     const int seq = blockIdx.z, head = blockIdx.x / blocks, row0 = 16 * RT * (blockIdx.x % blocks), split = blockIdx.y;
@@ -59,17 +70,6 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
     const TreeKeys keys = tree_keys(part, a.window);
     const int tile0 = split * split_tiles, tile1 = min(tile0 + split_tiles, keys.tiles);
     if (row0 >= rows || tile0 >= tile1) return;
-    __shared__ u64 lines[TREE_MAX];
-    __shared__ int places[TREE_MAX];
-    {
-        const Tree tree = tree_of(parents, part, a.kv.status);
-        if (!tree.good) return;
-        if (wave == 0) {
-            lines[lane] = near_line(tree.line, a.window);
-            places[lane] = part.ctx + tree.depth;
-        }
-    }
-    __syncthreads();
     int index[RT];  // of the row's token among the new ones
     vec q[RT][STEPS];
     Rows16<DIM> st[RT];
@@ -83,24 +83,38 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
         for (int s = 0; s < STEPS; s++) q[rt][s] = *(const loose *)(p + 8 * s);
         st[rt].clear();
     }
+    // 32 tiles of this wave at once: lane l looks up the block of 16 keys of half l % 2 of tile l / 2
+    int my_block = 0, my_good = 0;
+    float my_k = 1, my_v = 1;
+    const auto look_up = [&](int batch) {
+        const int t = batch + 4 * (lane / 2), key = keys.lo + 32 * t + 16 * (lane % 2);
+        my_block = my_good = 0;
+        my_k = my_v = 1;
+        if (t < tile1 && key <= keys.last && (a.window <= 0 || key + KV_BLOCK - 1 > part.ctx - a.window)) {
+            const int block = block_of(a, seq, head, key);
+            if (block >= 0) {
+                my_block = block;
+                my_good = 1;
+                my_k = a.kv.ks[block];
+                my_v = fmaxf(a.kv.vs[block], 0x1p-64f);
+            } else
+                atomicOr(a.kv.status, ENSI_KV_BAD_PAGE);
+        }
+    };
+    look_up(tile0 + wave);
+    // lines and positions, where a tile has new tokens or the edge of a window (what is left out for its tree is left out by those workgroups and the join)
+    if (keys.lo + 32 * tile1 > part.ctx || a.window > 0) {
+        const Tree tree = tree_of(parents, part, a.kv.status);
+        if (!tree.good) return;
+        if (wave == 0) {
+            lines[lane] = near_line(tree.line, a.window);
+            places[lane] = part.ctx + tree.depth;
+        }
+        __syncthreads();
+    }
     int nan_from = INT32_MAX, nan_to = -1;  // keys between which values had NaN
     for (int batch = tile0 + wave; batch < tile1; batch += 4 * 32) {
-        // 32 tiles of this wave at once: lane l looks up the block of 16 keys of half l % 2 of tile l / 2
-        int my_block = 0, my_good = 0;
-        float my_k = 1, my_v = 1;
-        {
-            const int t = batch + 4 * (lane / 2), key = keys.lo + 32 * t + 16 * (lane % 2);
-            if (t < tile1 && key <= keys.last && (a.window <= 0 || key + KV_BLOCK - 1 > part.ctx - a.window)) {
-                const int block = block_of(a, seq, head, key);
-                if (block >= 0) {
-                    my_block = block;
-                    my_good = 1;
-                    my_k = a.kv.ks[block];
-                    my_v = fmaxf(a.kv.vs[block], 0x1p-64f);
-                } else
-                    atomicOr(a.kv.status, ENSI_KV_BAD_PAGE);
-            }
-        }
+        if (batch != tile0 + wave) look_up(batch);
         const int turns = min(32, (tile1 - batch + 3) / 4);
         // keys: lane (n, g) has places DIM / 4 g .. of key n; values: places PIECE n .. of keys 4 g .. 4 g + 3 of either half
         constexpr int WORDS = (PIECE + REST + 3) / 4;
@@ -109,7 +123,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
             u32 v[2][WORDS][4];
         };
         const int k_at = n * DIM + g * (DIM / 4), v_at = 4 * g * DIM + PIECE * n, rest_at = 4 * g * DIM + MAIN + REST * n;
-        const auto fetch = [&](Codes &to, int i) {
+        const auto fetch_keys = [&](Codes &to, int i) {
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 // a wave's base and a lane's offset of 32 bits: no registers for 64-bit addresses
@@ -117,6 +131,8 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
 #pragma unroll
                 for (int s = 0; s < STEPS; s++) to.k[h][s] = *(const u32x2 *)(p + (u32)(k_at + 8 * s));
             }
+        };
+        const auto fetch_values = [&](Codes &to, int i) {
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 const unsigned char *p = a.kv.v + (int64_t)__builtin_amdgcn_readlane(my_block, 2 * i + h) * (KV_BLOCK * DIM);
@@ -131,6 +147,9 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                 }
             }
         };
+        Codes now, next;
+        fetch_keys(now, 0);
+        if (VALUES_AHEAD) fetch_values(now, 0);
         for (int i = 0; i < turns; i++) {
             const int key0 = keys.lo + 32 * (batch + 4 * i);
             int good[2];
@@ -142,14 +161,18 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                 vs[h] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 2 * i + h));
                 lv[h] = SCORE == ENSI_SCORE_SIGMOID ? 0 : __builtin_amdgcn_logf(vs[h]);
             }
-            Codes now;
-            fetch(now, i);
+            if (!VALUES_AHEAD) fetch_values(now, i);
             const bool masked = key0 + 31 >= part.ctx || (a.window > 0 && key0 <= keys.last - a.window) || !good[0] || !good[1];
             vec k[2][STEPS];
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int s = 0; s < STEPS; s++) k[h][s] = W::widen(now.k[h][s][0], now.k[h][s][1]);
+            // the next tile's keys are under way while this one is computed, its values too where they fit the registers
+            if (i + 1 < turns) {
+                fetch_keys(now, i + 1);
+                if (VALUES_AHEAD) fetch_values(next, i + 1);
+            }
             Weights p[RT];
 #pragma unroll
             for (int rt = 0; rt < RT; rt++) {
@@ -250,6 +273,13 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                     }
                 }
             }
+            if (VALUES_AHEAD)
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int x = 0; x < WORDS; x++)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) now.v[h][x][r] = next.v[h][x][r];
         }
     }
     for (int key = nan_from; key <= min(nan_to, keys.last); key++) {
@@ -267,125 +297,128 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                     if (is_nan(v[j < PIECE ? PIECE * (4 * g + r) + j : MAIN + REST * (4 * g + r) + j - PIECE])) st[rt].o[j][r] = __builtin_nanf("");
         }
     }
-    const bool whole = keys.tiles <= split_tiles;
-    __shared__ f32x4 part_o[2][TILES][64];
-    __shared__ float part_m[2][64], part_l[2][64];
+    // the four waves' sums through LDS, a row's floats side by side; every thread then joins and stores neighbouring ones
+    float *const ms = tree_lds + 4 * L::ROWS * L::ROW, *const ls = ms + 4 * L::ROWS;
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
         Rows16<DIM> &s = st[rt];
         // a lane has the sum of its keys only
         s.l += __shfl_xor(s.l, 16);
         s.l += __shfl_xor(s.l, 32);
-        // waves 2 and 3 into 0 and 1, wave 1 into 0
+        const int row = wave * L::ROWS + 16 * rt + n;
+        float *to = tree_lds + row * L::ROW;
 #pragma unroll
-        for (int half = 2; half >= 1; half /= 2) {
-            if (wave >= half && wave < 2 * half) {
+        for (int r = 0; r < 4; r++) {
+            typedef float piece __attribute__((ext_vector_type(PIECE)));
+            piece v;
 #pragma unroll
-                for (int j = 0; j < TILES; j++) part_o[wave - half][j][lane] = s.o[j];
-                part_m[wave - half][lane] = s.m;
-                part_l[wave - half][lane] = s.l;
+            for (int j = 0; j < PIECE; j++) v[j] = s.o[j][r];
+            *(piece *)(to + PIECE * (4 * g + r)) = v;
+            if constexpr (REST > 0) {
+                typedef float rest __attribute__((ext_vector_type(REST), aligned(8)));
+                rest w;
+#pragma unroll
+                for (int j = 0; j < REST; j++) w[j] = s.o[PIECE + j][r];
+                *(rest *)(to + MAIN + REST * (4 * g + r)) = w;
             }
-            __syncthreads();
-            if (wave < half) {
-                const float om = part_m[wave][lane], m = most_of(s.m, om), base = m == -__builtin_inff() ? 0.0f : m;
-                const float h0 = half_lift(s.m, base), h1 = half_lift(om, base);
-#pragma unroll
-                for (int j = 0; j < TILES; j++) {
-                    const f32x4 o = part_o[wave][j][lane];
-#pragma unroll
-                    for (int r = 0; r < 4; r++) s.o[j][r] = s.o[j][r] * h0 * h0 + o[r] * h1 * h1;
-                }
-                s.l = s.l * h0 * h0 + part_l[wave][lane] * h1 * h1;
-                s.m = m;
-            }
-            __syncthreads();
         }
-        if (wave == 0 && row0 + 16 * rt + n < rows) {
-            const Last end = last_of<SCORE>(s.m, s.l, [&] { return whole && sees_any_of(a, seq, part, lines[index[rt]], places[index[rt]]); });
-            float *ws = a.ws + (((int64_t)seq * a.kv.heads + head) * a.row_tiles + row0 / 16 + rt) * a.splits * (16 * DIM + 32) + (int64_t)split * (16 * DIM + 32);
-            T *out = (T *)a.out + (int64_t)(part.first + index[rt]) * a.out_stride + (int64_t)(head * a.group + (row0 + 16 * rt + n) % a.group) * DIM;
-            const auto put = [&](int at, auto first, auto count) {  // registers r of tiles first .. first + count - 1, at place `at` of the row
+        if (g == 0) {
+            ms[row] = s.m;
+            ls[row] = s.l;
+        }
+    }
+    __syncthreads();
+    const bool whole = keys.tiles <= split_tiles;
+    constexpr int QUADS = DIM / 4;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < L::ROWS * QUADS; i += 256) {
+        const int r = i / QUADS, quad = i % QUADS, row = row0 + r;
+        if (row >= rows) break;
+        float m = ms[r], l = 0;
 #pragma unroll
-                for (int r = 0; r < 4; r++)
+        for (int w = 1; w < 4; w++) m = most_of(m, ms[w * L::ROWS + r]);
+        const float base = m == -__builtin_inff() ? 0.0f : m;
+        f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-                    for (int j = 0; j < decltype(count)::value; j++) {
-                        const float v = s.o[decltype(first)::value + j][r];
-                        const int d = at + decltype(count)::value * (4 * g + r) + j;
-                        if (whole) out[d] = (T)end(v);
-                        else ws[n * DIM + d] = v;
-                    }
-            };
-            put(0, std::integral_constant<int, 0>(), std::integral_constant<int, PIECE>());
-            if constexpr (REST > 0) put(MAIN, std::integral_constant<int, PIECE>(), std::integral_constant<int, REST>());
-            if (!whole && g == 0) {
-                ws[16 * DIM + n] = s.m;
-                ws[16 * DIM + 16 + n] = s.l;
+        for (int w = 0; w < 4; w++) {
+            const float h = half_lift(ms[w * L::ROWS + r], base);
+            const f32x4 v = *(const f32x4 *)(tree_lds + (w * L::ROWS + r) * L::ROW + 4 * quad);
+#pragma unroll
+            for (int e = 0; e < 4; e++) o[e] += v[e] * h * h;
+            l += ls[w * L::ROWS + r] * h * h;
+        }
+        const int token = row / a.group;
+        if (whole) {
+            const Last end = last_of<SCORE>(m, l, [&] { return sees_any_of(a, seq, part, lines[token], places[token]); });
+            typedef T quad_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            quad_t w;
+#pragma unroll
+            for (int e = 0; e < 4; e++) w[e] = (T)end(o[e]);
+            *(quad_t *)((T *)a.out + (int64_t)(part.first + token) * a.out_stride + (int64_t)(head * a.group + row % a.group) * DIM + 4 * quad) = w;
+        } else {
+            float *ws = a.ws + ((((int64_t)seq * a.kv.heads + head) * a.row_tiles + row / 16) * a.splits + split) * (16 * DIM + 32);
+            *(f32x4 *)(ws + row % 16 * DIM + 4 * quad) = o;
+            if (quad == 0) {
+                ws[16 * DIM + row % 16] = m;
+                ws[16 * DIM + 16 + row % 16] = l;
             }
         }
     }
 }
 
-// Joins the parts of a row: a workgroup to a row.  The references first, a thread to a part, then the outputs: DIM / 4 threads to a part, as many
-// parts side by side as there are threads, added in LDS.
+// Joins the parts of a row, a wave to a row: the references first, a lane to a part, then the outputs, DIM / 4 lanes to a part and as many parts side by side as
+// there are lanes.
+#define TREE_SPLITS 64
 template <int TYPE, int DIM, int SCORE>
 __global__ __launch_bounds__(256) void k_clear_attention_tree_join(AttentionView a, const int32_t *parents, int split_tiles) {
     typedef typename Elem<TYPE>::type T;
-    constexpr int QUADS = DIM / 4, SLICES = 256 / QUADS;
-    const int seq = blockIdx.z, head = blockIdx.x / a.row_tiles, tile = blockIdx.x % a.row_tiles, n = blockIdx.y, t = threadIdx.x, row = 16 * tile + n;
+    constexpr int QUADS = DIM / 4, SLICES = 64 / QUADS;
+    const int lane = threadIdx.x % 64, seq = blockIdx.z, head = blockIdx.x / a.row_tiles, tile = blockIdx.x % a.row_tiles;
+    const int n = __builtin_amdgcn_readfirstlane(4 * blockIdx.y + threadIdx.x / 64), row = 16 * tile + n;
     const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
     const TreeKeys keys = tree_keys(part, a.window);
     if (row >= part.count * a.group || keys.tiles <= split_tiles) return;
-    const Tree tree = tree_of(parents, part, a.kv.status);
-    if (!tree.good) return;
     const int splits = (keys.tiles + split_tiles - 1) / split_tiles, index = row / a.group;
     const float *ws = a.ws + ((int64_t)seq * gridDim.x + blockIdx.x) * a.splits * (16 * DIM + 32);
-    __shared__ float factor[JOIN_MAX], top[4], sums[4];
-    __shared__ f32x4 parts[SLICES][QUADS];
-    const int quad = t % QUADS, slice = t / QUADS;
-    float m = -__builtin_inff(), l = 0;
-    if (t < splits) {
-        m = ws[(int64_t)t * (16 * DIM + 32) + 16 * DIM + n];
-        l = ws[(int64_t)t * (16 * DIM + 32) + 16 * DIM + 16 + n];
-    }
-    float most = m;
+    const int up = lane < part.count ? parents[part.first + lane] : -1;
+    if (__any(up < -1 || up >= lane)) return;  // (the status says so by now)
+    const float m = lane < splits ? ws[(int64_t)lane * (16 * DIM + 32) + 16 * DIM + n] : -__builtin_inff();
+    float l = lane < splits ? ws[(int64_t)lane * (16 * DIM + 32) + 16 * DIM + 16 + n] : 0, most = m;
 #pragma unroll
-    for (int k = 1; k < 64; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
-    if (t % 64 == 0) top[t / 64] = most;
-    __syncthreads();
-    most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    for (int k = 1; k < 64; k *= 2) most = most_of(most, __shfl_xor(most, k));
     if (most == -__builtin_inff()) most = 0;
     const float h = half_lift(m, most);
-    if (t < splits) factor[t] = h;
-    l = t < splits ? l * h * h : 0;
+    l *= h * h;
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) l += __shfl_xor(l, k);
-    if (t % 64 == 0) sums[t / 64] = l;
-    __syncthreads();
     f32x4 o = {0, 0, 0, 0};
-    if (slice < SLICES) {
+    const int quad = lane % QUADS, slice = lane / QUADS;
 #pragma unroll 4
-        for (int s = slice; s < splits; s += SLICES) {
-            const f32x4 v = *(const f32x4 *)(ws + (int64_t)s * (16 * DIM + 32) + n * DIM + 4 * quad);
-            const float f = factor[s];
+    for (int s = 0; s < splits; s += SLICES) {
+        const int mine = s + slice;
+        const float f = __shfl(h, mine & 63);
+        if (slice < SLICES && mine < splits) {
+            const f32x4 v = *(const f32x4 *)(ws + (int64_t)mine * (16 * DIM + 32) + n * DIM + 4 * quad);
 #pragma unroll
             for (int i = 0; i < 4; i++) o[i] = __builtin_fmaf(v[i] * f, f, o[i]);
         }
-        parts[slice][quad] = o;
     }
-    const u32 lo = __shfl((u32)tree.line, index), hi = __shfl((u32)(tree.line >> 32), index);
-    const int depth = __shfl(tree.depth, index);
-    __syncthreads();
-    if (t >= QUADS) return;
-    l = sums[0] + sums[1] + sums[2] + sums[3];
-    o = (f32x4){0, 0, 0, 0};
-    for (int s = 0; s < SLICES; s++) o += parts[s][t];
-    const int token = part.first + index, q_head = head * a.group + row % a.group;
-    const Last end = last_of<SCORE>(most, l, [&] { return sees_any_of(a, seq, part, near_line((u64)hi << 32 | lo, a.window), part.ctx + depth); });
+#pragma unroll
+    for (int k = SLICES / 2; k >= 1; k /= 2)
+#pragma unroll
+        for (int i = 0; i < 4; i++) o[i] += __shfl(o[i], (lane + k * QUADS) & 63);
+    if (lane >= QUADS) return;
+    const int q_head = head * a.group + row % a.group;
+    const Last end = last_of<SCORE>(most, l, [&] {
+        u64 line = 0;  // of the row's token
+        for (int t = index; t >= 0; t = parents[part.first + t]) line |= (u64)1 << t;
+        return sees_any_of(a, seq, part, near_line(line, a.window), part.ctx + __popcll(line) - 1);
+    });
     typedef T quad_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     quad_t w;
 #pragma unroll
     for (int i = 0; i < 4; i++) w[i] = (T)end(o[i]);
-    *(quad_t *)((T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM + 4 * t) = w;
+    *(quad_t *)((T *)a.out + (int64_t)(part.first + index) * a.out_stride + (int64_t)q_head * DIM + 4 * quad) = w;
 }
 
 template <int TYPE, int DIM, int SCORE>
@@ -397,7 +430,7 @@ static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipS
     const int rt = v.row_tiles == 1 ? 1 : v.row_tiles == 2 || DIM > 128 ? 2 : 4;
     const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + rt - 1) / rt);
     int splits = max((tiles + 31) / 32, base < 256 && tiles > 16 ? (int)(512 / base) : 1);
-    splits = min(splits, min((tiles + 3) / 4, JOIN_MAX));
+    splits = min(splits, min((tiles + 3) / 4, TREE_SPLITS));
     splits = max(splits, 1);
     const int64_t room = (int64_t)CLEAR_WS_FLOATS / ((int64_t)v.s.seqs * heads * v.row_tiles * (16 * DIM + 32));
     if (splits > room) splits = (int)max((int64_t)1, room);
@@ -407,15 +440,18 @@ static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipS
     v.splits = splits;
     {
         ScopedTimer timer(ctx, "k_clear_attention_tree", st);
-        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(heads * ((v.row_tiles + rt - 1) / rt), splits, v.s.seqs), dim3(256), 0, st, v, parents, split_tiles); };
-        if (rt == 1) go(k_clear_attention_tree<TYPE, DIM, SCORE, 1>);
-        else if (rt == 2) go(k_clear_attention_tree<TYPE, DIM, SCORE, 2>);
-        else if constexpr (DIM <= 128) go(k_clear_attention_tree<TYPE, DIM, SCORE, 4>);
+        const auto go = [&](auto kernel, int bytes) {
+            if (bytes > 48 * 1024) clear_lds(ctx, (const void *)kernel, bytes);
+            hipLaunchKernelGGL(kernel, dim3(heads * ((v.row_tiles + rt - 1) / rt), splits, v.s.seqs), dim3(256), bytes, st, v, parents, split_tiles);
+        };
+        if (rt == 1) go(k_clear_attention_tree<TYPE, DIM, SCORE, 1>, TreeLds<DIM, 1>::BYTES);
+        else if (rt == 2) go(k_clear_attention_tree<TYPE, DIM, SCORE, 2>, TreeLds<DIM, 2>::BYTES);
+        else if constexpr (DIM <= 128) go(k_clear_attention_tree<TYPE, DIM, SCORE, 4>, TreeLds<DIM, 4>::BYTES);
     }
     if (splits == 1) return;
     ScopedTimer timer(ctx, "k_clear_attention_tree_join", st);
     const int rows = min(16, v.s.max_new * v.group);
-    hipLaunchKernelGGL((k_clear_attention_tree_join<TYPE, DIM, SCORE>), dim3(heads * v.row_tiles, rows, v.s.seqs), dim3(256), 0, st, v, parents, split_tiles);
+    hipLaunchKernelGGL((k_clear_attention_tree_join<TYPE, DIM, SCORE>), dim3(heads * v.row_tiles, (rows + 3) / 4, v.s.seqs), dim3(256), 0, st, v, parents, split_tiles);
 }
 
 template <int TYPE, int SCORE>

@@ -215,7 +215,7 @@ struct StageSlot {
     bool pending = false;
 };
 #define ENSI_STAGE_SLOTS 8
-#define CLEAR_LDS_KERNELS 64
+#define CLEAR_LDS_KERNELS 128
 
 // Two words of a ciphertext at a time.  Wrapped batches are u64 arrays of the caller, aligned to a word and no more: these
 // may be read and written in one access all the same, but not by a type that claims 16 bytes.
