@@ -246,6 +246,15 @@ __device__ __forceinline__ float half_lift(float from, float to) { return from =
 
 #define JOIN_MAX 256  // parts of a row that a join takes
 
+// A tile of 64 keys and their values in LDS, widened to 16 bits
+template <int DIM>
+struct RowsLds {
+    static constexpr int KEYS = 64, K_ROW = DIM * 2 + 16, V_ROW = KEYS * 2 + 16;  // bytes; 16 more keep the rows of a fragment on different banks,
+    // and the chunks of 8 keys of a row of values are permuted with the row's number by 16, which does so for the rows, 4 apart, that a wave writes
+    static constexpr int K_BYTES = KEYS * K_ROW, V_BYTES = DIM * V_ROW, BUFFER = K_BYTES + V_BYTES;
+    static constexpr int BUFFERS = 2 * BUFFER <= 80 * 1024 ? 2 : 1;
+};
+
 inline AttentionView attention_view(ensi_ctx *ctx, const KvView &kv, const ensi_clear_attention_args &a) {
     AttentionView v = {kv, a.s, a.q, a.out, a.q_stride, a.out_stride, a.q_heads, a.q_heads / kv.heads, a.window, a.max_length, a.cap, 0, 0, a.bias * LOG2E, 0, 0, ctx->ws_clear};
     const float root = 1.0f / sqrtf((float)kv.dim);

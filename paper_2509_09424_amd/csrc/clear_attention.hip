@@ -316,14 +316,6 @@ __global__ __launch_bounds__(256) void k_clear_attention_join(AttentionView a, i
 // LDS, values transposed and in the order in which the score's registers hold their keys; two buffers, one barrier a tile.  Matrix instructions (48 a wave and tile at
 // 128 places, a third of them for the weights' second term: 258 us without it, 317 with it for 2048 + 4096 tokens of 20 over 5 heads) and the softmax's vector
 // instructions (three more a weight for the two terms) decide; LDS reads are 32 KB a wave and tile.
-template <int DIM>
-struct RowsLds {
-    static constexpr int KEYS = 64, K_ROW = DIM * 2 + 16, V_ROW = KEYS * 2 + 16;  // bytes; 16 more keep the rows of a fragment on different banks,
-    // and the chunks of 8 keys of a row of values are permuted with the row's number by 16, which does so for the rows, 4 apart, that a wave writes
-    static constexpr int K_BYTES = KEYS * K_ROW, V_BYTES = DIM * V_ROW, BUFFER = K_BYTES + V_BYTES;
-    static constexpr int BUFFERS = 2 * BUFFER <= 80 * 1024 ? 2 : 1;
-};
-
 template <int TYPE, int DIM, int SCORE, bool CAP>
 __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_rows(AttentionView a) {
     typedef typename Elem<TYPE>::type T;

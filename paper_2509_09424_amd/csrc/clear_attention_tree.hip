@@ -58,7 +58,6 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
     typedef typename W::vec vec;
     typedef TreeLds<DIM, RT> L;
     constexpr int STEPS = DIM / 32, TILES = DIM / 16, PIECE = Split<DIM>::PIECE, REST = Split<DIM>::REST, MAIN = Split<DIM>::MAIN;
-    constexpr bool VALUES_AHEAD = RT == 4;  // one wave to a SIMD in any case
     extern __shared__ __align__(16) float tree_lds[];
     __shared__ u64 lines[TREE_MAX];
     __shared__ int places[TREE_MAX];
@@ -147,9 +146,8 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                 }
             }
         };
-        Codes now, next;
+        Codes now;
         fetch_keys(now, 0);
-        if (VALUES_AHEAD) fetch_values(now, 0);
         for (int i = 0; i < turns; i++) {
             const int key0 = keys.lo + 32 * (batch + 4 * i);
             int good[2];
@@ -161,18 +159,15 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                 vs[h] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 2 * i + h));
                 lv[h] = SCORE == ENSI_SCORE_SIGMOID ? 0 : __builtin_amdgcn_logf(vs[h]);
             }
-            if (!VALUES_AHEAD) fetch_values(now, i);
+            fetch_values(now, i);
             const bool masked = key0 + 31 >= part.ctx || (a.window > 0 && key0 <= keys.last - a.window) || !good[0] || !good[1];
             vec k[2][STEPS];
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int s = 0; s < STEPS; s++) k[h][s] = W::widen(now.k[h][s][0], now.k[h][s][1]);
-            // the next tile's keys are under way while this one is computed, its values too where they fit the registers
-            if (i + 1 < turns) {
-                fetch_keys(now, i + 1);
-                if (VALUES_AHEAD) fetch_values(next, i + 1);
-            }
+            // the next tile's keys are under way while this one is computed (its values too would not fit two waves' registers)
+            if (i + 1 < turns) fetch_keys(now, i + 1);
             Weights p[RT];
 #pragma unroll
             for (int rt = 0; rt < RT; rt++) {
@@ -273,13 +268,6 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                     }
                 }
             }
-            if (VALUES_AHEAD)
-#pragma unroll
-                for (int h = 0; h < 2; h++)
-#pragma unroll
-                    for (int x = 0; x < WORDS; x++)
-#pragma unroll
-                        for (int r = 0; r < 4; r++) now.v[h][x][r] = next.v[h][x][r];
         }
     }
     for (int key = nan_from; key <= min(nan_to, keys.last); key++) {
@@ -366,6 +354,343 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
     }
 }
 
+// Many rows: 32 RW of them to a workgroup, 32 to a wave, and tiles of 64 keys widened once for all of them in LDS (RowsLds; a wave fetches and widens a block of 16 keys and values while
+// the tile before is computed).  With 64 rows two waves have the same ones, and half of a tile's keys each.
+template <int TYPE, int DIM, int SCORE, int RW>
+__global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tree_rows(AttentionView a, const int32_t *parents, int split_tiles) {
+    typedef typename Elem<TYPE>::type T;
+    typedef Wide<TYPE> W;
+    typedef typename W::vec vec;
+    typedef RowsLds<DIM> L;
+    constexpr int STEPS = DIM / 16, TILES = DIM / 32, ITEMS = (DIM / 2 + 63) / 64;  // of the values: 8 keys x 4 places
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ int nan_tiles[2];  // first and last tile whose values had NaN
+    __shared__ u64 lines[TREE_MAX];
+    __shared__ int places[TREE_MAX];
+    constexpr int HALVES = RW / 2;  // of a tile's keys to a wave
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 32, half = lane / 32;
+    const int row_wave = wave % RW, b0 = 2 * HALVES * (wave / RW);  // the wave's rows, and the first of its blocks of 16 keys
+    const int blocks = (a.row_tiles + 2 * RW - 1) / (2 * RW);
+    const int seq = blockIdx.z, head = blockIdx.x / blocks, block_row = 32 * RW * (blockIdx.x % blocks), split = blockIdx.y;
+    const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
+    const int rows = part.count * a.group;
+    const TreeKeys keys = tree_keys(part, a.window);
+    const int tile0 = split * split_tiles, tile1 = min(tile0 + split_tiles, keys.tiles);  // of 32 keys, two of which are a tile here
+    if (block_row >= rows || tile0 >= tile1) return;
+    const int row0 = block_row + 32 * row_wave, lo = keys.lo + 32 * tile0, tiles = (tile1 - tile0 + 1) / 2;
+    const int row = min(row0 + n, rows - 1), index = row / a.group, token = part.first + index;
+    const int q_head = head * a.group + row % a.group;
+    vec q[STEPS];
+    {
+        typedef vec loose __attribute__((aligned(2)));
+        const T *p = (const T *)a.q + (int64_t)token * a.q_stride + (int64_t)q_head * DIM + 8 * half;
+#pragma unroll
+        for (int s = 0; s < STEPS; s++) q[s] = *(const loose *)(p + 16 * s);
+    }
+    f32x16 o[TILES];
+#pragma unroll
+    for (int j = 0; j < TILES; j++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) o[j][r] = 0;
+    float st_m = -__builtin_inff(), st_l = 0;
+    // what 16 tiles need to know of their blocks of 16 keys: lane l has block l % 4 of tile l / 4
+    int my_block = 0, my_good = 0;
+    float my_k = 1, my_v = 1;
+    const auto look_up = [&](int first) {
+        const int key = lo + 64 * first + 16 * lane;
+        my_block = my_good = 0;
+        my_k = my_v = 1;
+        if (key < keys.lo + 32 * tile1 && key <= keys.last && (a.window <= 0 || key + KV_BLOCK - 1 > part.ctx - a.window)) {
+            const int block = block_of(a, seq, head, key);
+            if (block >= 0) {
+                my_block = block;
+                my_good = 1;
+                my_k = a.kv.ks[block];
+                my_v = fmaxf(a.kv.vs[block], 0x1p-64f);
+            } else
+                atomicOr(a.kv.status, ENSI_KV_BAD_PAGE);
+        }
+    };
+    // a wave's block of a tile: keys, DIM / 4 bytes of row lane / 4; values, items (half of the block's keys, 4 places)
+    u32x2 kc[DIM / 32];
+    u32 vc[ITEMS][8];
+    const auto fetch = [&](int t) {
+        const int64_t block = __builtin_amdgcn_readlane(my_block, 4 * (t % 16) + wave);
+        const unsigned char *k = a.kv.k + block * (KV_BLOCK * DIM), *v = a.kv.v + block * (KV_BLOCK * DIM);
+#pragma unroll
+        for (int i = 0; i < DIM / 32; i++) kc[i] = *(const u32x2 *)(k + (u32)(lane * (DIM / 4) + 8 * i));
+#pragma unroll
+        for (int i = 0; i < ITEMS; i++) {
+            const int item = lane + 64 * i, h = item / (DIM / 4), places = 4 * (item % (DIM / 4));
+            if (DIM / 2 % 64 == 0 || item < DIM / 2) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) vc[i][e] = *(const u32 *)(v + (u32)((4 * h + 8 * (e / 4) + e % 4) * DIM + places));
+            }
+        }
+    };
+    const auto put = [&](int t) {
+        unsigned char *at = lds + (L::BUFFERS == 2 ? t % 2 * L::BUFFER : 0);
+        unsigned char *k = at + (16 * wave + lane / 4) * L::K_ROW + (lane % 4) * (DIM / 2);
+#pragma unroll
+        for (int i = 0; i < DIM / 32; i++) *(vec *)(k + 16 * i) = W::widen(kc[i][0], kc[i][1]);
+        u32 nans = 0;
+#pragma unroll
+        for (int i = 0; i < ITEMS; i++)
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (DIM / 2 % 64 == 0 || lane + 64 * i < DIM / 2) nans |= nan_bytes(vc[i][e]);
+        if (__any((nans & 0x80808080) != 0)) {
+            bool inside = false;  // of a token of the sequence, not of what lies behind its end
+#pragma unroll
+            for (int i = 0; i < ITEMS; i++) {
+                const int item = lane + 64 * i, h = item / (DIM / 4);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const u32 hit = item < DIM / 2 ? nan_bytes(vc[i][e]) & 0x80808080 : 0;
+                    inside |= hit && lo + 64 * t + 16 * wave + 4 * h + 8 * (e / 4) + e % 4 <= keys.last;
+                    vc[i][e] &= ~((hit >> 7) * 0xff);
+                }
+            }
+            if (inside) {
+                atomicMin(&nan_tiles[0], t);
+                atomicMax(&nan_tiles[1], t);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; i++) {
+            const int item = lane + 64 * i, h = item / (DIM / 4), places = 4 * (item % (DIM / 4));
+            if (DIM / 2 % 64 == 0 || item < DIM / 2) {
+                u32 x[2][4];
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e / 4][e % 4] = vc[i][e];
+                transpose4(x[0]);
+                transpose4(x[1]);
+#pragma unroll
+                for (int j = 0; j < 4; j++) *(bf16x8 *)(at + L::K_BYTES + (places + j) * L::V_ROW + 16 * ((2 * wave + h) ^ (places / 16 % 4))) = Wide<ENSI_T_BF16>::widen(x[0][j], x[1][j]);
+            }
+        }
+    };
+    if (threadIdx.x == 0) {
+        nan_tiles[0] = INT32_MAX;
+        nan_tiles[1] = -1;
+    }
+    look_up(0);
+    fetch(0);
+    // lines and positions, where a tile has new tokens or the edge of a window (what is left out for its tree is left out by those workgroups and the join)
+    if (keys.lo + 32 * tile1 > part.ctx || a.window > 0) {
+        const Tree tree = tree_of(parents, part, a.kv.status);
+        if (!tree.good) return;
+        if (wave == 0) {
+            lines[lane] = near_line(tree.line, a.window);
+            places[lane] = part.ctx + tree.depth;
+        }
+    }
+    __syncthreads();
+    put(0);
+    __syncthreads();
+    for (int t = 0; t < tiles; t++) {
+        const int key0 = lo + 64 * t;
+        int good[2 * HALVES];
+        float ks[2 * HALVES], vs[2 * HALVES];
+#pragma unroll
+        for (int b = 0; b < 2 * HALVES; b++) {
+            good[b] = __builtin_amdgcn_readlane(my_good, 4 * (t % 16) + b0 + b);
+            ks[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), 4 * (t % 16) + b0 + b));
+            vs[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 4 * (t % 16) + b0 + b));
+        }
+        if (t + 1 < tiles) {
+            if ((t + 1) % 16 == 0) look_up(t + 1);
+            fetch(t + 1);
+        }
+        if (row0 < rows) {
+            const unsigned char *at = lds + (L::BUFFERS == 2 ? t % 2 * L::BUFFER : 0);
+            // fragments of AHEAD steps under way: left to itself, the compiler keeps two reads under way, and a wave waits for LDS most of its time
+            f32x16 qk[HALVES];
+            constexpr int AHEAD = STEPS < 4 ? STEPS : 4;
+            vec kf[AHEAD][HALVES];
+            const auto read_keys = [&](int s) {
+#pragma unroll
+                for (int x = 0; x < HALVES; x++) kf[s % AHEAD][x] = *(const vec *)(at + (16 * b0 + 32 * x + n) * L::K_ROW + 32 * s + 16 * half);
+            };
+#pragma unroll
+            for (int s = 0; s < AHEAD; s++) read_keys(s);
+#pragma unroll
+            for (int x = 0; x < HALVES; x++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) qk[x][r] = 0;
+#pragma unroll
+            for (int s = 0; s < STEPS; s++) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int x = 0; x < HALVES; x++) qk[x] = W::mfma32(kf[s % AHEAD][x], q[s], qk[x]);
+                if (s + AHEAD < STEPS) read_keys(s + AHEAD);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            // register r of half x, block b = 2 x + r / 8: key 16 b + 8 (r % 8 / 4) + 4 half + r % 4 of the wave's
+            bool masked = key0 + 63 >= part.ctx || (a.window > 0 && key0 <= keys.last - a.window);
+            float u[2 * HALVES][8], most = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+#pragma unroll
+            for (int b = 0; b < 2 * HALVES; b++) {
+                masked |= !good[b];
+#pragma unroll
+                for (int e = 0; e < 8; e++) u[b][e] = qk[b / 2][8 * (b % 2) + e];
+            }
+            // softmax without a cap: the product itself, its factor enters with the exponent
+            const bool scaled = a.cap > 0 || SCORE == ENSI_SCORE_SIGMOID;
+            if (a.cap > 0) scores_of<SCORE, true>(u, ks, a);
+            else if (SCORE == ENSI_SCORE_SIGMOID) scores_of<SCORE, false>(u, ks, a);
+            if (SCORE == ENSI_SCORE_SIGMOID)
+#pragma unroll
+                for (int b = 0; b < 2 * HALVES; b++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) u[b][e] = vs[b] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[b][e]));
+            if (masked) {
+                const u64 line = lines[index];
+                const int place = places[index];
+#pragma unroll
+                for (int x = 0; x < HALVES; x++) {
+                    u32 seen = seen_keys(part, a.window, line, place, key0 + 16 * b0 + 32 * x);
+                    seen &= (good[2 * x] ? 0xffffu : 0) | (good[2 * x + 1] ? 0xffff0000u : 0);
+                    seen >>= 4 * half;
+#pragma unroll
+                    for (int b = 0; b < 2; b++)
+#pragma unroll
+                        for (int e = 0; e < 8; e++) u[2 * x + b][e] = seen >> (16 * b + 8 * (e / 4) + e % 4) & 1 ? u[2 * x + b][e] : SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+                }
+            }
+            float factor[2 * HALVES], lv[2 * HALVES];
+#pragma unroll
+            for (int b = 0; b < 2 * HALVES; b++) {
+                factor[b] = scaled ? 1.0f : a.factor * ks[b];
+                lv[b] = __builtin_amdgcn_logf(vs[b]);
+                const float top = most_of(most_of(most_of(u[b][0], u[b][1], u[b][2]), u[b][3], u[b][4]), most_of(u[b][5], u[b][6], u[b][7]));
+                most = most_of(most, SCORE == ENSI_SCORE_SOFTMAX ? __builtin_fmaf(top, factor[b], lv[b]) : top);
+            }
+            most = most_of(most, __shfl_xor(most, 32));
+            if (SCORE == ENSI_SCORE_SIGMOID) most = most_of(__builtin_amdgcn_logf(most), -120.0f);
+            const float m = most_of(st_m, most), base = m == -__builtin_inff() ? 0.0f : m;
+            const float lift = half_lift(st_m, base);
+            st_m = m;
+            if (__any(lift != 1.0f)) {
+                const bool deep = __any(lift < HALF_LIFT_DEEP);
+                const auto scale = [&](float f) {
+#pragma unroll
+                    for (int j = 0; j < TILES; j++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++) o[j][r] *= f;
+                };
+                if (deep) scale(lift);
+                scale(deep ? lift : lift * lift);
+                st_l = st_l * lift * lift;
+            }
+            // A block of 16 keys at a time: its values are read and its weights formed while the matrix cores have the block before (the weights of all four in two terms
+            // would not fit the registers at 128 places).
+            bf16x8 vf[2][TILES];
+            const auto read_values = [&](int b) {
+#pragma unroll
+                for (int j = 0; j < TILES; j++) vf[b % 2][j] = *(const bf16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 16 * ((2 * (b0 + b) + half) ^ (2 * (j % 2) + n / 16)));
+            };
+            const float unit = __builtin_amdgcn_exp2f(0.5f * (WEIGHT_LIFT - base));  // sigmoid: half of the way to the reference
+            Weights p[2];
+            const auto weigh = [&](int b) {
+                Weights &to = p[b % 2];
+                if (SCORE == ENSI_SCORE_SIGMOID) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) to.set(e, u[b][e] * unit * unit, u[b][e + 1] * unit * unit);
+                } else {
+                    const float scale = scale_of_terms(vs[b]);
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e], factor[b], TERM_LIFT - base)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[b][e + 1], factor[b], TERM_LIFT - base));
+                        st_l = add_terms(st_l, e0, e1);
+                        to.set(e, e0 * scale, e1 * scale);
+                    }
+                }
+            };
+            read_values(0);
+            __builtin_amdgcn_sched_barrier(0);
+            weigh(0);
+#pragma unroll
+            for (int b = 0; b < 2 * HALVES; b++) {
+                if (b + 1 < 2 * HALVES) read_values(b + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < TILES; j++) o[j] = Wide<ENSI_T_BF16>::mfma32(vf[b % 2][j], p[b % 2].hi.v, o[j]);
+#pragma unroll
+                for (int j = 0; j < TILES; j++) o[j] = Wide<ENSI_T_BF16>::mfma32(vf[b % 2][j], p[b % 2].lo.v, o[j]);
+                if (b + 1 < 2 * HALVES) weigh(b + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (L::BUFFERS == 1) __syncthreads();  // everybody has read this tile
+        if (t + 1 < tiles) put(t + 1);
+        __syncthreads();
+    }
+    if (nan_tiles[1] >= 0 && b0 == 0)
+        for (int key = lo + 64 * nan_tiles[0]; key <= min(lo + 64 * nan_tiles[1] + 63, keys.last); key++) {
+            const int block = block_of(a, seq, head, key);
+            if (block < 0 || !(seen_keys(part, a.window, lines[index], places[index], key) & 1)) continue;
+            const unsigned char *v = a.kv.v + ((int64_t)block * KV_BLOCK + key % KV_BLOCK) * DIM + 4 * half;
+#pragma unroll
+            for (int j = 0; j < TILES; j++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    if (is_nan(v[32 * j + 8 * (r / 4) + r % 4])) o[j][r] = __builtin_nanf("");
+        }
+    st_l += __shfl_xor(st_l, 32);
+    if (RW == 2) {
+        // the other half's sums, of waves with the same rows
+        float *const to = (float *)lds + (row_wave * 64 + lane) * 4, *const ml = (float *)lds + 2 * 64 * 16 * TILES + (row_wave * 64 + lane) * 2;
+        if (b0 > 0) {
+#pragma unroll
+            for (int j = 0; j < TILES; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) *(f32x4 *)(to + (4 * j + e) * 512) = (f32x4){o[j][4 * e], o[j][4 * e + 1], o[j][4 * e + 2], o[j][4 * e + 3]};
+            ml[0] = st_m;
+            ml[1] = st_l;
+        }
+        __syncthreads();
+        if (b0 > 0) return;
+        const float om = ml[0], m = most_of(st_m, om), base = m == -__builtin_inff() ? 0.0f : m;
+        const float h0 = half_lift(st_m, base), h1 = half_lift(om, base);
+#pragma unroll
+        for (int j = 0; j < TILES; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const f32x4 v = *(const f32x4 *)(to + (4 * j + e) * 512);
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[j][4 * e + i] = o[j][4 * e + i] * h0 * h0 + v[i] * h1 * h1;
+            }
+        st_l = st_l * h0 * h0 + ml[1] * h1 * h1;
+        st_m = m;
+    }
+    if (row0 + n >= rows) return;
+    if (keys.tiles > split_tiles) {
+        float *ws = a.ws + ((((int64_t)seq * a.kv.heads + head) * a.row_tiles + row / 16) * a.splits + split) * (16 * DIM + 32);
+#pragma unroll
+        for (int j = 0; j < TILES; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) *(f32x4 *)(ws + row % 16 * DIM + 32 * j + 8 * e + 4 * half) = (f32x4){o[j][4 * e], o[j][4 * e + 1], o[j][4 * e + 2], o[j][4 * e + 3]};
+        if (half == 0) {
+            ws[16 * DIM + row % 16] = st_m;
+            ws[16 * DIM + 16 + row % 16] = st_l;
+        }
+        return;
+    }
+    const Last end = last_of<SCORE>(st_m, st_l, [&] { return sees_any_of(a, seq, part, lines[index], places[index]); });
+    T *out = (T *)a.out + (int64_t)token * a.out_stride + (int64_t)q_head * DIM;
+#pragma unroll
+    for (int j = 0; j < TILES; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            typedef T quad __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            quad w;
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = (T)end(o[j][4 * e + i]);
+            *(quad *)(out + 32 * j + 8 * e + 4 * half) = w;
+        }
+}
+
 // Joins the parts of a row, a wave to a row: the references first, a lane to a part, then the outputs, DIM / 4 lanes to a part and as many parts side by side as
 // there are lanes.
 #define TREE_SPLITS 64
@@ -393,14 +718,19 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree_join(AttentionView
     for (int k = 1; k < 64; k *= 2) l += __shfl_xor(l, k);
     f32x4 o = {0, 0, 0, 0};
     const int quad = lane % QUADS, slice = lane / QUADS;
-#pragma unroll 4
-    for (int s = 0; s < splits; s += SLICES) {
-        const int mine = s + slice;
-        const float f = __shfl(h, mine & 63);
-        if (slice < SLICES && mine < splits) {
-            const f32x4 v = *(const f32x4 *)(ws + (int64_t)mine * (16 * DIM + 32) + n * DIM + 4 * quad);
+    constexpr int AHEAD = 8;
+    for (int s = 0; s < splits; s += AHEAD * SLICES) {
+        f32x4 v[AHEAD];
+        // (the last part in place of those behind it, which do not count)
 #pragma unroll
-            for (int i = 0; i < 4; i++) o[i] = __builtin_fmaf(v[i] * f, f, o[i]);
+        for (int e = 0; e < AHEAD; e++) v[e] = *(const f32x4 *)(ws + (int64_t)min(s + e * SLICES + slice, splits - 1) * (16 * DIM + 32) + n * DIM + 4 * quad);
+#pragma unroll
+        for (int e = 0; e < AHEAD; e++) {
+            const int mine = s + e * SLICES + slice;
+            const float f = __shfl(h, mine & 63);
+            if (slice < SLICES && mine < splits)
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[i] = __builtin_fmaf(v[e][i] * f, f, o[i]);
         }
     }
 #pragma unroll
@@ -421,14 +751,22 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree_join(AttentionView
     *(quad_t *)((T *)a.out + (int64_t)(part.first + index) * a.out_stride + (int64_t)q_head * DIM + 4 * quad) = w;
 }
 
+// Waves of rows to a workgroup where keys are shared through LDS, 0 where every wave has its own
+static int tree_by_rows(const AttentionView &v, int rows) {
+#ifdef TREE_NO_ROWS
+    return 0;
+#endif
+    return rows > 64 ? 4 : rows > 32 ? 2 : 0;
+}
+
 template <int TYPE, int DIM, int SCORE>
 static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipStream_t st) {
     const int heads = v.kv.heads;
     const int span = v.window > 0 ? (int)min((int64_t)v.max_length, (int64_t)v.window + v.s.max_new - 1 + 31) : v.max_length;
     v.row_tiles = (v.s.max_new * v.group + 15) / 16;
     const int tiles = (span + 31) / 32;
-    const int rt = v.row_tiles == 1 ? 1 : v.row_tiles == 2 || DIM > 128 ? 2 : 4;
-    const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + rt - 1) / rt);
+    const int rows = v.s.max_new * v.group, rw = tree_by_rows(v, rows), rt = v.row_tiles == 1 ? 1 : 2, width = rw ? 2 * rw : rt;  // tiles of 16 rows to a workgroup
+    const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + width - 1) / width);
     int splits = max((tiles + 31) / 32, base < 256 && tiles > 16 ? (int)(512 / base) : 1);
     splits = min(splits, min((tiles + 3) / 4, TREE_SPLITS));
     splits = max(splits, 1);
@@ -442,16 +780,18 @@ static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipS
         ScopedTimer timer(ctx, "k_clear_attention_tree", st);
         const auto go = [&](auto kernel, int bytes) {
             if (bytes > 48 * 1024) clear_lds(ctx, (const void *)kernel, bytes);
-            hipLaunchKernelGGL(kernel, dim3(heads * ((v.row_tiles + rt - 1) / rt), splits, v.s.seqs), dim3(256), bytes, st, v, parents, split_tiles);
+            hipLaunchKernelGGL(kernel, dim3(heads * ((v.row_tiles + width - 1) / width), splits, v.s.seqs), dim3(256), bytes, st, v, parents, split_tiles);
         };
-        if (rt == 1) go(k_clear_attention_tree<TYPE, DIM, SCORE, 1>, TreeLds<DIM, 1>::BYTES);
-        else if (rt == 2) go(k_clear_attention_tree<TYPE, DIM, SCORE, 2>, TreeLds<DIM, 2>::BYTES);
-        else if constexpr (DIM <= 128) go(k_clear_attention_tree<TYPE, DIM, SCORE, 4>, TreeLds<DIM, 4>::BYTES);
+        constexpr int rows_bytes = RowsLds<DIM>::BUFFERS * RowsLds<DIM>::BUFFER;
+        static_assert(rows_bytes >= 2 * 64 * (DIM / 32 * 16 + 2) * 4, "two waves' sums");
+        if (rw == 4) go(k_clear_attention_tree_rows<TYPE, DIM, SCORE, 4>, rows_bytes);
+        else if (rw == 2) go(k_clear_attention_tree_rows<TYPE, DIM, SCORE, 2>, rows_bytes);
+        else if (rt == 1) go(k_clear_attention_tree<TYPE, DIM, SCORE, 1>, TreeLds<DIM, 1>::BYTES);
+        else go(k_clear_attention_tree<TYPE, DIM, SCORE, 2>, TreeLds<DIM, 2>::BYTES);
     }
     if (splits == 1) return;
     ScopedTimer timer(ctx, "k_clear_attention_tree_join", st);
-    const int rows = min(16, v.s.max_new * v.group);
-    hipLaunchKernelGGL((k_clear_attention_tree_join<TYPE, DIM, SCORE>), dim3(heads * v.row_tiles, (rows + 3) / 4, v.s.seqs), dim3(256), 0, st, v, parents, split_tiles);
+    hipLaunchKernelGGL((k_clear_attention_tree_join<TYPE, DIM, SCORE>), dim3(heads * v.row_tiles, (min(rows, 16) + 3) / 4, v.s.seqs), dim3(256), 0, st, v, parents, split_tiles);
 }
 
 template <int TYPE, int SCORE>
