@@ -753,9 +753,6 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree_join(AttentionView
 
 // Waves of rows to a workgroup where keys are shared through LDS, 0 where every wave has its own
 static int tree_by_rows(const AttentionView &v, int rows) {
-#ifdef TREE_NO_ROWS
-    return 0;
-#endif
     return rows > 64 ? 4 : rows > 32 ? 2 : 0;
 }
 
@@ -767,9 +764,11 @@ static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipS
     const int tiles = (span + 31) / 32;
     const int rows = v.s.max_new * v.group, rw = tree_by_rows(v, rows), rt = v.row_tiles == 1 ? 1 : 2, width = rw ? 2 * rw : rt;  // tiles of 16 rows to a workgroup
     const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + width - 1) / width);
-    int splits = max((tiles + 31) / 32, base < 256 && tiles > 16 ? (int)(512 / base) : 1);
-    splits = min(splits, min((tiles + 3) / 4, TREE_SPLITS));
-    splits = max(splits, 1);
+    // Parts of a row's keys: up to 32 tiles each, which evens out sequences of different lengths; down to 12 while the workgroups are fewer than the CUs have room for, and down
+    // to 4, one for every wave, where CUs would stand idle.
+    int splits = max((tiles + 31) / 32, (int)min(1024 / base, (int64_t)tiles / 12));
+    if (base * splits < 256) splits = (int)min(512 / base, (int64_t)(tiles + 3) / 4);
+    splits = max(min(splits, TREE_SPLITS), 1);
     const int64_t room = (int64_t)CLEAR_WS_FLOATS / ((int64_t)v.s.seqs * heads * v.row_tiles * (16 * DIM + 32));
     if (splits > room) splits = (int)max((int64_t)1, room);
     int split_tiles = (tiles + splits - 1) / splits;
