@@ -190,9 +190,12 @@ def _handles(caches):
     if isinstance(caches, ClearCache):
         caches = (caches,)
     try:
-        return struct.pack("%dQ" % len(caches), *[c.h.value for c in caches])
+        handles = struct.pack("%dQ" % len(caches), *[c.h.value for c in caches])
     except (struct.error, AttributeError, TypeError):
-        raise EnsiError("caches must be a cache that is not freed, or a list of them") from None
+        handles = b""
+    if not handles:
+        raise EnsiError("caches must be a cache that is not freed, or a list of them")
+    return handles
 
 
 class Context:
