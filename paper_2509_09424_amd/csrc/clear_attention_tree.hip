@@ -45,6 +45,36 @@ __device__ __forceinline__ u64 near_line(u64 line, int window) {
     return line;
 }
 
+// Products q c to what the exponent takes, and the factor with which it takes them.  Softmax without a cap: the products as they are, a key's scale enters with the exponent.
+template <int SCORE, int B, int E>
+__device__ __forceinline__ void tree_scores(float (&u)[B][E], float (&factor)[B], const float (&ks)[B], const float (&vs)[B], const AttentionView &a) {
+    const bool capped = a.cap > 0;
+#pragma unroll
+    for (int b = 0; b < B; b++) factor[b] = a.factor * ks[b];
+    if (capped) {
+#pragma unroll
+        for (int b = 0; b < B; b++)
+#pragma unroll
+            for (int e = 0; e < E; e++) u[b][e] *= factor[b];
+        cap_scores(u, a.cap, a.cap_inv);
+#pragma unroll
+        for (int b = 0; b < B; b++) factor[b] = LOG2E;
+    }
+    if (SCORE == ENSI_SCORE_SIGMOID)
+#pragma unroll
+        for (int b = 0; b < B; b++)
+#pragma unroll
+            for (int e = 0; e < E; e++) u[b][e] = vs[b] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-__builtin_fmaf(u[b][e], factor[b], a.bias)));
+}
+// A lane's largest one of a block, against the reference: log2 of the weight, or the weight of the sigmoid
+template <int SCORE, int E>
+__device__ __forceinline__ float tree_most(const float (&u)[E], float factor, float log_v) {
+    float top = u[0];
+#pragma unroll
+    for (int e = 1; e < E; e++) top = most_of(top, u[e]);
+    return SCORE == ENSI_SCORE_SIGMOID ? top : __builtin_fmaf(top, factor, log_v);
+}
+
 template <int DIM, int RT>
 struct TreeLds {
     static constexpr int ROWS = 16 * RT, ROW = DIM + 4;  // floats of a row; 4 more put the rows that are written at once on different banks
@@ -183,13 +213,8 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                 for (int h = 0; h < 2; h++)
 #pragma unroll
                     for (int r = 0; r < 4; r++) u[h][r] = qk[h][r];
-                if (a.cap > 0) scores_of<SCORE, true>(u, ks, a);
-                else scores_of<SCORE, false>(u, ks, a);
-                if (SCORE == ENSI_SCORE_SIGMOID)
-#pragma unroll
-                    for (int h = 0; h < 2; h++)
-#pragma unroll
-                        for (int r = 0; r < 4; r++) u[h][r] = vs[h] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[h][r]));
+                float factor[2];
+                tree_scores<SCORE>(u, factor, ks, vs, a);
                 if (masked) {
                     u32 seen = seen_keys(part, a.window, lines[index[rt]], places[index[rt]], key0);
                     seen &= (good[0] ? 0xffffu : 0) | (good[1] ? 0xffff0000u : 0);
@@ -201,7 +226,7 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                 }
                 float most = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
 #pragma unroll
-                for (int h = 0; h < 2; h++) most = most_of(most, most_of(most_of(u[h][0], u[h][1], u[h][2]), u[h][3]) + lv[h]);
+                for (int h = 0; h < 2; h++) most = most_of(most, tree_most<SCORE>(u[h], factor[h], lv[h]));
                 most = most_of(most, __shfl_xor(most, 16));
                 most = most_of(most, __shfl_xor(most, 32));
                 if (SCORE == ENSI_SCORE_SIGMOID) most = most_of(__builtin_amdgcn_logf(most), -120.0f);
@@ -222,34 +247,37 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
                         if (SCORE == ENSI_SCORE_SIGMOID) {
                             p[rt].set(4 * h + r, u[h][r] * unit * unit, u[h][r + 1] * unit * unit);
                         } else {
-                            const float e0 = __builtin_amdgcn_exp2f(u[h][r] - (base - TERM_LIFT)), e1 = __builtin_amdgcn_exp2f(u[h][r + 1] - (base - TERM_LIFT)), scale = scale_of_terms(vs[h]);
+                            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[h][r], factor[h], TERM_LIFT - base)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(u[h][r + 1], factor[h], TERM_LIFT - base)), scale = scale_of_terms(vs[h]);
                             st[rt].l = add_terms(st[rt].l, e0, e1);
                             p[rt].set(4 * h + r, e0 * scale, e1 * scale);
                         }
                     }
             }
-            u32 nans = 0;
-#pragma unroll
-            for (int h = 0; h < 2; h++)
-#pragma unroll
-                for (int x = 0; x < WORDS; x++)
-#pragma unroll
-                    for (int r = 0; r < 4; r++) nans |= nan_bytes(now.v[h][x][r]);
-            if (__any((nans & 0x80808080) != 0)) {
-                bool inside = false;  // of a token of the sequence, not of what lies behind its end
+            // values that some row does not see: NaN among them is taken as 0 (elsewhere it finds its way through the products)
+            if (masked) {
+                u32 nans = 0;
 #pragma unroll
                 for (int h = 0; h < 2; h++)
 #pragma unroll
                     for (int x = 0; x < WORDS; x++)
 #pragma unroll
-                        for (int r = 0; r < 4; r++) {
-                            const u32 hit = nan_bytes(now.v[h][x][r]) & 0x80808080;
-                            inside |= hit && key0 + 16 * h + 4 * g + r <= keys.last;
-                            now.v[h][x][r] &= ~((hit >> 7) * 0xff);
-                        }
-                if (__any(inside)) {
-                    nan_from = min(nan_from, key0);
-                    nan_to = key0 + 31;
+                        for (int r = 0; r < 4; r++) nans |= nan_bytes(now.v[h][x][r]);
+                if (__any((nans & 0x80808080) != 0)) {
+                    bool inside = false;  // of a token of the sequence, not of what lies behind its end
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int x = 0; x < WORDS; x++)
+#pragma unroll
+                            for (int r = 0; r < 4; r++) {
+                                const u32 hit = nan_bytes(now.v[h][x][r]) & 0x80808080;
+                                inside |= hit && key0 + 16 * h + 4 * g + r <= keys.last;
+                                now.v[h][x][r] &= ~((hit >> 7) * 0xff);
+                            }
+                    if (__any(inside)) {
+                        nan_from = min(nan_from, key0);
+                        nan_to = key0 + 31;
+                    }
                 }
             }
 #pragma unroll
@@ -433,12 +461,14 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
         unsigned char *k = at + (16 * wave + lane / 4) * L::K_ROW + (lane % 4) * (DIM / 2);
 #pragma unroll
         for (int i = 0; i < DIM / 32; i++) *(vec *)(k + 16 * i) = W::widen(kc[i][0], kc[i][1]);
+        // values that some row does not see: NaN among them is taken as 0 (elsewhere it finds its way through the products)
         u32 nans = 0;
+        if (lo + 64 * t + 63 >= part.ctx || (a.window > 0 && lo + 64 * t <= keys.last - a.window) || !__builtin_amdgcn_readlane(my_good, 4 * (t % 16) + wave))
 #pragma unroll
-        for (int i = 0; i < ITEMS; i++)
+            for (int i = 0; i < ITEMS; i++)
 #pragma unroll
-            for (int e = 0; e < 8; e++)
-                if (DIM / 2 % 64 == 0 || lane + 64 * i < DIM / 2) nans |= nan_bytes(vc[i][e]);
+                for (int e = 0; e < 8; e++)
+                    if (DIM / 2 % 64 == 0 || lane + 64 * i < DIM / 2) nans |= nan_bytes(vc[i][e]);
         if (__any((nans & 0x80808080) != 0)) {
             bool inside = false;  // of a token of the sequence, not of what lies behind its end
 #pragma unroll
@@ -535,15 +565,8 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
 #pragma unroll
                 for (int e = 0; e < 8; e++) u[b][e] = qk[b / 2][8 * (b % 2) + e];
             }
-            // softmax without a cap: the product itself, its factor enters with the exponent
-            const bool scaled = a.cap > 0 || SCORE == ENSI_SCORE_SIGMOID;
-            if (a.cap > 0) scores_of<SCORE, true>(u, ks, a);
-            else if (SCORE == ENSI_SCORE_SIGMOID) scores_of<SCORE, false>(u, ks, a);
-            if (SCORE == ENSI_SCORE_SIGMOID)
-#pragma unroll
-                for (int b = 0; b < 2 * HALVES; b++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) u[b][e] = vs[b] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u[b][e]));
+            float factor[2 * HALVES], lv[2 * HALVES];
+            tree_scores<SCORE>(u, factor, ks, vs, a);
             if (masked) {
                 const u64 line = lines[index];
                 const int place = places[index];
@@ -558,13 +581,10 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
                         for (int e = 0; e < 8; e++) u[2 * x + b][e] = seen >> (16 * b + 8 * (e / 4) + e % 4) & 1 ? u[2 * x + b][e] : SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
                 }
             }
-            float factor[2 * HALVES], lv[2 * HALVES];
 #pragma unroll
             for (int b = 0; b < 2 * HALVES; b++) {
-                factor[b] = scaled ? 1.0f : a.factor * ks[b];
                 lv[b] = __builtin_amdgcn_logf(vs[b]);
-                const float top = most_of(most_of(most_of(u[b][0], u[b][1], u[b][2]), u[b][3], u[b][4]), most_of(u[b][5], u[b][6], u[b][7]));
-                most = most_of(most, SCORE == ENSI_SCORE_SOFTMAX ? __builtin_fmaf(top, factor[b], lv[b]) : top);
+                most = most_of(most, tree_most<SCORE>(u[b], factor[b], lv[b]));
             }
             most = most_of(most, __shfl_xor(most, 32));
             if (SCORE == ENSI_SCORE_SIGMOID) most = most_of(__builtin_amdgcn_logf(most), -120.0f);
