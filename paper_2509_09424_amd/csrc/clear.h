@@ -67,16 +67,17 @@ struct KvView {
 struct SeqPart {
     int first, count, ctx;  // first new token, number of them, tokens before them
 };
-__device__ __forceinline__ SeqPart seq_part(const ensi_clear_seqs &s, int seq, int page, int64_t most, int *status) {
+__device__ __forceinline__ SeqPart seq_part(const ensi_clear_seqs &s, int seq, int page, int64_t most, int *status, bool notes) {
     const int64_t b0 = s.begin[seq], b1 = s.begin[seq + 1], ctx = s.lengths[seq], n = b1 - b0;
     const bool ok = b0 >= 0 && n >= 0 && b1 <= s.tokens && n <= s.max_new && ctx >= 0 && ctx + n <= most && ctx + n <= (int64_t)s.table_width * page;
     SeqPart p = {(int)b0, (int)n, (int)ctx};
     if (!ok) {
-        if (threadIdx.x == 0) atomicOr(status, ENSI_KV_BAD_LENGTH);
+        if (notes) atomicOr(status, ENSI_KV_BAD_LENGTH);
         p.count = 0;
     }
     return p;
 }
+__device__ __forceinline__ SeqPart seq_part(const ensi_clear_seqs &s, int seq, int page, int64_t most, int *status) { return seq_part(s, seq, page, most, status, threadIdx.x == 0); }
 
 // A tree of a sequence's new tokens, a wave's width of them at most: each names an earlier one as its parent, or none (-1).  Lane t of a wave gets token t's line, the bits
 // of itself and its ancestors, in as many steps as the number of tokens has bits: every step adds the line of the first ancestor that is not in it yet.

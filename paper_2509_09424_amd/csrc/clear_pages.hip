@@ -39,17 +39,18 @@ __global__ __launch_bounds__(256) void k_clear_accept(ensi_clear_accept_args a) 
     }
 }
 
-// A wave: one sequence, one head of the keys or values of one cache.  Lane j looks after the j-th accepted token.  Blocks of 16 places are filled one after the other, each read
-// whole before it is written; tokens only move towards the front, so what a later block needs is not overwritten by then.
+// A wave: one sequence, one head of one cache, keys and values side by side.  Lane j looks after the j-th accepted token.  Blocks of 16 places are filled one after the other, each read
+// whole before it is written; tokens only move towards the front, so what a later block needs is not overwritten by then.  A chain of latencies (path, page, scale, codes) decides:
+// 64 sequences in 30 caches of 5 heads take 9600 waves, little more than the card holds at once.
 template <int ITEMS>
-__global__ __launch_bounds__(256) void k_clear_keep(CacheList list, ensi_clear_keep_args a) {
-    const KvView kv = list.kv[blockIdx.z];
+__global__ __launch_bounds__(256) void k_clear_keep(CacheList list, ensi_clear_keep_args a, int caches, int heads) {
     const int lane = threadIdx.x % 64, seq = blockIdx.y;
-    const int slot = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64);
-    if (slot >= 2 * kv.heads) return;
-    const bool is_k = slot < kv.heads;
-    const int head = is_k ? slot : slot - kv.heads, dim = kv.dim, chunks = dim / 16;
-    const SeqPart part = seq_part(a.s, seq, kv.page, 1 << 30, kv.status);
+    const int slot = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64), head = slot % heads;
+    if (slot >= caches * heads) return;
+    const KvView kv = list.kv[slot / heads];
+    if (head >= kv.heads) return;
+    const int dim = kv.dim, chunks = dim / 16;
+    const SeqPart part = seq_part(a.s, seq, kv.page, 1 << 30, kv.status, lane == 0);  // (a workgroup's waves may have different caches)
     const int count = a.count[seq];
     if (part.count == 0 && count == 0) return;
     int from = lane < min(max(count, 0), a.s.max_new) ? a.path[seq * a.path_stride + lane] : INT32_MAX;
@@ -63,71 +64,88 @@ __global__ __launch_bounds__(256) void k_clear_keep(CacheList list, ensi_clear_k
     const u64 moves = __ballot(lane < count && from != lane);
     if (!moves) return;
     const int first = __ffsll((unsigned long long)moves) - 1;  // tokens before it stay where they are
-    // the lane's token: the row of the cache that it lies in, and its block's scale
-    int64_t src = 0;
-    float scale = 0;
-    bool good = true;
-    unsigned char *codes = is_k ? kv.k : kv.v;
-    float *scales = is_k ? kv.ks : kv.vs;
     const auto block_of = [&](int place) -> int64_t {  // of 16 rows; -1: its page is outside the cache
         const int page = a.s.table[seq * a.s.table_stride + place / kv.page];
         if (page < 0 || page >= kv.pages) return -1;
         return (((int64_t)page * kv.heads + head) * kv.page + place % kv.page) / KV_BLOCK;
     };
+    // the lane's token: the block that it lies in (a cache has fewer than 2^31) with its scales; and lane b's, the b-th block that tokens come to (5 at most)
+    const int block0 = (part.ctx + first) / KV_BLOCK, block1 = (part.ctx + count - 1) / KV_BLOCK;
+    int src = 0, dst = 0;
+    bool good = true;
+    float scale[2] = {0, 0}, was[2] = {0, 0};
     if (lane >= first && lane < count) {
         const int64_t block = block_of(part.ctx + from);
         good = block >= 0;
         if (good) {
-            src = block * KV_BLOCK + (part.ctx + from) % KV_BLOCK;
-            scale = scales[block];
+            src = (int)block;
+            scale[0] = kv.ks[block];
+            scale[1] = kv.vs[block];
         }
     }
-    // all or nothing: the pages that tokens come to, too
-    const int block0 = (part.ctx + first) / KV_BLOCK, block1 = (part.ctx + count - 1) / KV_BLOCK;
-    if (lane <= block1 - block0 && block_of((block0 + lane) * KV_BLOCK) < 0) good = false;
-    if (!__all(good)) {
+    if (lane <= block1 - block0) {
+        const int64_t block = block_of((block0 + lane) * KV_BLOCK);
+        good = good && block >= 0;
+        if (block >= 0) {
+            dst = (int)block;
+            was[0] = kv.ks[block];
+            was[1] = kv.vs[block];
+        }
+    }
+    if (!__all(good)) {  // all or nothing
         if (lane == 0) atomicOr(kv.status, ENSI_KV_BAD_PAGE);
         return;
     }
+    const int line = (part.ctx + from) % KV_BLOCK;  // of its block
     for (int b = block0; b <= block1; b++) {
         const int start = b * KV_BLOCK, j0 = max(first, start - part.ctx), j1 = min(count, start + KV_BLOCK - part.ctx);  // tokens that arrive in the block
         const int stay = max(0, part.ctx + first - start);                                                               // of its tokens
-        const int64_t block = block_of(start);
-        const float old = scales[block];
-        float most = lane >= j0 && lane < j1 ? scale : stay > 0 ? old : 0.0f;
+        const int64_t block = __builtin_amdgcn_readlane(dst, b - block0);
+        float old[2], most[2];
 #pragma unroll
-        for (int k = 1; k < 64; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
-        const auto ratio_of = [&](float s) { return s == most ? 1.0f : s / most; };
-        const auto again = [&](u32x4 w, float ratio) {
-            if (ratio != 1.0f)
+        for (int c = 0; c < 2; c++) {
+            old[c] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, was[c]), b - block0));
+            most[c] = lane >= j0 && lane < j1 ? scale[c] : stay > 0 ? old[c] : 0.0f;
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const u32 u = w[k];
-                    w[k] = to_e4m3(__builtin_amdgcn_cvt_f32_fp8(u, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8(u, 1) * ratio, __builtin_amdgcn_cvt_f32_fp8(u, 2) * ratio,
-                                   __builtin_amdgcn_cvt_f32_fp8(u, 3) * ratio);
-                }
-            return w;
-        };
+            for (int k = 1; k < 64; k *= 2) most[c] = fmaxf(most[c], __shfl_xor(most[c], k));
+        }
         // chunks of 16 codes: of the tokens that arrive, and of those that stay where their scale grows
-        const int arrive = (j1 - j0) * chunks, kept = stay > 0 && old != most ? stay * chunks : 0;
-        u32x4 w[ITEMS];
-        float ratio[ITEMS];
+        const int arrive = (j1 - j0) * chunks, kept = stay > 0 && (old[0] != most[0] || old[1] != most[1]) ? stay * chunks : 0;
+        u32x4 w[2][ITEMS];
+        float ratio[2][ITEMS];
 #pragma unroll
         for (int i = 0; i < ITEMS; i++) {
-            const int item = lane + 64 * i, j = j0 + item / chunks;
-            const u32 src_lo = __shfl((u32)src, j & 63), src_hi = __shfl((u32)(src >> 32), j & 63);
-            const float s = __shfl(scale, j & 63);
-            ratio[i] = ratio_of(item < arrive ? s : old);
-            const int64_t row = item < arrive ? (int64_t)src_hi << 32 | src_lo : block * KV_BLOCK + (item - arrive) / chunks;
-            if (item < arrive + kept) w[i] = *(const u32x4 *)(codes + row * dim + 16 * ((item < arrive ? item : item - arrive) % chunks));
+            const int item = lane + 64 * i, j = (j0 + item / chunks) & 63;
+            const int64_t at = __shfl(src, j);
+            const int from_line = __shfl(line, j);
+            const int64_t row = item < arrive ? at * KV_BLOCK + from_line : block * KV_BLOCK + (item - arrive) / chunks;
+            const int64_t byte = row * dim + 16 * ((item < arrive ? item : item - arrive) % chunks);
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                const float s = __shfl(scale[c], j), mine = item < arrive ? s : old[c];
+                ratio[c][i] = mine == most[c] ? 1.0f : mine / most[c];
+                if (item < arrive + kept) w[c][i] = *(const u32x4 *)((c ? kv.v : kv.k) + byte);
+            }
         }
 #pragma unroll
         for (int i = 0; i < ITEMS; i++) {
             const int item = lane + 64 * i;
             const int row = item < arrive ? part.ctx + j0 - start + item / chunks : (item - arrive) / chunks;
-            if (item < arrive + kept) *(u32x4 *)(codes + (block * KV_BLOCK + row) * dim + 16 * ((item < arrive ? item : item - arrive) % chunks)) = again(w[i], ratio[i]);
+            const int64_t byte = (block * KV_BLOCK + row) * dim + 16 * ((item < arrive ? item : item - arrive) % chunks);
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                if (ratio[c][i] != 1.0f)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        const u32 u = w[c][i][k];
+                        const float f = ratio[c][i];
+                        w[c][i][k] = to_e4m3(__builtin_amdgcn_cvt_f32_fp8(u, 0) * f, __builtin_amdgcn_cvt_f32_fp8(u, 1) * f, __builtin_amdgcn_cvt_f32_fp8(u, 2) * f, __builtin_amdgcn_cvt_f32_fp8(u, 3) * f);
+                    }
+                if (item < arrive + kept) *(u32x4 *)((c ? kv.v : kv.k) + byte) = w[c][i];
+            }
         }
-        if (lane == 0 && old != most) scales[block] = most;
+        if (lane == 0 && old[0] != most[0]) kv.ks[block] = most[0];
+        if (lane == 0 && old[1] != most[1]) kv.vs[block] = most[1];
     }
 }
 
@@ -212,11 +230,11 @@ static void for_caches(const ensi_kv *const *kv, int caches, const GO &go) {
 void launch_clear_keep(ensi_ctx *ctx, const ensi_kv *const *kv, int caches, const ensi_clear_keep_args &a, hipStream_t st) {
     for_caches(kv, caches, [&](const CacheList &list, int n, int heads, int dim, bool) {
         ScopedTimer timer(ctx, "k_clear_keep", st);
-        const dim3 grid((2 * heads + 3) / 4, a.s.seqs, n);
+        const dim3 grid((n * heads + 3) / 4, a.s.seqs);
         // 16 rows of a block, moved or rounded again, dim / 16 chunks each
-        if (dim <= 64) hipLaunchKernelGGL(k_clear_keep<1>, grid, dim3(256), 0, st, list, a);
-        else if (dim <= 128) hipLaunchKernelGGL(k_clear_keep<2>, grid, dim3(256), 0, st, list, a);
-        else hipLaunchKernelGGL(k_clear_keep<4>, grid, dim3(256), 0, st, list, a);
+        if (dim <= 64) hipLaunchKernelGGL(k_clear_keep<1>, grid, dim3(256), 0, st, list, a, n, heads);
+        else if (dim <= 128) hipLaunchKernelGGL(k_clear_keep<2>, grid, dim3(256), 0, st, list, a, n, heads);
+        else hipLaunchKernelGGL(k_clear_keep<4>, grid, dim3(256), 0, st, list, a, n, heads);
     });
 }
 

@@ -162,13 +162,15 @@ def test_paths_and_pages_that_do_not_fit_leave_the_sequence_out(ctx):  # noqa: F
         cache.check()
     assert same_codes(c.dev[0].cpu(), codes["k"])
     cache.free()
-    # a sequence whose new tokens do not fit the path's width
-    cache = c.wrap(ctx)
-    ctx.clear_keep(cache, *c.where, int32([good[:8], good[:8]]), int32([4, 0]))
-    with pytest.raises(EnsiError, match="do not fit the arguments"):
-        cache.check()
-    assert same_codes(c.dev[0].cpu(), c.codes["k"])
-    cache.free()
+    # a sequence whose new tokens do not fit the path's width, noted in every cache
+    made = [Cache(ctx, [20, 30], [9, 9], heads, 64, 16, 7) for heads in (1, 3, 1, 1, 2)]
+    caches = [x.wrap(ctx) for x in made]
+    ctx.clear_keep(caches, *c.where, int32([good[:8], good[:8]]), int32([4, 0]))
+    for x, cache in zip(made, caches):
+        with pytest.raises(EnsiError, match="do not fit the arguments"):
+            cache.check()
+        assert same_codes(x.dev[0].cpu(), x.codes["k"])
+        cache.free()
 
 
 def test_keep_rounds_every_code_as_torch_does(ctx):  # noqa: F811
