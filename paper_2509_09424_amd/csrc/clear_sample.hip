@@ -40,7 +40,8 @@ struct SampleShared {
     u64 bins[SAMPLE_BINS], sum[SAMPLE_SEGMENTS], list[SAMPLE_LIST];
     float most[SAMPLE_PARTS], threads[SAMPLE_PARTS * SAMPLE_THREADS];  // the largest values of the parts, and of their threads
     int first[SAMPLE_PARTS];
-    int listed, pad;
+    int listed, border;  // the bin of top_p's bound, and what is left there of its target
+    u64 rest;
 };
 
 // Values of other lanes, within a row of 16 and from the rows before: a scan takes 6 of them, a twentieth of what it takes through LDS.  Lanes without a source get `none`.
@@ -918,8 +919,13 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_gather(SamplePa
         r.gather(g.tile0, g.tile1, min(lds.found, SAMPLE_BINS - 1));
     } else {
         r.set_roots();
-        find_part(r, row, mode);
-        r.sums_above(g.segment0, g.segment1, row.sum, lds.found);
+        const u64 rest = find_part(r, row, mode);
+        const int border = lds.found;
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            row.border = border;
+            row.rest = rest;
+        }
+        r.sums_above(g.segment0, g.segment1, row.sum, border);
     }
     const int listed = lds.listed;
     if (threadIdx.x == 0) at = atomicAdd(&row.listed, listed);  // (past the list's end where there are too many)
@@ -949,13 +955,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_finish(SamplePa
                 if (token >= 0) s.a.out[blockIdx.x] = token;
                 return;
             }
-            if (mode == SAMPLE_TOP) {
-                __syncthreads();
-                token = r.finish_listed(SAMPLE_BINS - 1);
-            } else {
-                const u64 rest = find_part(r, row, mode);
-                token = r.finish_part(rest, lds.found, row.sum);
-            }
+            const int border = row.border;
+            const u64 rest = row.rest;
+            __syncthreads();
+            token = mode == SAMPLE_TOP ? r.finish_listed(SAMPLE_BINS - 1) : r.finish_part(rest, border, row.sum);
         } else {
             mode = SAMPLE_SLOW;
             __syncthreads();
