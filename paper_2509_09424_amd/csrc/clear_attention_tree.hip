@@ -382,9 +382,10 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
     }
 }
 
-// Many rows: 32 RW of them to a workgroup, 32 to a wave, and tiles of 64 keys widened once for all of them in LDS (RowsLds; a wave fetches and widens a block of 16 keys and values while
-// the tile before is computed).  With 64 rows two waves have the same ones, and half of a tile's keys each.
-template <int TYPE, int DIM, int SCORE, int RW>
+// Many rows: 128 of them to a workgroup, 32 to a wave, and tiles of 64 keys widened once for all of them in LDS (RowsLds; a wave fetches and widens a block of 16 keys and values while
+// the tile before is computed).  Widening a tile in every wave takes a third of the kernel above's vector instructions: 64 sequences of 64 tokens behind 300 on 20 over 5 heads of
+// 128 59 us there, 37 here; 16 behind 2048 60 and 47.  What bounds it: vector instructions (exponentials, reciprocals and conversions take four times an ordinary one's cycles) and rounds of workgroups.
+template <int TYPE, int DIM, int SCORE>
 __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tree_rows(AttentionView a, const int32_t *parents, int split_tiles) {
     typedef typename Elem<TYPE>::type T;
     typedef Wide<TYPE> W;
@@ -395,17 +396,15 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
     __shared__ int nan_tiles[2];  // first and last tile whose values had NaN
     __shared__ u64 lines[TREE_MAX];
     __shared__ int places[TREE_MAX];
-    constexpr int HALVES = RW / 2;  // of a tile's keys to a wave
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 32, half = lane / 32;
-    const int row_wave = wave % RW, b0 = 2 * HALVES * (wave / RW);  // the wave's rows, and the first of its blocks of 16 keys
-    const int blocks = (a.row_tiles + 2 * RW - 1) / (2 * RW);
-    const int seq = blockIdx.z, head = blockIdx.x / blocks, block_row = 32 * RW * (blockIdx.x % blocks), split = blockIdx.y;
+    const int blocks = (a.row_tiles + 7) / 8;
+    const int seq = blockIdx.z, head = blockIdx.x / blocks, block_row = 128 * (blockIdx.x % blocks), split = blockIdx.y;
     const SeqPart part = seq_part(a.s, seq, a.kv.page, a.max_length, a.kv.status);
     const int rows = part.count * a.group;
     const TreeKeys keys = tree_keys(part, a.window);
     const int tile0 = split * split_tiles, tile1 = min(tile0 + split_tiles, keys.tiles);  // of 32 keys, two of which are a tile here
     if (block_row >= rows || tile0 >= tile1) return;
-    const int row0 = block_row + 32 * row_wave, lo = keys.lo + 32 * tile0, tiles = (tile1 - tile0 + 1) / 2;
+    const int row0 = block_row + 32 * wave, lo = keys.lo + 32 * tile0, tiles = (tile1 - tile0 + 1) / 2;
     const int row = min(row0 + n, rows - 1), index = row / a.group, token = part.first + index;
     const int q_head = head * a.group + row % a.group;
     vec q[STEPS];
@@ -520,13 +519,13 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
     __syncthreads();
     for (int t = 0; t < tiles; t++) {
         const int key0 = lo + 64 * t;
-        int good[2 * HALVES];
-        float ks[2 * HALVES], vs[2 * HALVES];
+        int good[4];
+        float ks[4], vs[4];
 #pragma unroll
-        for (int b = 0; b < 2 * HALVES; b++) {
-            good[b] = __builtin_amdgcn_readlane(my_good, 4 * (t % 16) + b0 + b);
-            ks[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), 4 * (t % 16) + b0 + b));
-            vs[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 4 * (t % 16) + b0 + b));
+        for (int b = 0; b < 4; b++) {
+            good[b] = __builtin_amdgcn_readlane(my_good, 4 * (t % 16) + b);
+            ks[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), 4 * (t % 16) + b));
+            vs[b] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), 4 * (t % 16) + b));
         }
         if (t + 1 < tiles) {
             if ((t + 1) % 16 == 0) look_up(t + 1);
@@ -535,44 +534,44 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
         if (row0 < rows) {
             const unsigned char *at = lds + (L::BUFFERS == 2 ? t % 2 * L::BUFFER : 0);
             // fragments of AHEAD steps under way: left to itself, the compiler keeps two reads under way, and a wave waits for LDS most of its time
-            f32x16 qk[HALVES];
+            f32x16 qk[2];
             constexpr int AHEAD = STEPS < 4 ? STEPS : 4;
-            vec kf[AHEAD][HALVES];
+            vec kf[AHEAD][2];
             const auto read_keys = [&](int s) {
 #pragma unroll
-                for (int x = 0; x < HALVES; x++) kf[s % AHEAD][x] = *(const vec *)(at + (16 * b0 + 32 * x + n) * L::K_ROW + 32 * s + 16 * half);
+                for (int x = 0; x < 2; x++) kf[s % AHEAD][x] = *(const vec *)(at + (32 * x + n) * L::K_ROW + 32 * s + 16 * half);
             };
 #pragma unroll
             for (int s = 0; s < AHEAD; s++) read_keys(s);
 #pragma unroll
-            for (int x = 0; x < HALVES; x++)
+            for (int x = 0; x < 2; x++)
 #pragma unroll
                 for (int r = 0; r < 16; r++) qk[x][r] = 0;
 #pragma unroll
             for (int s = 0; s < STEPS; s++) {
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < HALVES; x++) qk[x] = W::mfma32(kf[s % AHEAD][x], q[s], qk[x]);
+                for (int x = 0; x < 2; x++) qk[x] = W::mfma32(kf[s % AHEAD][x], q[s], qk[x]);
                 if (s + AHEAD < STEPS) read_keys(s + AHEAD);
             }
             __builtin_amdgcn_sched_barrier(0);
             // register r of half x, block b = 2 x + r / 8: key 16 b + 8 (r % 8 / 4) + 4 half + r % 4 of the wave's
             bool masked = key0 + 63 >= part.ctx || (a.window > 0 && key0 <= keys.last - a.window);
-            float u[2 * HALVES][8], most = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
+            float u[4][8], most = SCORE == ENSI_SCORE_SIGMOID ? 0 : -__builtin_inff();
 #pragma unroll
-            for (int b = 0; b < 2 * HALVES; b++) {
+            for (int b = 0; b < 4; b++) {
                 masked |= !good[b];
 #pragma unroll
                 for (int e = 0; e < 8; e++) u[b][e] = qk[b / 2][8 * (b % 2) + e];
             }
-            float factor[2 * HALVES], lv[2 * HALVES];
+            float factor[4], lv[4];
             tree_scores<SCORE>(u, factor, ks, vs, a);
             if (masked) {
                 const u64 line = lines[index];
                 const int place = places[index];
 #pragma unroll
-                for (int x = 0; x < HALVES; x++) {
-                    u32 seen = seen_keys(part, a.window, line, place, key0 + 16 * b0 + 32 * x);
+                for (int x = 0; x < 2; x++) {
+                    u32 seen = seen_keys(part, a.window, line, place, key0 + 32 * x);
                     seen &= (good[2 * x] ? 0xffffu : 0) | (good[2 * x + 1] ? 0xffff0000u : 0);
                     seen >>= 4 * half;
 #pragma unroll
@@ -582,7 +581,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
                 }
             }
 #pragma unroll
-            for (int b = 0; b < 2 * HALVES; b++) {
+            for (int b = 0; b < 4; b++) {
                 lv[b] = __builtin_amdgcn_logf(vs[b]);
                 most = most_of(most, tree_most<SCORE>(u[b], factor[b], lv[b]));
             }
@@ -608,7 +607,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
             bf16x8 vf[2][TILES];
             const auto read_values = [&](int b) {
 #pragma unroll
-                for (int j = 0; j < TILES; j++) vf[b % 2][j] = *(const bf16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 16 * ((2 * (b0 + b) + half) ^ (2 * (j % 2) + n / 16)));
+                for (int j = 0; j < TILES; j++) vf[b % 2][j] = *(const bf16x8 *)(at + L::K_BYTES + (32 * j + n) * L::V_ROW + 16 * ((2 * b + half) ^ (2 * (j % 2) + n / 16)));
             };
             const float unit = __builtin_amdgcn_exp2f(0.5f * (WEIGHT_LIFT - base));  // sigmoid: half of the way to the reference
             Weights p[2];
@@ -631,14 +630,14 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
             __builtin_amdgcn_sched_barrier(0);
             weigh(0);
 #pragma unroll
-            for (int b = 0; b < 2 * HALVES; b++) {
-                if (b + 1 < 2 * HALVES) read_values(b + 1);
+            for (int b = 0; b < 4; b++) {
+                if (b + 1 < 4) read_values(b + 1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int j = 0; j < TILES; j++) o[j] = Wide<ENSI_T_BF16>::mfma32(vf[b % 2][j], p[b % 2].hi.v, o[j]);
 #pragma unroll
                 for (int j = 0; j < TILES; j++) o[j] = Wide<ENSI_T_BF16>::mfma32(vf[b % 2][j], p[b % 2].lo.v, o[j]);
-                if (b + 1 < 2 * HALVES) weigh(b + 1);
+                if (b + 1 < 4) weigh(b + 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -646,7 +645,7 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
         if (t + 1 < tiles) put(t + 1);
         __syncthreads();
     }
-    if (nan_tiles[1] >= 0 && b0 == 0)
+    if (nan_tiles[1] >= 0)
         for (int key = lo + 64 * nan_tiles[0]; key <= min(lo + 64 * nan_tiles[1] + 63, keys.last); key++) {
             const int block = block_of(a, seq, head, key);
             if (block < 0 || !(seen_keys(part, a.window, lines[index], places[index], key) & 1)) continue;
@@ -658,32 +657,6 @@ __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tre
                     if (is_nan(v[32 * j + 8 * (r / 4) + r % 4])) o[j][r] = __builtin_nanf("");
         }
     st_l += __shfl_xor(st_l, 32);
-    if (RW == 2) {
-        // the other half's sums, of waves with the same rows
-        float *const to = (float *)lds + (row_wave * 64 + lane) * 4, *const ml = (float *)lds + 2 * 64 * 16 * TILES + (row_wave * 64 + lane) * 2;
-        if (b0 > 0) {
-#pragma unroll
-            for (int j = 0; j < TILES; j++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) *(f32x4 *)(to + (4 * j + e) * 512) = (f32x4){o[j][4 * e], o[j][4 * e + 1], o[j][4 * e + 2], o[j][4 * e + 3]};
-            ml[0] = st_m;
-            ml[1] = st_l;
-        }
-        __syncthreads();
-        if (b0 > 0) return;
-        const float om = ml[0], m = most_of(st_m, om), base = m == -__builtin_inff() ? 0.0f : m;
-        const float h0 = half_lift(st_m, base), h1 = half_lift(om, base);
-#pragma unroll
-        for (int j = 0; j < TILES; j++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const f32x4 v = *(const f32x4 *)(to + (4 * j + e) * 512);
-#pragma unroll
-                for (int i = 0; i < 4; i++) o[j][4 * e + i] = o[j][4 * e + i] * h0 * h0 + v[i] * h1 * h1;
-            }
-        st_l = st_l * h0 * h0 + ml[1] * h1 * h1;
-        st_m = m;
-    }
     if (row0 + n >= rows) return;
     if (keys.tiles > split_tiles) {
         float *ws = a.ws + ((((int64_t)seq * a.kv.heads + head) * a.row_tiles + row / 16) * a.splits + split) * (16 * DIM + 32);
@@ -771,18 +744,18 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree_join(AttentionView
     *(quad_t *)((T *)a.out + (int64_t)(part.first + index) * a.out_stride + (int64_t)q_head * DIM + 4 * quad) = w;
 }
 
-// Waves of rows to a workgroup where keys are shared through LDS, 0 where every wave has its own
-static int tree_by_rows(const AttentionView &v, int rows) {
-    return rows > 64 ? 4 : rows > 32 ? 2 : 0;
-}
-
 template <int TYPE, int DIM, int SCORE>
 static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipStream_t st) {
     const int heads = v.kv.heads;
     const int span = v.window > 0 ? (int)min((int64_t)v.max_length, (int64_t)v.window + v.s.max_new - 1 + 31) : v.max_length;
     v.row_tiles = (v.s.max_new * v.group + 15) / 16;
     const int tiles = (span + 31) / 32;
-    const int rows = v.s.max_new * v.group, rw = tree_by_rows(v, rows), rt = v.row_tiles == 1 ? 1 : 2, width = rw ? 2 * rw : rt;  // tiles of 16 rows to a workgroup
+    const int rows = v.s.max_new * v.group, rt = v.row_tiles == 1 ? 1 : 2;
+    // Keys shared through LDS from 65 rows on; with up to 64, of which half the waves would have none, that gains nothing (two waves to the same rows and half of the keys each: 16 sequences of
+    // 64 tokens behind 1000 on 16 heads of 64 30 us and 25, 16 of 10 behind 2000 on 32 over 8 heads of 128 25 and 31).  32 rows to a wave where it has keys of its own, 16 where there are no
+    // more (64 leave one wave to a SIMD: 16 sequences of 64 tokens behind 2048 81 us instead of 60).
+    const bool by_rows = rows > 64;
+    const int width = by_rows ? 8 : rt;  // tiles of 16 rows to a workgroup
     const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + width - 1) / width);
     // Parts of a row's keys: up to 32 tiles each, which evens out sequences of different lengths; down to 12 while the workgroups are fewer than the CUs have room for, and down
     // to 4, one for every wave, where CUs would stand idle.
@@ -802,9 +775,7 @@ static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipS
             hipLaunchKernelGGL(kernel, dim3(heads * ((v.row_tiles + width - 1) / width), splits, v.s.seqs), dim3(256), bytes, st, v, parents, split_tiles);
         };
         constexpr int rows_bytes = RowsLds<DIM>::BUFFERS * RowsLds<DIM>::BUFFER;
-        static_assert(rows_bytes >= 2 * 64 * (DIM / 32 * 16 + 2) * 4, "two waves' sums");
-        if (rw == 4) go(k_clear_attention_tree_rows<TYPE, DIM, SCORE, 4>, rows_bytes);
-        else if (rw == 2) go(k_clear_attention_tree_rows<TYPE, DIM, SCORE, 2>, rows_bytes);
+        if (by_rows) go(k_clear_attention_tree_rows<TYPE, DIM, SCORE>, rows_bytes);
         else if (rt == 1) go(k_clear_attention_tree<TYPE, DIM, SCORE, 1>, TreeLds<DIM, 1>::BYTES);
         else go(k_clear_attention_tree<TYPE, DIM, SCORE, 2>, TreeLds<DIM, 2>::BYTES);
     }
