@@ -441,8 +441,9 @@ int ensi_ccmm_av(ensi_ctx *ctx, const ensi_gk *rk, const ensi_gk *gk, const ensi
  * encrypted product of the same 8-bit codes.  Activations are device arrays of one ENSI_T_* type;
  * products, sums, norms and softmax statistics are held in 32 bits and rounded once at the end; the weights of the attention enter
  * their product with the values in 16 bits (two terms of bf16: half a step of 2^-16, and the exponents of 32 bits).  Strides are in elements.
- * These calls only enqueue kernels on the stream, allocate nothing and may be captured into a graph.  Calls of one context must
- * not overlap on different streams (the attention and products of many rows of unaligned codes have a workspace).
+ * These calls only enqueue kernels on the stream, allocate nothing (but for a workspace with the first cache, weights or sampling call of a context) and may be
+ * captured into a graph.  Calls of one context must not overlap on different streams (the attention, products of many rows of unaligned codes and
+ * the sampling of few long rows have a workspace).
  * What lies on the device (lengths, tables) cannot be checked by a call that does not wait: the kernels check it,
  * leave out what is wrong and note it in the cache's status (ensi_clear_cache_status). */
 #define ENSI_T_F32 0
@@ -553,8 +554,8 @@ int ensi_clear_attention_tree(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_atten
  * at least (all with top_p >= 1, one with top_p <= 0); of these the ones with w >= min_p (a min_p above 1 counts as 1).  out: the first of them, by index, at which
  * the running sum of w exceeds uniform times their sum; uniform is in [0, 1), and counts as the nearest of these elsewhere.  temperature 0: the first of the largest.
  * -1 where there is no distribution: NaN or +inf among the logits, nothing but -inf, a temperature that is negative, infinite or NaN, NaN in one of the others.
- * Weights are rounded to whole multiples of 2^-S, S = 50 or what sums of vocab of them leave room for in 62 bits, so that the result does not hang on an order
- * of summation.  uniform: device float [rows]; the others device arrays [rows], or NULL for the number that follows, for all rows. */
+ * Weights are rounded to whole multiples of 2^-S, S = 50 or what sums of vocab of them leave room for in 62 bits (45 for 128000), so that the result does not hang on
+ * an order of summation.  uniform: device float [rows]; the others device arrays [rows], or NULL for the number that follows, for all rows. */
 typedef struct ensi_clear_sample_args {
     const void *logits;
     const float *uniform, *temperature;

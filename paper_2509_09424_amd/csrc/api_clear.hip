@@ -305,10 +305,13 @@ extern "C" int ensi_clear_sample(ensi_ctx *ctx, const ensi_clear_sample_args *a,
     if (Span(a->logits, a->rows, a->stride, a->vocab, size).meets(o) || meets(a->uniform) || meets(a->temperature) || meets(a->top_k) || meets(a->top_p) || meets(a->min_p))
         ENSI_FAIL(ctx, ENSI_E_BADARG, "clear sample: out overlaps an input");
     if (int rc = current_device(ctx)) return rc;
-    // rows are split over workgroups where there is a workspace; the first call of a context makes it, unless it is captured
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusActive;
-    if (!ctx->ws_clear && hipStreamIsCapturing((hipStream_t)stream, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone)
-        if (int rc = clear_workspace(ctx)) return rc;
+    // Rows are split over workgroups where there is a workspace; the first call of a context makes it, unless it is captured or there is no memory: without one
+    // the tokens are the same.
+    if (!ctx->ws_clear) {
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusActive;
+        if (hipStreamIsCapturing((hipStream_t)stream, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone) (void)clear_workspace(ctx);
+        (void)hipGetLastError();
+    }
     launch_clear_sample(ctx, *a, (hipStream_t)stream);
     ENSI_HIP(ctx, hipGetLastError());
     return ENSI_OK;
