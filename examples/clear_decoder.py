@@ -37,13 +37,13 @@ class Layer:
         scales = [torch.zeros(pages, kv_heads, page // 16, device="cuda") for _ in range(2)]
         self.cache = ctx.clear_cache(*cache, *scales)
 
-    def __call__(self, x, residual, seqs, turn, parents=None, **bounds):
+    def __call__(self, x, residual, seqs, turn, tree={}, **bounds):
         """(what the layer adds, the sum before it): both enter the next layer's first norm."""
         ctx, q = self.ctx, self.q_heads
         codes, scales = ctx.clear_norm(x, self.gains[0], residual=residual, sum_out=residual)
         heads = ctx.clear_matmul(self.qkv, codes, scales, dtype=x.dtype).view(x.shape[0], -1, self.dim)
-        queries = ctx.clear_append(self.cache, *seqs, heads[:, q:q + self.kv_heads], heads[:, q + self.kv_heads:], *turn, q=heads[:, :q], q_out=heads[:, :q], max_new=bounds["max_new"], parents=parents)
-        self.attention = ctx.clear_attention(self.cache, *seqs, queries, parents=parents, **bounds).view(x.shape[0], -1)
+        queries = ctx.clear_append(self.cache, *seqs, heads[:, q:q + self.kv_heads], heads[:, q + self.kv_heads:], *turn, q=heads[:, :q], q_out=heads[:, :q], max_new=bounds["max_new"], **tree)
+        self.attention = ctx.clear_attention(self.cache, *seqs, queries, **bounds, **tree).view(x.shape[0], -1)
         y = ctx.clear_matmul(self.out, *ctx.clear_norm(self.attention, self.gains[1]), dtype=x.dtype)
         codes, scales = ctx.clear_norm(y, self.gains[2], residual=residual, sum_out=residual)
         hidden = ctx.clear_matmul(self.up, codes, scales, dtype=x.dtype).relu_().square_()
@@ -74,9 +74,9 @@ class Decoder:
 
     def __call__(self, x, begin, max_new, max_length=None, parents=None):
         """x: [tokens][width] embeddings of the new tokens, sequence i's from begin[i] on.  Advances the lengths, unless the tokens are trees (parents)."""
-        seqs, residual = (self.table, begin, self.lengths), torch.zeros_like(x)
+        seqs, residual, tree = (self.table, begin, self.lengths), torch.zeros_like(x), {} if parents is None else {"parents": parents}
         for layer in self.layers:
-            x, residual = layer(x, residual, seqs, self.turn, parents=parents, max_new=max_new, max_length=max_length or self.length)
+            x, residual = layer(x, residual, seqs, self.turn, tree, max_new=max_new, max_length=max_length or self.length)
         if parents is None:
             self.lengths += begin[1:] - begin[:-1]
         return x + residual
