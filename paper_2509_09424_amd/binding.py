@@ -715,10 +715,11 @@ class Context:
             args = _APPEND.pack(*_seqs(table, begin, lengths, tokens, min(tokens, 64) if max_new is None and parents is not None else max_new, at), pq, pk, pv, po, pc, ps, sq, so, sk, sv, heads, rot, min(positions, 1 << 30), pair_code, _type("k", kind), 0)
         except (struct.error, OverflowError) as e:
             _no_number(e)
-        if parents is None:
+        tree = None if parents is None else _whole("parents", parents, (tokens,), _TORCH[2]["int32"], at)
+        if tree:
+            rc = self.lib.ensi_clear_append_tree(self.h, cache.h, args, tree, stream)
+        else:  # (an empty tensor has no address)
             rc = self.lib.ensi_clear_append(self.h, cache.h, args, stream)
-        else:
-            rc = self.lib.ensi_clear_append_tree(self.h, cache.h, args, _whole("parents", parents, (tokens,), _TORCH[2]["int32"], at), stream)
         if rc:
             self._check(rc)
         return q_out
@@ -747,10 +748,11 @@ class Context:
             args = _ATTENTION.pack(*s, pq, po, sq, so, shape[1], _type("q", kind), score_code, window, max_length, cap, bias, 0)
         except (struct.error, OverflowError) as e:
             _no_number(e)
-        if parents is None:
-            rc = self.lib.ensi_clear_attention(self.h, cache.h, args, stream)
+        tree = None if parents is None else _whole("parents", parents, shape[:1], _TORCH[2]["int32"], at)
+        if tree:
+            rc = self.lib.ensi_clear_attention_tree(self.h, cache.h, args, tree, stream)
         else:
-            rc = self.lib.ensi_clear_attention_tree(self.h, cache.h, args, _whole("parents", parents, shape[:1], _TORCH[2]["int32"], at), stream)
+            rc = self.lib.ensi_clear_attention(self.h, cache.h, args, stream)
         if rc:
             self._check(rc)
         return out
@@ -820,7 +822,7 @@ class Context:
         i32, seqs = _TORCH[2]["int32"], lengths.shape[0]
         pp, sp = _rows("path", path, (seqs, max_new), i32, at)
         try:
-            args = _KEEP.pack(*_seqs(table, begin, lengths, seqs * max_new, max_new, at), pp, _whole("count", count, (seqs,), i32, at), sp)
+            args = _KEEP.pack(*_seqs(table, begin, lengths, 2 ** 31 - 1 if seqs and max_new else 0, max_new, at), pp, _whole("count", count, (seqs,), i32, at), sp)
         except (struct.error, OverflowError) as e:
             _no_number(e)
         rc = self.lib.ensi_clear_keep(self.h, handles, len(handles) // 8, args, stream)

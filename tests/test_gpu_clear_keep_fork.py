@@ -141,6 +141,22 @@ def test_keep_in_many_layers_and_one(ctx):  # noqa: F811
         handle.free()
 
 
+def test_keep_of_some_of_a_batchs_sequences(ctx):  # noqa: F811
+    """Rows of a batch's arrays: their tokens begin behind those of the rows before."""
+    c = Cache(ctx, [20, 30, 9, 41], [64, 50, 5, 7], 2, 64, 16, 8)
+    c.fill_new()
+    paths = [[], [0, 7, 8, 49], [1, 4], []]
+    codes, scales = keep_reference(c, paths)
+    cache = c.wrap(ctx)
+    table, begin, lengths = c.where
+    path, count = int32([p + [-1] * (50 - len(p)) for p in paths[1:3]]), int32([4, 2])
+    ctx.clear_keep(cache, table[1:3], begin[1:4], lengths[1:3], path, count)
+    cache.check()
+    for x, cd, sc in (("k", c.dev[0], c.dev[2]), ("v", c.dev[1], c.dev[3])):
+        assert same_codes(cd.cpu(), codes[x]) and torch.equal(sc.cpu().nan_to_num(nan=-1.0), scales[x].nan_to_num(nan=-1.0))
+    cache.free()
+
+
 def test_paths_and_pages_that_do_not_fit_leave_the_sequence_out(ctx):  # noqa: F811
     from paper_2509_09424_amd import EnsiError
     c = Cache(ctx, [20, 30], [9, 9], 1, 64, 16, 7)

@@ -242,3 +242,22 @@ def test_many_sequences_and_a_long_one(ctx):  # noqa: F811
         tree_near(c, "bf16", got, q, parents)
         assert torch.equal(got, ctx.clear_attention(cache, *c.where, q.cuda(), max_new=max(news), max_length=max(a + b for a, b in zip(ctxs, news)), parents=parents.cuda()))
         cache.free()
+
+
+def test_batches_without_new_tokens(ctx):  # noqa: F811
+    """No sequences, and sequences with nothing new: an empty tensor of parents is one."""
+    c = Cache(ctx, [20, 3], [0, 0], 2, 64, 16, 4)
+    cache = c.wrap(ctx)
+    before = [t.clone() for t in c.dev]
+    x = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    parents = torch.empty(0, dtype=torch.int32, device="cuda")
+    for n in (2, 0):
+        table, begin, lengths = c.where[0][:n], c.where[1][:n + 1], c.where[2][:n]
+        ctx.clear_append(cache, table, begin, lengths, x, x, None, None, parents=parents)
+        assert ctx.clear_attention(cache, table, begin, lengths, x, parents=parents).shape == (0, 2, 64)
+        path, count, following = ctx.clear_accept(begin, parents, parents, parents, max_new=0)
+        assert path.shape == (n, 0) and count.tolist() == [0] * n and following.tolist() == [-1] * n
+        ctx.clear_keep(cache, table, begin, lengths, path, count)
+    cache.check()
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, c.dev))
+    cache.free()
