@@ -1,8 +1,10 @@
 // Attention of trees of drafted tokens over a paged cache (the mathematics: clear_attention.h).  New token t of a sequence sees the cached tokens, itself and its ancestors; its
 // position is the length and its depth.
 //
-// A sequence has up to 64 new tokens, so one word of 64 bits holds what a row sees of them, and 64 rows or fewer read the same long cache: a wave takes RT tiles of 16 rows
-// at once, widens a tile of 32 keys and values once for all of them, and the keys are split over the waves and over workgroups.
+// A sequence has up to 64 new tokens, so one word of 64 bits holds what a row sees of them, and the rows of a sequence and key head read the same long cache.  Two kernels: up to
+// 64 rows (a few tokens each) are bound by the cache's bytes, so a workgroup takes 16 or 32 of them and its four waves a quarter of its keys each, a tile of 32 widened once for all
+// of a wave's rows and the next one under way (48 sequences of 8 tokens behind up to 8191 on 20 over 5 heads of 128: 223 MB in 66 us); more rows are bound by vector
+// instructions, and share keys that are widened once for 128 of them.  Either splits long caches over workgroups; a third kernel joins the parts.
 #include "clear_attention.h"
 
 // Which of the 32 keys from key0 on a row sees: cached ones within the window of its place, and those of its line.
@@ -757,10 +759,15 @@ static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipS
     const bool by_rows = rows > 64;
     const int width = by_rows ? 8 : rt;  // tiles of 16 rows to a workgroup
     const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + width - 1) / width);
-    // Parts of a row's keys: up to 32 tiles each, which evens out sequences of different lengths; down to 12 while the workgroups are fewer than the CUs have room for, and down
-    // to 4, one for every wave, where CUs would stand idle.
-    int splits = max((tiles + 31) / 32, (int)min(1024 / base, (int64_t)tiles / 12));
-    if (base * splits < 256) splits = (int)min(512 / base, (int64_t)(tiles + 3) / 4);
+    // Parts of a row's keys.  A CU has room for two workgroups, for one from 192 places on.  Keys of one length, of one sequence or within a window: as many parts as fill that room once.
+    // Sequences of different lengths, of which only the longest is known here: half as many again, and parts of up to 40 tiles.  Each part is also written and read again, so there are no
+    // more than 1.6 sqrt(tiles), where turns of a wave and parts of a row cost about the same.  Against four turns a workgroup wherever CUs stand idle, and otherwise parts of 12 to 32 tiles: one sequence
+    // of 16 tokens behind 4096 on 20 over 5 heads of 128 19 -> 16 us; 48 behind up to 1000 36 -> 25; 48 of 8 tokens behind up to 8191 64 -> 59; 16 of 64 tokens with a window of 2048 on 16 heads
+    // of 96 63 -> 54; 8 behind up to 4096 on 16 over 4 heads of 256 84 -> 66 (and on 32 over 4 heads of 64 43 -> 47).
+    const int room_for = v.kv.dim <= 128 ? 512 : 256;
+    const bool even = v.s.seqs == 1 || span < v.max_length;
+    int splits = (int)min((int64_t)(even ? room_for : room_for + room_for * 9 / 16) / base, (int64_t)sqrtf(2.56f * tiles));
+    if (!even) splits = max(splits, tiles / 40);
     splits = max(min(splits, TREE_SPLITS), 1);
     const int64_t room = (int64_t)CLEAR_WS_FLOATS / ((int64_t)v.s.seqs * heads * v.row_tiles * (16 * DIM + 32));
     if (splits > room) splits = (int)max((int64_t)1, room);
