@@ -753,9 +753,9 @@ static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipS
     v.row_tiles = (v.s.max_new * v.group + 15) / 16;
     const int tiles = (span + 31) / 32;
     const int rows = v.s.max_new * v.group, rt = v.row_tiles == 1 ? 1 : 2;
-    // Keys shared through LDS from 65 rows on; with up to 64, of which half the waves would have none, that gains nothing (two waves to the same rows and half of the keys each: 16 sequences of
-    // 64 tokens behind 1000 on 16 heads of 64 30 us and 25, 16 of 10 behind 2000 on 32 over 8 heads of 128 25 and 31).  32 rows to a wave where it has keys of its own, 16 where there are no
-    // more (64 leave one wave to a SIMD: 16 sequences of 64 tokens behind 2048 81 us instead of 60).
+    // Keys shared through LDS from 65 rows on; with up to 64 half the waves would have none there (16 sequences of 64 tokens behind up to 1000 on 16 heads of 64 28 us by rows and 19; 48 of 16 behind
+    // up to 4096 on 20 over 5 heads of 128 81 and 65).  32 rows to a workgroup where its waves have keys of their own, 16 where there are no more (64 leave one wave to a SIMD: 16 sequences of 64
+    // tokens behind 2048 81 us instead of 60).
     const bool by_rows = rows > 64;
     const int width = by_rows ? 8 : rt;  // tiles of 16 rows to a workgroup
     const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + width - 1) / width);
