@@ -13,7 +13,7 @@
 // Where there are more candidates than room (flat rows, thousands of equal logits) the bound is found in the row itself, by bins over the bits of the values where it lies.
 //
 // What bounds it: latencies in short rows (32000 logits in bf16: 6 us greedy, 9.6 with top_k, 13 with none of the filters, 29 with top_p alone); in many long ones the passes over memory, three of
-// them in four launches (256 rows of 128003 in f32: 21 us a pass, 45 greedy, 60 with top_k = 50, 61 with no filter), and 64-bit arithmetic (112 with top_p alone, where each weight is formed twice).
+// them in four launches (256 rows of 128003 in f32: 21 us a pass, 45 greedy, 55 with top_k = 50, 61 with no filter), and 64-bit arithmetic (112 with top_p alone, where each weight is formed twice).
 #include "clear.h"
 
 #define SAMPLE_THREADS 1024
@@ -21,8 +21,8 @@
 #define SAMPLE_BINS 2048
 #define SAMPLE_SEGMENTS 512  // of a row: one wave looks through one of them at the end
 #define SAMPLE_LIST 4096     // candidates
-#define SAMPLE_PAIRS 256     // candidates that are compared each with each (64 rows of 128000, top 50 and top_p: 29 us, in bins 35; one of 32000 9.3 and 13.3)
-#define SAMPLE_FEW 512       // top_k up to which the threads' largest values choose the candidates (256 rows, top 50: 60 us, with counts of all values 78; 64 rows 29 and 32)
+#define SAMPLE_PAIRS 256     // candidates that are compared each with each (64 rows of 128000, top 50 and top_p as arrays: 29 us, in bins 35; one of 32000 9.3 and 13.3)
+#define SAMPLE_FEW 512       // top_k up to which the threads' largest values choose the candidates (256 rows, top 50: 55 us, with counts of all values 78; 64 rows 26 and 32)
 #define SAMPLE_PARTS 8       // workgroups to a row
 #define LN2 0.69314718055994530942
 
@@ -996,7 +996,9 @@ static void sample_type(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStrea
     const SampleParts s = {a, (SampleShared *)ctx->ws_clear, parts};
     const dim3 grid(parts, (u32)a.rows);
     hipLaunchKernelGGL(k_clear_sample_most<TYPE>, grid, block, 0, st, s);
-    hipLaunchKernelGGL(k_clear_sample_bins<TYPE>, grid, block, 0, st, s);
+    // (nothing to do there with a few of every row's tokens: 64 rows of 128000, top 50 29 us with it, 26 without)
+    const bool few = !a.temperature && a.all_temperature > 0 && !a.top_k && a.all_top_k > 0 && a.all_top_k <= SAMPLE_FEW * parts && a.all_top_k < a.vocab;
+    if (!few) hipLaunchKernelGGL(k_clear_sample_bins<TYPE>, grid, block, 0, st, s);
     if (a.top_k || a.top_p || a.all_top_k > 0 || a.all_top_p < 1) hipLaunchKernelGGL(k_clear_sample_gather<TYPE>, grid, block, 0, st, s);
     hipLaunchKernelGGL(k_clear_sample_finish<TYPE>, dim3((u32)a.rows), block, 0, st, s);
 }

@@ -239,3 +239,13 @@ def test_binding(tmp_path):
                 call()
     finally:
         binding._TORCH = before
+
+
+def test_a_few_of_every_rows_tokens_take_a_launch_less(tmp_path):
+    calls = run(tmp_path, SEQS + """
+u, out, x = at(64), at(64), at(2 * 128000 * 2)
+for t, k, each in ((0.8, 50, 0), (0.8, 3584, 0), (0.8, 3585, 0), (0.0, 50, 0), (0.8, 50, at(64))):
+    check(lib.ensi_clear_sample(ctx.h, binding._SAMPLE.pack(x, u, 0, each, 0, 0, out, 2, 128000, 128000, 1, t, k, 0.9, 0.0), st), None, "")
+""")
+    kinds = "".join({"_most": "m", "_bins": "b", "_gather": "g", "_finish": "f"}[n.split("k_clear_sample")[1].split("ILi")[0]] for n in names(calls))
+    assert kinds == "mgf" * 2 + "mbgf" * 3  # (7 workgroups to a row, 512 tokens each)

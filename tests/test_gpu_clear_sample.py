@@ -166,3 +166,17 @@ def test_a_captured_call_follows_its_inputs(ctx):
         assert got == ctx.clear_sample(x, u, temperature=0.8, top_k=50, top_p=0.9).cpu().tolist()
         numbers, un = x.cpu().numpy(), u.cpu().numpy()
         assert got == [reference(numbers[r], float(un[r]), float(np.float32(0.8)), 50, float(np.float32(0.9)), 0.0) for r in range(7)]
+
+
+@pytest.mark.parametrize("kind, vocab", [("bf16", 70001), ("f32", 40000), ("f16", 128000), ("bf16", 500)])
+def test_numbers_for_all_rows_are_arrays_of_them(ctx, kind, vocab):
+    """Which passes a call makes depends on what it knows of the rows; the tokens do not."""
+    rng = np.random.default_rng(vocab)
+    x = torch.from_numpy(rng.standard_normal((5, vocab)).astype(np.float32) * 3).to(TYPES[kind])
+    x[3] = -math.inf
+    x[4, :vocab // 2] = 2.0  # equal ones, more than there is room for
+    u = rng.random(5).astype(np.float32)
+    for t, k, p, m in ((0.8, 50, 0.95, 0.0), (1.0, 1, 1.0, 0.0), (1.3, 2000, 0.9, 0.01), (1.3, 5000, 1.0, 0.0), (0.0, 50, 0.9, 0.0), (0.7, vocab, 0.9, 0.0), (0.7, vocab - 1, 1.0, 0.0), (0.7, 0, 0.9, 0.0), (0.7, -3, 1.0, 0.1)):
+        logits = check(ctx, x, u, t, k, p, m)
+        numbers = [reference(x[r].float().numpy(), float(u[r]), *(float(np.float32(a)) if i != 1 else a for i, a in enumerate((t, k, p, m)))) for r in range(5)]
+        assert ctx.clear_sample(logits, torch.from_numpy(u).cuda(), temperature=t, top_k=k, top_p=p, min_p=m).cpu().tolist() == numbers, (t, k, p, m)
