@@ -261,3 +261,20 @@ def test_batches_without_new_tokens(ctx):  # noqa: F811
     cache.check()
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, c.dev))
     cache.free()
+
+
+@pytest.mark.parametrize("new, group, dim, score", [(5, 3, 64, "softmax"), (20, 4, 64, "sigmoid"), (3, 8, 192, "softmax")])
+def test_a_long_sequence_in_many_parts(ctx, new, group, dim, score):  # noqa: F811
+    """61440 cached tokens, 60 times the same 64 pages, in up to 64 parts of a row's keys."""
+    c = Cache(ctx, [1024], [new], 1, dim, 16, dim + new)
+    c.fill_new()
+    c.table = torch.cat([c.table[:, :64].repeat(1, 60), c.table[:, 64:]], 1)
+    c.ctxs, c.lengths = [61440], torch.tensor([61440], dtype=torch.int32)
+    parents = trees([new], 3)
+    q = (torch.randn(new, group, dim, generator=c.g) / 16).bfloat16()
+    cache = c.wrap(ctx)
+    bias = -math.log(61440) if score == "sigmoid" else 0.0
+    out = ctx.clear_attention(cache, *c.where, q.cuda(), score=score, bias=bias, max_length=61440 + new, parents=parents.cuda())
+    cache.check()
+    tree_near(c, "bf16", out, q, parents, score=score, bias=bias)
+    cache.free()
