@@ -117,10 +117,12 @@ def draft(a, ctx):
     each = 1 + 2 * fan
     model = Decoder(ctx, layers=a.layers, seqs=a.seqs, length=a.prompt + 3 * (a.steps + 8) + each, vocab=vocab)
     begin = torch.arange(a.seqs + 1, dtype=torch.int32, device="cuda")
-    prompt = torch.randint(0, vocab, (a.seqs * a.prompt,), device="cuda")
-    model(model.embeddings[prompt], begin * a.prompt, a.prompt, a.prompt)
+    prompt = torch.randint(0, vocab, (a.seqs, a.prompt), device="cuda")
+    rest = a.prompt - 1  # a prompt's last token is the first of a tree
+    if rest:
+        model(model.embeddings[prompt[:, :rest].reshape(-1)], begin * rest, rest, rest)
     generator = torch.Generator(device="cuda")
-    tokens, parents = drafts(model, prompt[a.prompt - 1::a.prompt].int(), fan, generator)
+    tokens, parents = drafts(model, prompt[:, rest].int(), fan, generator)
     uniform, total = torch.rand(a.seqs * each, device="cuda"), torch.zeros(a.seqs, dtype=torch.int32, device="cuda")
 
     def step():
