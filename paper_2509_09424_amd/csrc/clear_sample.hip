@@ -119,10 +119,10 @@ struct SampleRow {
     float t, p, m, u;
     int k;
     // weights
-    float top;             // the largest value
+    float top, half_top;   // the largest value, and half of it
     double rate;           // y = (x - top) rate, 512 to a power of two
     int shift;             // S
-    float bins;            // to a unit of distance
+    float bins;            // to two units of distance
     // kept so far: values above `edge`, and of the equal ones those up to index `last`
     float edge, small;     // small: the smallest value that min_p leaves
     int last;
@@ -158,7 +158,8 @@ struct SampleRow {
         const int bits = 32 - __clz(vocab);
         shift = min(50, 62 - bits);
         rate = 512 / LN2 / (double)t;
-        bins = fminf((float)rate * (SAMPLE_BINS / 512) / (float)(shift + 2), 3e38f);  // 2^-(S + 2) after the last
+        half_top = 0.5f * top;
+        bins = fminf((float)rate * (SAMPLE_BINS / 256) / (float)(shift + 2), 3e38f);  // 2^-(S + 2) after the last
         if (m > 0) {
             // min_p keeps values from some place on: found by all lanes, a 64th of what is left at a time
             const double least = 512 * log2((double)fminf(m, 1.0f));
@@ -279,8 +280,10 @@ struct SampleRow {
         weights<1>(w, v, in);
         return w[0] - NO_WEIGHT;
     }
-    // Bins over the distance to the largest value: what lies beyond the last has no weight
-    __device__ __forceinline__ int bin(float f) const { return (int)fminf((top - f) * bins, (float)SAMPLE_BINS); }
+    // Bins over the distance to the largest value: what lies beyond the last has no weight.  Half of the distance stays in range where the logits are at both ends of 32 bits, and at high
+    // temperatures what lies that far off has a weight.
+    __device__ __forceinline__ float half_distance(float f) const { return __builtin_fmaf(-0.5f, f, half_top); }
+    __device__ __forceinline__ int bin(float f) const { return (int)fminf(half_distance(f) * bins, (float)SAMPLE_BINS); }
 
     // ---- over the workgroup
     __device__ __forceinline__ u64 total(u64 v) const {
@@ -646,7 +649,7 @@ struct SampleRow {
     template <bool COUNTS>
     __device__ __forceinline__ void bound_listed(u64 target, int from, int to) {
         const float finer = (float)SAMPLE_BINS / (to + 1 - from);
-        const auto bin_of = [&](u32 key) { return max(0, min((int)(((top - of_key(key)) * bins - from) * finer), SAMPLE_BINS - 1)); };
+        const auto bin_of = [&](u32 key) { return max(0, min((int)((half_distance(of_key(key)) * bins - from) * finer), SAMPLE_BINS - 1)); };
         const auto by_value = [&](const auto &todo) {
             each_listed([&](u32 key, u32 i) { todo(bin_of(key), (u64)key << 32 | ~i, [&] { return weight(of_key(key)); }); });
         };
