@@ -581,7 +581,7 @@ typedef struct ensi_clear_accept_args {
 } ensi_clear_accept_args;
 int ensi_clear_accept(ensi_ctx *ctx, const ensi_clear_accept_args *args, void *stream);
 
-/* Moves the accepted tokens together, in the caches of any number of layers, which have pages of one size: the new token path[i][j] of sequence i, j < count[i], comes to place lengths[i] + j (lengths
+/* Moves the accepted tokens together, in the caches of any number of layers (up to 1024), which have pages of one size and no memory in common: the new token path[i][j] of sequence i, j < count[i], comes to place lengths[i] + j (lengths
  * and begin are those of the step).  The scale of a block of 16 that tokens come to is the largest scale that its tokens had, those that stay where they are among
  * them; codes whose scale was smaller are rounded again.  Codes behind the last accepted token that nothing comes to are left as they are.  A path that does not ascend
  * within the new tokens, or a page outside the cache, leaves the sequence out. */
@@ -592,7 +592,7 @@ typedef struct ensi_clear_keep_args {
 } ensi_clear_keep_args;
 int ensi_clear_keep(ensi_ctx *ctx, ensi_kv *const *kv, int32_t caches, const ensi_clear_keep_args *args, void *stream);
 
-/* Rows that continue sequences, in the caches of any number of layers, which have pages of one size: row i has the length of sequence source[i] and the same full pages; a page that is begun
+/* Rows that continue sequences, in the caches of any number of layers as above: row i has the length of sequence source[i] and the same full pages; a page that is begun
  * is copied, as far as it is in use, to page fresh[i], which stands in its place (the next append's, where none is begun).  What follows in table_out is -1.  fresh[i] may be the
  * begun page itself (the row goes on in it), or -1 where no page is begun; other than that it must be a page that none of the sequences has: this is not
  * checked, but a page given to two rows is, and the later row left out.  A row that is left out has length 0 and no pages.

@@ -810,7 +810,7 @@ class Context:
         return path, count, following
 
     def clear_keep(self, caches, table, begin, lengths, path, count, max_new=None, stream=None):
-        """Moves the accepted tokens of a step together in a cache, or in those of all layers (a list; pages of one size): new token path[i][j] of sequence i, j < count[i], to place
+        """Moves the accepted tokens of a step together in a cache, or in those of all layers (a list; pages of one size, no memory in common): new token path[i][j] of sequence i, j < count[i], to place
         lengths[i] + j.  A block of 16 that tokens come to has the largest scale of its tokens, the others are rounded again.  begin and lengths as for clear_append, from before
         the step; path int32 [seqs][max_new], count int32 [seqs] as clear_accept makes them."""
         at, stream = self._on(stream)

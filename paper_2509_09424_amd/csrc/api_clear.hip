@@ -1,6 +1,7 @@
 // C ABI of the decoder layer on clear activations: argument checks, handles; the kernels are in clear_*.hip.
 #include <math.h>
 
+#include <algorithm>
 #include <new>
 
 #include "api_util.h"
@@ -339,15 +340,22 @@ extern "C" int ensi_clear_accept(ensi_ctx *ctx, const ensi_clear_accept_args *a,
     return ENSI_OK;
 }
 
-// The caches of a call: this context's, with pages of one size, each of them once.
+// The caches of a call: this context's, with pages of one size, no array of one within another's: waves and workgroups of different caches have no order between them.
 static int check_caches(ensi_ctx *ctx, const char *who, ensi_kv *const *kv, int caches) {
     if (!kv || caches < 1 || caches > CLEAR_MAX_CACHES) ENSI_FAIL(ctx, kv ? ENSI_E_SHAPE : ENSI_E_BADARG, "%s: %d caches (1 to %d)", who, caches, CLEAR_MAX_CACHES);
+    struct Range {
+        uintptr_t from, to;
+    } ranges[4 * CLEAR_MAX_CACHES];
     for (int i = 0; i < caches; i++) {
         if (!kv[i] || kv[i]->ctx != ctx) ENSI_FAIL(ctx, ENSI_E_BADARG, "%s: no cache, or that of another context", who);
         if (kv[i]->view.page != kv[0]->view.page) ENSI_FAIL(ctx, ENSI_E_SHAPE, "%s: caches with pages of %d and of %d tokens", who, kv[0]->view.page, kv[i]->view.page);
-        for (int j = 0; j < i; j++)
-            if (kv[i]->view.k == kv[j]->view.k) ENSI_FAIL(ctx, ENSI_E_BADARG, "%s: a cache is there twice", who);
+        const CacheSpans spans(kv[i]->view);
+        for (int j = 0; j < 4; j++) ranges[4 * i + j] = {spans.part[j].from, spans.part[j].to};
     }
+    if (caches == 1) return ENSI_OK;  // (one cache's arrays are apart: it was wrapped so)
+    std::sort(ranges, ranges + 4 * caches, [](const Range &a, const Range &b) { return a.from < b.from; });
+    for (int i = 1; i < 4 * caches; i++)
+        if (ranges[i].from < ranges[i - 1].to) ENSI_FAIL(ctx, ENSI_E_BADARG, "%s: a cache is there twice, or arrays of two caches overlap", who);
     return ENSI_OK;
 }
 
