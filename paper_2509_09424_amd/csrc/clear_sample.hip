@@ -10,7 +10,7 @@
 //   top_k: counts in 2048 bins over the distance to the largest value show up to which bin the first k reach; for a small k the largest values of the threads do (the k-th of them
 //          is not above the row's k-th);
 //   top_p of all tokens: sums in these bins show in which one the bound lies; what is above it is kept.
-// Where there are more candidates than room (flat rows, thousands of equal logits) the bound is found in the row itself, by bins over the bits of the values where it lies.
+// Where there are more candidates than room (flat rows, thousands of equal logits, k near 4096 in rows of less than six workgroups, or above) the bound is found in the row itself, by bins over the bits of the values where it lies.
 //
 // What bounds it: latencies in short rows (32000 logits in bf16: 6 us greedy, 9.6 with top_k, 13 with none of the filters, 29 with top_p alone); in many long ones the passes over memory, three of
 // them in four launches (256 rows of 128003 in f32: 21 us a pass, 45 greedy, 55 with top_k = 50, 61 with no filter), and 64-bit arithmetic (112 with top_p alone, where each weight is formed twice).
@@ -21,16 +21,18 @@
 #define SAMPLE_BINS 2048
 #define SAMPLE_SEGMENTS 512  // of a row: one wave looks through one of them at the end
 #define SAMPLE_LIST 4096     // candidates
+#define SAMPLE_LONG 8192     // of a row that six workgroups or more share
 #define SAMPLE_PAIRS 256     // candidates that are compared each with each (64 rows of 128000, top 50 and top_p as arrays: 29 us, in bins 35; one of 32000 9.3 and 13.3)
 #define SAMPLE_FEW 512       // top_k up to which the threads' largest values choose the candidates (256 rows, top 50: 55 us, with counts of all values 78; 64 rows 26 and 32)
 #define SAMPLE_PARTS 8       // workgroups to a row
 #define LN2 0.69314718055994530942
 
+template <int LIST>
 struct SampleLds {
     double roots[512];     // 2^(k / 512)
     u64 sum[SAMPLE_BINS];  // of the bins, of the segments of a row, or the candidates' weights
     u32 count[SAMPLE_BINS];
-    u64 list[SAMPLE_LIST];  // bits of the value in their order, and inverted index: the order of the filters is the falling one of these
+    u64 list[LIST];  // bits of the value in their order, and inverted index: the order of the filters is the falling one of these
     u64 part[SAMPLE_WAVES];
     u32 low[SAMPLE_WAVES], high[SAMPLE_WAVES];
     int found, listed, few;
@@ -40,7 +42,7 @@ struct SampleLds {
 
 // What the workgroups of a row leave for each other, in the workspace
 struct SampleShared {
-    u64 bins[SAMPLE_BINS], sum[SAMPLE_SEGMENTS], list[SAMPLE_LIST];
+    u64 bins[SAMPLE_BINS], sum[SAMPLE_SEGMENTS], list[SAMPLE_LONG];
     float most[SAMPLE_PARTS], threads[SAMPLE_PARTS * SAMPLE_THREADS];  // the largest values of the parts, and of their threads
     int first[SAMPLE_PARTS];
     int listed, border;  // the bin of top_p's bound, and what is left there of its target
@@ -107,12 +109,12 @@ enum SampleMode { SAMPLE_NONE, SAMPLE_FIRST, SAMPLE_TOP, SAMPLE_PART, SAMPLE_ALL
 __device__ __forceinline__ u32 larger(u32 a, u32 b) { return __builtin_bit_cast(u32, __builtin_elementwise_maximum(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b))); }
 
 // HELD: a row of up to 64 tiles stays in registers, four tiles to a wave
-template <int TYPE, bool HELD>
+template <int TYPE, bool HELD, int LIST = SAMPLE_LIST>
 struct SampleRow {
     typedef typename Elem<TYPE>::type T;
     static constexpr int E = TYPE == ENSI_T_F32 ? 4 : 8, TILE = 64 * E, AHEAD = 2;  // elements of a lane and of a wave; tiles under way (four: 1 to 3 % slower)
     typedef T vec __attribute__((ext_vector_type(E), aligned(sizeof(T))));
-    SampleLds &lds;
+    SampleLds<LIST> &lds;
     const T *x;
     int vocab, tiles, per;  // tiles of a row, tiles to a segment
     int lane, wave;
@@ -128,7 +130,7 @@ struct SampleRow {
     int last;
     vec held0, held1, held2, held3;
 
-    __device__ __forceinline__ SampleRow(const ensi_clear_sample_args &a, int64_t row, SampleLds &l) : lds(l) {
+    __device__ __forceinline__ SampleRow(const ensi_clear_sample_args &a, int64_t row, SampleLds<LIST> &l) : lds(l) {
         x = (const T *)a.logits + row * a.stride;
         vocab = a.vocab;
         tiles = (vocab + TILE - 1) / TILE;
@@ -420,7 +422,7 @@ struct SampleRow {
             const int b = bin(f[i]);
             if (b >= low && b <= high) {
                 const int n = atomicAdd(&lds.listed, 1);
-                if (n < SAMPLE_LIST) lds.list[n] = (u64)key_of(f[i]) << 32 | ~(u32)(at + i);
+                if (n < LIST) lds.list[n] = (u64)key_of(f[i]) << 32 | ~(u32)(at + i);
             }
         }
     }
@@ -776,7 +778,7 @@ struct SampleRow {
 // A workgroup to a row
 template <int TYPE, bool HELD>
 __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample(ensi_clear_sample_args a) {
-    __shared__ SampleLds lds;
+    __shared__ SampleLds<SAMPLE_LIST> lds;
     __shared__ u64 above[SAMPLE_SEGMENTS];
     SampleRow<TYPE, HELD> r(a, blockIdx.x, lds);
     r.set_roots();
@@ -862,7 +864,7 @@ __device__ __forceinline__ u64 find_part(const ROW &r, const SampleShared &row, 
 
 template <int TYPE>
 __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_most(SampleParts s) {
-    __shared__ SampleLds lds;
+    __shared__ SampleLds<SAMPLE_LIST> lds;
     SampleShared &row = s.row[blockIdx.y];
     const SampleRow<TYPE, false> r(s.a, blockIdx.y, lds);
     const SampleRange<SampleRow<TYPE, false>> g(r, s.parts, blockIdx.x);
@@ -875,7 +877,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_most(SamplePart
 }
 template <int TYPE>
 __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_bins(SampleParts s) {
-    __shared__ SampleLds lds;
+    __shared__ SampleLds<SAMPLE_LIST> lds;
     SampleShared &row = s.row[blockIdx.y];
     SampleRow<TYPE, false> r(s.a, blockIdx.y, lds);
     const SampleRange<SampleRow<TYPE, false>> g(r, s.parts, blockIdx.x);
@@ -900,7 +902,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_bins(SamplePart
 }
 template <int TYPE>
 __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_gather(SampleParts s) {
-    __shared__ SampleLds lds;
+    __shared__ SampleLds<SAMPLE_LIST> lds;
     __shared__ int at;
     SampleShared &row = s.row[blockIdx.y];
     SampleRow<TYPE, false> r(s.a, blockIdx.y, lds);
@@ -934,15 +936,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_gather(SamplePa
         r.sums_above(g.segment0, g.segment1, row.sum, border);
     }
     const int listed = lds.listed;
-    if (threadIdx.x == 0) at = atomicAdd(&row.listed, listed);  // (past the list's end where there are too many)
+    if (threadIdx.x == 0) at = atomicAdd(&row.listed, listed <= SAMPLE_LIST ? listed : SAMPLE_LONG + 1);  // (past the list's end where there are too many, of this part or of all)
     __syncthreads();
-    for (int i = threadIdx.x; i < min(listed, SAMPLE_LIST) && at + i < SAMPLE_LIST; i += SAMPLE_THREADS) row.list[at + i] = lds.list[i];
+    for (int i = threadIdx.x; i < min(listed, SAMPLE_LIST) && at + i < SAMPLE_LONG; i += SAMPLE_THREADS) row.list[at + i] = lds.list[i];
 }
-template <int TYPE>
+template <int TYPE, int LIST>
 __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_finish(SampleParts s) {
-    __shared__ SampleLds lds;
+    __shared__ SampleLds<LIST> lds;
     SampleShared &row = s.row[blockIdx.x];
-    SampleRow<TYPE, false> r(s.a, blockIdx.x, lds);
+    SampleRow<TYPE, false, LIST> r(s.a, blockIdx.x, lds);
     SampleMode mode = begin_part(r, row, s.parts);
     int token = -1;
     r.set_roots();
@@ -952,7 +954,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void k_clear_sample_finish(SamplePa
     }
     if (mode == SAMPLE_TOP || mode == SAMPLE_PART) {
         const int listed = row.listed;
-        if (listed <= SAMPLE_LIST) {
+        if (listed <= LIST) {
             for (int i = threadIdx.x; i < listed; i += SAMPLE_THREADS) lds.list[i] = row.list[i];
             if (threadIdx.x == 0) lds.listed = listed;
             if (mode == SAMPLE_TOP && listed <= SAMPLE_PAIRS) {
@@ -989,7 +991,7 @@ static void sample_type(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStrea
     // two, 110 whole).  A row that the registers of one workgroup hold stays there between the passes (32000: 9.7 us, 10.2 without).
     int parts = (int)min((int64_t)SAMPLE_PARTS, 1024 / a.rows);
     parts = min(parts, a.vocab / (2 * SAMPLE_THREADS * E));
-    if (a.rows * sizeof(SampleShared) > CLEAR_WS_FLOATS * 4) parts = 1;
+    static_assert(512 * sizeof(SampleShared) <= CLEAR_WS_FLOATS * 4, "rows that are split are 512 at most");
     ScopedTimer timer(ctx, "k_clear_sample", st);
     if (parts < 2 || !ctx->ws_clear) {
         if (a.vocab <= 64 * TILE) hipLaunchKernelGGL((k_clear_sample<TYPE, true>), dim3((u32)a.rows), block, 0, st, a);
@@ -1003,7 +1005,10 @@ static void sample_type(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStrea
     const bool few = !a.temperature && a.all_temperature > 0 && !a.top_k && a.all_top_k > 0 && a.all_top_k <= SAMPLE_FEW * parts && a.all_top_k < a.vocab;
     if (!few) hipLaunchKernelGGL(k_clear_sample_bins<TYPE>, grid, block, 0, st, s);
     if (a.top_k || a.top_p || a.all_top_k > 0 || a.all_top_p < 1) hipLaunchKernelGGL(k_clear_sample_gather<TYPE>, grid, block, 0, st, s);
-    hipLaunchKernelGGL(k_clear_sample_finish<TYPE>, dim3((u32)a.rows), block, 0, st, s);
+    // The k-th of T largest values of threads leaves T ln(T / (T - k)) candidates on the average, 1.4 k of them for the largest k that is looked for there: from six workgroups on more than
+    // SAMPLE_LIST, which two rows to a CU have room for; rows that so many share are one to a CU.  (One row of 131072, top 3584: 37 us, 174 where the row itself is searched; 128 rows 70 and 209.)
+    if (SAMPLE_FEW * parts * 1.5f > SAMPLE_LIST) hipLaunchKernelGGL((k_clear_sample_finish<TYPE, SAMPLE_LONG>), dim3((u32)a.rows), block, 0, st, s);
+    else hipLaunchKernelGGL((k_clear_sample_finish<TYPE, SAMPLE_LIST>), dim3((u32)a.rows), block, 0, st, s);
 }
 
 void launch_clear_sample(ensi_ctx *ctx, const ensi_clear_sample_args &a, hipStream_t st) {
