@@ -18,7 +18,7 @@ static int current_device(ensi_ctx *ctx) {
     if (hipGetDevice(&cur) != hipSuccess || cur != ctx->device) ENSI_FAIL(ctx, ENSI_E_HIP, "the context's device is not current");
     return ENSI_OK;
 }
-// The workspace of the clear calls, made with the first cache or the first weights of a context.
+// The workspace of the clear calls, made with the first cache, weights or sampling call of a context.
 static int clear_workspace(ensi_ctx *ctx) {
     if (ctx->ws_clear) return ENSI_OK;
     hipError_t e = ctx->pool->alloc((void **)&ctx->ws_clear, CLEAR_WS_FLOATS * sizeof(float));
@@ -307,10 +307,10 @@ extern "C" int ensi_clear_sample(ensi_ctx *ctx, const ensi_clear_sample_args *a,
         ENSI_FAIL(ctx, ENSI_E_BADARG, "clear sample: out overlaps an input");
     if (int rc = current_device(ctx)) return rc;
     // Rows are split over workgroups where there is a workspace; the first call of a context makes it, unless it is captured or there is no memory: without one
-    // the tokens are the same.
-    if (!ctx->ws_clear) {
+    // the tokens are the same.  It is asked for once: an allocation that fails takes as long as the call, or more (the next cache or weights try again).
+    if (!ctx->ws_clear && !ctx->ws_clear_refused) {
         hipStreamCaptureStatus capture = hipStreamCaptureStatusActive;
-        if (hipStreamIsCapturing((hipStream_t)stream, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone) (void)clear_workspace(ctx);
+        if (hipStreamIsCapturing((hipStream_t)stream, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone) ctx->ws_clear_refused = clear_workspace(ctx) != ENSI_OK;
         (void)hipGetLastError();
     }
     launch_clear_sample(ctx, *a, (hipStream_t)stream);

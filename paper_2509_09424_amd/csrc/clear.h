@@ -147,6 +147,7 @@ inline void clear_lds(ensi_ctx *ctx, const void *kernel, int bytes) {
     if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess && ctx->clear_lds_n < CLEAR_LDS_KERNELS) ctx->clear_lds[ctx->clear_lds_n++] = kernel;
 }
 
-// Workspace of the clear calls: partial results of keys split over workgroups (attention), aligned copies of codes (matmul).  One allocation of fixed size, made
-// with the first cache or weights of a context and never moved, so that calls allocate nothing and a captured graph's pointers stay good.
+// Workspace of the clear calls: partial results of keys split over workgroups (attention), aligned copies of codes (matmul), what the workgroups of a row leave for each other
+// (sampling).  One allocation of fixed size, made with the first cache, weights or sampling call of a context and never moved, so that other calls allocate nothing and a captured graph's
+// pointers stay good.
 #define CLEAR_WS_FLOATS ((size_t)16 << 20)

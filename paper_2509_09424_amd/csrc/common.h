@@ -310,7 +310,8 @@ struct ensi_ctx {
     u64 sampler_ctr = 0;
     void *static_scratch = nullptr;  // this device's copy of the statically linked workspace (api_static.hip)
     size_t static_scratch_bytes = 0;
-    float *ws_clear = nullptr;   // workspace of the calls on clear activations: fixed size, made with the first cache or weights
+    float *ws_clear = nullptr;   // workspace of the calls on clear activations: fixed size, made with the first cache, weights or sampling call
+    bool ws_clear_refused = false;  // a sampling call found no memory for it
     const void *clear_lds[CLEAR_LDS_KERNELS];  // of their kernels, those whose limit of dynamic LDS is raised
     int clear_lds_n = 0;
     StageSlot stage[ENSI_STAGE_SLOTS];
