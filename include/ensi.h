@@ -544,7 +544,8 @@ int ensi_clear_attention(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_
  * The two calls above for a tree: new token t is stored at place lengths[i] + t of its sequence; its position, for the rotation and the window, is
  * lengths[i] + the number of its ancestors; it sees the lengths[i] tokens before, its ancestors and itself, with window > 0 those at the last `window` positions.  `positions`
  * of the append and max_length of the attention bound positions and places in turn; of the attention's rows without a key in the cache and with nothing but -inf it holds
- * what is said above. */
+ * what is said above.  A block of 16 has one scale for drafts and others: one that drafts raise stays when they are not kept, and the tokens before them in the block are rounded to it, so
+ * the cache may differ by a rounding of its 8 bits from that of the same tokens decoded one at a time. */
 #define ENSI_KV_BAD_TREE 4 /* parents or a path that do not fit: the sequence was left out */
 int ensi_clear_append_tree(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_append_args *args, const int32_t *parents, void *stream);
 int ensi_clear_attention_tree(ensi_ctx *ctx, ensi_kv *kv, const ensi_clear_attention_args *args, const int32_t *parents, void *stream);

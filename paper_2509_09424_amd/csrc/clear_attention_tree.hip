@@ -3,7 +3,7 @@
 //
 // A sequence has up to 64 new tokens, so one word of 64 bits holds what a row sees of them, and the rows of a sequence and key head read the same long cache.  Two kernels: up to
 // 64 rows (a few tokens each) are bound by the cache's bytes, so a workgroup takes 16 or 32 of them and its four waves a quarter of its keys each, a tile of 32 widened once for all
-// of a wave's rows and the next one under way (48 sequences of 8 tokens behind up to 8191 on 20 over 5 heads of 128: 223 MB in 66 us); more rows are bound by vector
+// of a wave's rows and the next one under way (48 sequences of 8 tokens behind up to 8191 on 20 over 5 heads of 128: 223 MB in 62 us, and the join 6); more rows are bound by vector
 // instructions, and share keys that are widened once for 128 of them.  Either splits long caches over workgroups; a third kernel joins the parts.
 #include "clear_attention.h"
 
@@ -385,8 +385,9 @@ __global__ __launch_bounds__(256) void k_clear_attention_tree(AttentionView a, c
 }
 
 // Many rows: 128 of them to a workgroup, 32 to a wave, and tiles of 64 keys widened once for all of them in LDS (RowsLds; a wave fetches and widens a block of 16 keys and values while
-// the tile before is computed).  Widening a tile in every wave takes a third of the kernel above's vector instructions: 64 sequences of 64 tokens behind 300 on 20 over 5 heads of
-// 128 59 us there, 37 here; 16 behind 2048 60 and 47.  What bounds it: vector instructions (exponentials, reciprocals and conversions take four times an ordinary one's cycles) and rounds of workgroups.
+// the tile before is computed).  Widening a tile in every wave takes a third of the kernel above's vector instructions: 64 sequences of up to 64 tokens behind up to 300 on 20 over 5 heads of
+// 128 59 us there, 37 here; 16 behind 2048 60 and 47.  What bounds it: 64 sequences of 64 tokens behind 300 each (47 us) are 640 workgroups on 512 places, 1.2 waves a SIMD of 2 on the average;
+// vector instructions have 32 % of the SIMDs' cycles, matrix ones 18 %, LDS 16 % of the CUs'.
 template <int TYPE, int DIM, int SCORE>
 __global__ __launch_bounds__(256, DIM <= 128 ? 2 : 1) void k_clear_attention_tree_rows(AttentionView a, const int32_t *parents, int split_tiles) {
     typedef typename Elem<TYPE>::type T;
@@ -760,10 +761,11 @@ static void tree_go(ensi_ctx *ctx, AttentionView v, const int32_t *parents, hipS
     const int width = by_rows ? 8 : rt;  // tiles of 16 rows to a workgroup
     const int64_t base = (int64_t)v.s.seqs * heads * ((v.row_tiles + width - 1) / width);
     // Parts of a row's keys.  A CU has room for two workgroups, for one from 192 places on.  Keys of one length, of one sequence or within a window: as many parts as fill that room once.
-    // Sequences of different lengths, of which only the longest is known here: half as many again, and parts of up to 40 tiles.  Each part is also written and read again, so there are no
-    // more than 1.6 sqrt(tiles), where turns of a wave and parts of a row cost about the same.  Against four turns a workgroup wherever CUs stand idle, and otherwise parts of 12 to 32 tiles: one sequence
-    // of 16 tokens behind 4096 on 20 over 5 heads of 128 19 -> 16 us; 48 behind up to 1000 36 -> 25; 48 of 8 tokens behind up to 8191 64 -> 59; 16 of 64 tokens with a window of 2048 on 16 heads
-    // of 96 63 -> 54; 8 behind up to 4096 on 16 over 4 heads of 256 84 -> 66 (and on 32 over 4 heads of 64 43 -> 47).
+    // Sequences of different lengths, of which only the longest is known here: 9/16 more.  Each part is also written and read again, so there are no more than 1.6 sqrt(tiles), where turns of a
+    // wave and parts of a row cost about the same; but of different lengths at least tiles / 40, rounded down (the tiles of a part are rounded up to fours).
+    // Against four turns a workgroup wherever CUs stand idle, and otherwise parts of 12 to 32 tiles: one sequence
+    // of 16 tokens behind 4096 on 20 over 5 heads of 128 19 -> 16 us; 48 behind up to 1000 36 -> 25; the kernel of 48 of 8 tokens behind up to 8191 66 -> 62; 16 of 64 tokens with a window of 2048 on 16
+    // heads of 96 63 -> 54; 8 behind up to 4096 on 16 over 4 heads of 256 84 -> 66 (and on 32 over 4 heads of 64 43 -> 47).
     const int room_for = v.kv.dim <= 128 ? 512 : 256;
     const bool even = v.s.seqs == 1 || span < v.max_length;
     int splits = (int)min((int64_t)(even ? room_for : room_for + room_for * 9 / 16) / base, (int64_t)sqrtf(2.56f * tiles));

@@ -1,6 +1,6 @@
 // Tokens from rows of logits: temperature, top-k, top-p and min-p, with given random numbers.
 //
-// Weights are whole multiples of 2^-S of the row's largest one, S as large as sums of the vocabulary leave room for in 64 bits (45 for 2^17 tokens): sums are then exact, do
+// Weights are whole multiples of 2^-S of the row's largest one, S as large as sums of the vocabulary leave room for in 62 bits (45 for 128000 tokens): sums are then exact, do
 // not hang on their order or on how a row is split, and compare with top_p and the random number as they are.  exp in 64 bits: 2^(y / 512) = 2^(k / 512) 2^(r / 512) with k the
 // nearest whole number, 512 values of the first in LDS, three terms of the second beside its 1 (2^-46 of it are left out), and the addition of 2^52 rounds to a whole number of
 // units.  That is about 24 instructions, 8 of them in 64 bits: 5 us for 32000 weights on one CU.
